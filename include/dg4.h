@@ -50,10 +50,12 @@ enum {
     DG4_FLAG_RESIDUAL = 1,     /* output projection adds the layer's input row                */
     DG4_FLAG_LEVEL_LAUNCHES = 2, /* levelised layer: one group of kernel launches per level instead of the
                                   single persistent kernel (same results; kept for comparison)   */
-    DG4_FLAG_FUSED_LAYER = 4   /* all-parallel layer: the K|V projection followed by ONE kernel (queries from
+    DG4_FLAG_FUSED_LAYER = 4,  /* all-parallel layer: the K|V projection followed by ONE kernel (queries from
                                   the X tiles, attention, output projection, residual; Q and O never reach
                                   memory) instead of three kernels.  Same results bit for bit; measured a
                                   little slower to equal, so it is not the default.  bf16, two hops at most */
+    DG4_FLAG_RMS_NORM = 8      /* dg4_norm_gate_fwd: both norms divide by the root mean square (no mean is taken
+                                  off) instead of being layer normalisations                     */
 };
 
 /* Per-call description of the attention layer. */
@@ -408,6 +410,106 @@ dg4_status dg4_blocks_fwd_levelised(const dg4_graph* g, const dg4_desc* desc, vo
                                     const float* const* b2, const float* const* ln2_gamma,
                                     const float* const* ln2_beta, float eps, int32_t d_ff, void* workspace,
                                     size_t workspace_bytes, void* stream);
+
+/*
+ * ---- Serving many requests in one batch --------------------------------------------------------------------------
+ *
+ * One handle can carry the circuits of many requests side by side (a disjoint union: each request's nodes are a run
+ * of consecutive ids).  The calls below serve such a batch: the shared projections with a low-rank adapter per
+ * request, the residual's gate per request, and keys and values held in 8 bits.  The paper has no counterpart.
+ * They enqueue on `stream`, allocate nothing, keep nothing between calls and can be captured; calls on different
+ * streams are independent.  Lists, offsets and ids on the device are not validated by the host: ids out of range
+ * are treated as stated below, and no value of them leads outside the tensors.
+ */
+
+/* Which rows belong to which request.  Rows before seg_ptr[0] and from seg_ptr[n_seg] on belong to none: the calls
+ * leave those rows of their outputs as they are. */
+typedef struct {
+    int32_t n_seg;             /* >= 1                                                        */
+    const int32_t* seg_ptr;    /* device, [n_seg + 1], non-decreasing row offsets; equal neighbours = an empty
+                                  request.  (Offsets that decrease: which rows are written, and for which
+                                  request, is unspecified.)                                   */
+    const int32_t* seg_id;     /* device, [n_seg]: the adapter (or gate) of each request; an id outside
+                                  0 .. n_adapters - 1 means none.  Requests may share one.     */
+} dg4_segments;
+
+/* Low-rank adapters of one projection, all of one rank (pad a smaller one with zero rows and columns). */
+typedef struct {
+    int32_t n_adapters;        /* >= 1                                                        */
+    int32_t rank;              /* a multiple of 8, 8 .. 64                                    */
+    const void* A;             /* device, [n_adapters, rank, d] bf16                          */
+    const void* B;             /* device, [n_adapters, n_out, rank] bf16 (n_out = 3d or d)    */
+    const float* scale;        /* device, [n_adapters] fp32                                   */
+} dg4_adapters;
+
+/*
+ * dg4_qkv_project and dg4_out_project with an adapter per request: for every row x of a request with adapter a
+ *     y = W x + scale_a * B_a (A_a x)   (+ the residual row),
+ * and y = W x (+ residual) for a request without one.  The products accumulate in fp32; scale_a * A_a x is rounded
+ * to bf16 between the two small products; y is rounded once.  An adapter's values (infinities and NaNs too) reach
+ * the rows of its own requests only.
+ * `segments` NULL: all rows are one request with adapter 0.  Other arguments as for the plain projections; the
+ * outputs must not overlap the inputs, except that H_out may be H_res (same leading dimension).
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype other than bf16; rank), CUDA; a device-side wait that runs out records
+ * DG4_ERR_TIMEOUT in the handle's status word.
+ */
+dg4_status dg4_qkv_project_adapters(const dg4_graph* g, const dg4_desc* desc, const void* X, int64_t ldx,
+                                    const void* W_qkv, const dg4_adapters* adapters, const dg4_segments* segments,
+                                    void* Q, int64_t ldq, void* K, int64_t ldk, void* V, int64_t ldv, void* stream);
+dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_desc* desc, const void* O, int64_t ldo,
+                                    const void* W_o, const dg4_adapters* adapters, const dg4_segments* segments,
+                                    const void* H_res, int64_t ldh, void* H_out, int64_t ldho, void* stream);
+
+/*
+ * Keys and values in 8 bits.  A table row of node v takes 288 bytes (DG4_KV8_ROW_BYTES), ldt bytes apart:
+ *     bytes 16 p .. 16 p + 7    codes of K[v, 8p .. 8p+7],  p = 0 .. 15
+ *     bytes 16 p + 8 .. + 15    codes of V[v, 8p .. 8p+7]
+ *     bytes 256 + 2 h, + 1      scale exponents of head h of K and of V, h < heads; the rest up to 288 is zero
+ * A code is an e4m3 number; code c under exponent byte b stands for c * 2^(b - 127).  b is the smallest value >= 0
+ * with max |x| <= 448 * 2^(b - 127) over the head's slice of the row, and codes are rounded to nearest, ties to even.
+ * A slice that holds an infinity or a NaN is stored as NaN throughout (b = 255, codes 0x7f).  heads <= 16.
+ *
+ * dg4_kv8_write: rows of K and V into the table.  dg4_kv8_read: the values the table stands for into rows of K and V
+ * (exact in fp32; in bf16 too unless they fall below its normal range).
+ *   T      device, [n, ldt] bytes, 16-byte aligned; ldt a multiple of 16, >= 288.  Must not overlap K or V
+ *   K, V   device, [n, d] of desc->dtype
+ *   nodes  device, [count] int32 or NULL: the nodes whose rows are written (the rows of others stay as they are);
+ *          ids outside 0 .. n - 1 are skipped, repeated ids are allowed.  NULL: all nodes (count 0 or n)
+ */
+#define DG4_KV8_ROW_BYTES 288
+dg4_status dg4_kv8_write(const dg4_graph* g, const dg4_desc* desc, const void* K, int64_t ldk, const void* V,
+                         int64_t ldv, void* T, int64_t ldt, const int32_t* nodes, int32_t count, void* stream);
+dg4_status dg4_kv8_read(const dg4_graph* g, const dg4_desc* desc, const void* T, int64_t ldt, void* K, int64_t ldk,
+                        void* V, int64_t ldv, const int32_t* nodes, int32_t count, void* stream);
+
+/*
+ * dg4_sparse_attn_fwd over the 8-bit table: the same formula with K and V the values the table stands for, fp32
+ * arithmetic, O rounded once.  For all nodes (nodes NULL) or for a list of them (a level, a single node); list,
+ * table and heads as above, cones of any depth.  O may be Q when there is no list (same leading dimension), and
+ * must not overlap T.
+ */
+dg4_status dg4_sparse_attn_kv8_fwd(const dg4_graph* g, const dg4_desc* desc, const void* Q, int64_t ldq, const void* T,
+                                   int64_t ldt, void* O, int64_t ldo, const int32_t* nodes, int32_t count,
+                                   void* stream);
+
+/*
+ * The norms after a sub-layer and before the next one, with the gate and the scaled residual between them:
+ *     R_out = res_scale * R + gate_a * Norm_post(S),     Y = Norm_pre(R_out)
+ * S the sub-layer's output, R the residual stream, gate_a the request's gate (a vector of d factors; ones for a
+ * request without one).  Norm(x) = (x - mean) / sqrt(var + eps) * gamma + beta as in dg4_layernorm_fwd, or with
+ * DG4_FLAG_RMS_NORM x / sqrt(mean(x^2) + eps) * gamma + beta.  fp32 arithmetic; Y is computed from R_out before that
+ * is rounded; each output is rounded once.
+ *   S, R, R_out, Y  device, [n, d] of desc->dtype.  Y may be NULL (R_out only; pre_gamma and pre_beta are then
+ *                   ignored).  R_out and Y may each be S or R (same leading dimension), but not one another
+ *   gate            device, [n_gates, d] fp32 or NULL (ones)
+ *   segments        NULL: all rows use gate 0 (n_gates must be 1)
+ *   gammas, betas   device, [d] fp32, 16-byte aligned; betas may be NULL (zeros)
+ */
+dg4_status dg4_norm_gate_fwd(const dg4_graph* g, const dg4_desc* desc, const void* S, int64_t lds, const void* R,
+                             int64_t ldr, float res_scale, const float* gate, int32_t n_gates,
+                             const dg4_segments* segments, const float* post_gamma, const float* post_beta,
+                             const float* pre_gamma, const float* pre_beta, float eps, void* R_out, int64_t ldro,
+                             void* Y, int64_t ldy, void* stream);
 
 /*
  * Diagnostic (the paper has no counterpart): launches one small CTA that waits, with the same bounded wait the

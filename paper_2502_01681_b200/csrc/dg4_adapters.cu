@@ -1,0 +1,596 @@
+// Shared projection with a low-rank adapter per request, on the 5th-generation tensor cores:
+//     Y = X W^T + U B_a^T (+ residual),    U = bf16(scale_a * X A_a^T),
+// K = 128, bf16 operands, fp32 accumulation in tensor memory.  U's rounding is that of any tensor-core operand: it
+// perturbs the adapter's contribution by at most 2^-8 of itself, as the rounding of y does to y.
+//
+// The work is cut into items: up to 128 consecutive rows of ONE request.  An item multiplies with its own adapter
+// only, and only its own rows are stored, so nothing is masked and no request's infinities or NaNs can meet
+// another's rows (0 * inf in a masked product would).  Each CTA takes a contiguous run of items, so neighbouring items mostly
+// share their adapter, which is fetched into shared memory only when it changes.
+//
+// One persistent CTA per SM, fourteen warps:
+//   warp 0       producer: W once, the item's rows of X (and of the residual) by TMA, the adapter when it changes; it
+//                alone walks the requests and passes each item on in a small ring of descriptors;
+//   warp 1       owns tensor memory, issues tcgen05.mma: U = X A^T first, then the base product of every 128-column
+//                block, then, once U stands in tensor memory as bf16, the products U B^T on top of the base blocks
+//                (A operand from tensor memory, B from shared memory);
+//   warps 2-9    epilogue: each owns 32 rows x 64 columns of a block; tensor memory -> bf16 -> its own 4 KB of
+//                staging -> TMA store, or 16-byte stores where the item ends inside the 32 rows;
+//   warps 10-13  U: tensor memory -> * scale -> bf16 -> tensor memory, while the base products run.
+// Bound by HBM: a QKV row is 256 bytes in, 768 out, and 98 + 1 r kflop (58 % of the machine's ratio at rank 64).
+// With few items (decoding: one row per request) the column blocks of an item go to different CTAs instead, so that
+// each fetches a third of W.
+//
+// Every mbarrier wait is bounded.  On expiry the kernel records DG4_ERR_TIMEOUT and raises an abort flag; every warp
+// leaves at its next item at the latest, without meeting others.  Then the producer waits for the copies it has started,
+// the MMA thread for its MMAs, the storing lanes for their stores, and only then is tensor memory freed.
+
+#include "dg4_internal.h"
+#include "dg4_sm100.cuh"
+
+#include <mutex>
+
+namespace {
+
+using namespace sm100;
+
+constexpr int kEpiWarps = 8, kUWarps = 4;
+constexpr int kThreads = 32 * (2 + kEpiWarps + kUWarps);
+constexpr int kTileM = 128;
+constexpr int kHalfBytes = 128 * 128;             // a 128-row x 64-column bf16 box
+constexpr int kTileBytes = 2 * kHalfBytes;
+constexpr int kMaxStages = 2;
+constexpr int kSlots = 3;                         // accumulator slots of 128 columns
+constexpr int kRing = 4;                          // item descriptors in flight
+constexpr int kTmemCols = 512;
+constexpr int kColU = kSlots * 128;               // U in fp32: 64 columns
+constexpr int kColUb = kColU + 64;                // U in bf16: 32 columns
+constexpr int kRankMax = 64;
+constexpr int kABytes = kRankMax * 256;           // A_a: two halves of rank rows x 128 bytes
+
+struct Item {
+    int32_t row0, rows;
+    int32_t adapter;          // -1: none
+    int32_t last;             // the next item uses another adapter (or there is none)
+};
+
+struct Bars {
+    uint64_t w_full;
+    uint64_t a_full[kMaxStages];
+    uint64_t a_empty[kMaxStages];
+    uint64_t r_empty[kMaxStages];
+    uint64_t acc_full[kSlots];
+    uint64_t acc_empty[kSlots];
+    uint64_t ad_full, ad_empty;     // the adapter in shared memory
+    uint64_t u_full, u_ready, ub_empty;
+    uint64_t item_full[kRing], item_empty[kRing];
+    uint64_t drain;
+    uint32_t tmem_base;
+    uint32_t abort_flag;
+    int32_t my_items;               // items of this CTA, and where they begin
+    int32_t first_seg, first_tile;
+    int64_t warp_sum[kThreads / 32];
+    Item ring[kRing];
+};
+
+struct Params {
+    const int32_t* seg_ptr;         // nullable: one request over all rows
+    const int32_t* seg_id;
+    const float* scale;
+    __nv_bfloat16* out[3]; int64_t ldo[3];
+    int32_t n, n_seg, n_adapters, rank;
+    int32_t n_out;                  // rows of W
+    int32_t nb;                     // column blocks per CTA (blockIdx.y picks the first one)
+    int32_t stages;                 // X (and residual) stages
+    int32_t off_a, off_b, off_x, off_r, off_stage, off_bar;
+    int32_t has_res;
+    int32_t* status;
+    uint32_t poll_limit;
+};
+
+struct OutMaps { CUtensorMap m[3]; };
+
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, const uint32_t* r) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t* r) {
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void st_global_v4(void* p, const uint32_t* r) {
+    asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&h);
+}
+__device__ __forceinline__ void raise_timeout(Bars* bars, int32_t* status) {
+    atomicExch(&bars->abort_flag, 1u);
+    if (status) atomicCAS(status, 0, (int)DG4_ERR_TIMEOUT);
+}
+
+// rows of request s, cut to the tensor: whatever the offsets hold, 0 <= lo <= hi <= n
+__device__ __forceinline__ void seg_rows(const Params& p, int s, int& lo, int& hi) {
+    lo = 0; hi = p.n;
+    if (p.seg_ptr) {
+        lo = min(max(p.seg_ptr[s], 0), p.n);
+        hi = max(lo, min(p.seg_ptr[s + 1], p.n));
+    }
+}
+__device__ __forceinline__ int seg_adapter(const Params& p, int s) {
+    const int id = p.seg_id ? p.seg_id[s] : 0;
+    return (uint32_t)id < (uint32_t)p.n_adapters ? id : -1;
+}
+
+// The walk over the items of a CTA, one request after the other (the producer's state).
+struct Walk {
+    int seg, lo, hi, adapter;
+    __device__ void open(const Params& p, int s, int tile) {
+        seg = s;
+        seg_rows(p, s, lo, hi);
+        lo += tile * kTileM;
+        adapter = seg_adapter(p, s);
+    }
+    __device__ void next(const Params& p) {             // to the next item, which exists
+        lo += kTileM;
+        while (lo >= hi && seg + 1 < p.n_seg) {
+            ++seg;
+            seg_rows(p, seg, lo, hi);
+            adapter = seg_adapter(p, seg);
+        }
+    }
+};
+
+// Cuts all items into one contiguous run per CTA: every thread counts the tiles of its share of the requests, the
+// CTA adds the counts up, and the thread in whose share this CTA's first item falls finds its place.
+__device__ __forceinline__ void find_items(const Params& p, Bars* bars) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int share = (p.n_seg + kThreads - 1) / kThreads;
+    const int64_t s0 = (int64_t)threadIdx.x * share;
+    const int64_t s1 = min(s0 + share, (int64_t)p.n_seg);
+    int64_t sum = 0;
+    for (int64_t s = s0; s < s1; ++s) {
+        int lo, hi;
+        seg_rows(p, (int)s, lo, hi);
+        sum += (hi - lo + kTileM - 1) / kTileM;
+    }
+    int64_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t below = __shfl_up_sync(0xffffffffu, (long long)incl, o);
+        if (lane >= o) incl += below;
+    }
+    if (lane == 31) bars->warp_sum[warp] = incl;
+    if (threadIdx.x == 0) { bars->my_items = 0; bars->first_seg = 0; bars->first_tile = 0; }
+    __syncthreads();
+    int64_t total = 0, before = incl - sum;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        const int64_t x = bars->warp_sum[w];
+        if (w < warp) before += x;
+        total += x;
+    }
+    const int64_t begin = total * blockIdx.x / gridDim.x, end = total * (blockIdx.x + 1) / gridDim.x;
+    if (end > begin && begin >= before && begin < before + sum) {
+        bars->my_items = (int32_t)(end - begin);
+        int64_t at = before;
+        for (int64_t s = s0; s < s1; ++s) {
+            int lo, hi;
+            seg_rows(p, (int)s, lo, hi);
+            const int64_t tiles = (hi - lo + kTileM - 1) / kTileM;
+            if (begin < at + tiles) {
+                bars->first_seg = (int32_t)s;
+                bars->first_tile = (int32_t)(begin - at);
+                break;
+            }
+            at += tiles;
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                    const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_a,
+                    const __grid_constant__ CUtensorMap map_b, const __grid_constant__ OutMaps map_o, Params p) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + p.off_bar);
+    const uint32_t sW = base, sA = base + p.off_a, sB = base + p.off_b, sX = base + p.off_x, sR = base + p.off_r;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nb = p.nb, block0 = blockIdx.y * p.nb, stages = p.stages;
+    const int rank16 = (p.rank + 15) & ~15;
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&bars->w_full), 1);
+        for (int s = 0; s < kMaxStages; ++s) {
+            mbar_init(smem_u32(&bars->a_full[s]), 1);
+            mbar_init(smem_u32(&bars->a_empty[s]), 1);
+            mbar_init(smem_u32(&bars->r_empty[s]), kEpiWarps);
+        }
+        for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&bars->acc_full[s]), 1); mbar_init(smem_u32(&bars->acc_empty[s]), kEpiWarps); }
+        mbar_init(smem_u32(&bars->ad_full), 1);
+        mbar_init(smem_u32(&bars->ad_empty), 1);
+        mbar_init(smem_u32(&bars->u_full), 1);
+        mbar_init(smem_u32(&bars->u_ready), kUWarps);
+        mbar_init(smem_u32(&bars->ub_empty), 1);
+        for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&bars->item_full[s]), 1); mbar_init(smem_u32(&bars->item_empty[s]), 1 + kEpiWarps + kUWarps); }
+        mbar_init(smem_u32(&bars->drain), 1);
+        bars->abort_flag = 0;
+        mbar_fence_init();
+        // W travels while the items are counted
+        mbar_expect_tx(smem_u32(&bars->w_full), (uint32_t)(nb * kTileBytes));
+        for (int j = 0; j < nb; ++j)
+            for (int h = 0; h < 2; ++h)
+                tma_load_2d(sW + (j * 2 + h) * kHalfBytes, &map_w, h * 64, (block0 + j) * 128, smem_u32(&bars->w_full));
+        tma_prefetch_desc(&map_x);
+        tma_prefetch_desc(&map_a);
+        tma_prefetch_desc(&map_b);
+        for (int j = 0; j < nb; ++j) tma_prefetch_desc(&map_o.m[block0 + j]);
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), kTmemCols);
+    __syncwarp();
+    find_items(p, bars);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;
+    const int items = bars->my_items;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ producer
+        if (lane == 0) {
+            int armed = 0, loads = 0;
+            Walk w;
+            if (items > 0) w.open(p, bars->first_seg, bars->first_tile);
+            int held = -1;                                     // the adapter in shared memory, -1 = released
+            for (int i = 0; i < items && !*abort_flag; ++i) {
+                Item it;
+                it.row0 = w.lo;
+                it.rows = min(w.hi - w.lo, kTileM);
+                it.adapter = w.adapter;
+                if (i + 1 < items) w.next(p);
+                it.last = i + 1 == items || w.adapter != it.adapter;
+                const int q = i % kRing, s = i % stages;
+                const uint32_t ph = (uint32_t)(i / stages) & 1u;
+                if (!mbar_wait(smem_u32(&bars->item_empty[q]), ((uint32_t)(i / kRing) & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                bars->ring[q] = it;
+                mbar_arrive(smem_u32(&bars->item_full[q]));
+                if (!mbar_wait(smem_u32(&bars->a_empty[s]), ph ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                if (p.has_res && !mbar_wait(smem_u32(&bars->r_empty[s]), ph ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                const uint32_t bar = smem_u32(&bars->a_full[s]);
+                mbar_expect_tx(bar, (uint32_t)(p.has_res ? 2 * kTileBytes : kTileBytes));
+                for (int h = 0; h < 2; ++h) {
+                    tma_load_2d(sX + s * kTileBytes + h * kHalfBytes, &map_x, h * 64, it.row0, bar);
+                    if (p.has_res) tma_load_2d(sR + s * kTileBytes + h * kHalfBytes, &map_r, h * 64, it.row0, bar);
+                }
+                armed = i + 1;
+                if (it.adapter >= 0 && it.adapter != held) {
+                    // the previous adapter's last products (load index `loads` - 1) must have read it
+                    if (!mbar_wait(smem_u32(&bars->ad_empty), ((uint32_t)loads & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                    const uint32_t ad = smem_u32(&bars->ad_full);
+                    mbar_expect_tx(ad, (uint32_t)(p.rank * 256 + nb * kHalfBytes));
+                    for (int h = 0; h < 2; ++h) tma_load_2d(sA + h * (kABytes / 2), &map_a, h * 64, it.adapter * p.rank, ad);
+                    for (int j = 0; j < nb; ++j)
+                        tma_load_2d(sB + j * kHalfBytes, &map_b, 0, it.adapter * p.n_out + (block0 + j) * 128, ad);
+                    ++loads;
+                    held = it.adapter;
+                }
+                if (it.last) held = -1;
+            }
+            // leave with no copy still landing in shared memory (these waits keep the default limit)
+            mbar_wait(smem_u32(&bars->w_full), 0);
+            for (int i = (armed > stages ? armed - stages : 0); i < armed; ++i)
+                mbar_wait(smem_u32(&bars->a_full[i % stages]), (uint32_t)(i / stages) & 1u);
+            if (loads > 0) mbar_wait(smem_u32(&bars->ad_full), (uint32_t)(loads - 1) & 1u);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            const uint32_t idesc = idesc_bf16_f32(128, 128), idesc_u = idesc_bf16_f32(128, rank16);
+            bool ok = mbar_wait(smem_u32(&bars->w_full), 0, p.poll_limit);
+            if (!ok) raise_timeout(bars, p.status);
+            int block = 0, loads = 0, u_items = 0;
+            bool fresh = true;                                 // the next adapter item brings a new adapter
+            for (int i = 0; i < items && ok && !*abort_flag; ++i) {
+                const int q = i % kRing, s = i % stages;
+                ok = mbar_wait(smem_u32(&bars->item_full[q]), (uint32_t)(i / kRing) & 1u, p.poll_limit);
+                if (!ok) { raise_timeout(bars, p.status); break; }
+                const Item it = bars->ring[q];
+                mbar_arrive(smem_u32(&bars->item_empty[q]));
+                const bool ad = it.adapter >= 0;
+                ok = mbar_wait(smem_u32(&bars->a_full[s]), (uint32_t)(i / stages) & 1u, p.poll_limit);
+                if (ok && ad && fresh) ok = mbar_wait(smem_u32(&bars->ad_full), (uint32_t)(loads++) & 1u, p.poll_limit);
+                if (!ok) { raise_timeout(bars, p.status); break; }
+                tc_fence_after();
+                const uint32_t x_base = sX + s * kTileBytes;
+                if (ad) {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)
+                        mma_bf16(tmem + kColU, smem_desc_sw128(x_base + (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32)),
+                                 smem_desc_sw128(sA + (uint32_t)((ks >> 2) * (kABytes / 2) + (ks & 3) * 32)), idesc_u, ks > 0 ? 1u : 0u);
+                    mma_commit(smem_u32(&bars->u_full));
+                }
+                for (int j = 0; j < nb; ++j) {
+                    const int slot = (block + j) % kSlots;
+                    ok = mbar_wait(smem_u32(&bars->acc_empty[slot]), ((uint32_t)((block + j) / kSlots) & 1u) ^ 1u, p.poll_limit);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t b_base = sW + j * kTileBytes;
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {
+                        const uint32_t off = (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32);
+                        mma_bf16(tmem + (uint32_t)(slot * 128), smem_desc_sw128(x_base + off), smem_desc_sw128(b_base + off), idesc, ks > 0 ? 1u : 0u);
+                    }
+                    if (!ad) mma_commit(smem_u32(&bars->acc_full[slot]));
+                }
+                if (!ok) { raise_timeout(bars, p.status); break; }
+                mma_commit(smem_u32(&bars->a_empty[s]));
+                if (ad) {
+                    ok = mbar_wait(smem_u32(&bars->u_ready), (uint32_t)(u_items++) & 1u, p.poll_limit);
+                    if (!ok) { raise_timeout(bars, p.status); break; }
+                    tc_fence_after();
+                    for (int j = 0; j < nb; ++j) {
+                        const int slot = (block + j) % kSlots;
+                        for (int ks = 0; ks < rank16 / 16; ++ks)
+                            mma_bf16_ta(tmem + (uint32_t)(slot * 128), tmem + (uint32_t)(kColUb + ks * 8),
+                                        smem_desc_sw128(sB + (uint32_t)(j * kHalfBytes + ks * 32)), idesc, 1u);
+                        mma_commit(smem_u32(&bars->acc_full[slot]));
+                    }
+                    mma_commit(smem_u32(&bars->ub_empty));
+                    fresh = it.last != 0;
+                    if (fresh) mma_commit(smem_u32(&bars->ad_empty));
+                }
+                block += nb;
+            }
+            mma_commit(smem_u32(&bars->drain));                // tensor memory is freed below: every MMA must be done
+            mbar_wait(smem_u32(&bars->drain), 0);
+        }
+    } else if (warp < 2 + kEpiWarps) {
+        // ------------------------------------------------------------------ epilogue (warps 2..9)
+        const int ew = warp - 2, quad = warp & 3, half = ew >> 2;
+        const uint32_t stage = base + p.off_stage + (uint32_t)(ew * 4096);
+        int block = 0;
+        bool ok = true;
+        for (int i = 0; i < items && ok; ++i) {
+            if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
+            const int q = i % kRing, s = i % stages;
+            if (!mbar_wait_warp(smem_u32(&bars->item_full[q]), (uint32_t)(i / kRing) & 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+            const Item it = bars->ring[q];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q]));
+            const int valid = it.rows - quad * 32;             // rows of the item among this warp's 32
+            for (int j = 0; j < nb; ++j, ++block) {
+                const int slot = block % kSlots;
+                ok = mbar_wait_warp(smem_u32(&bars->acc_full[slot]), (uint32_t)(block / kSlots) & 1u, p.poll_limit);
+                if (!ok) { raise_timeout(bars, p.status); break; }
+                tc_fence_after();
+                const uint32_t t_addr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * 128 + half * 64);
+                if (lane == 0) bulk_wait_read0();              // the previous store has read the staging rows
+                __syncwarp();
+#pragma unroll 1
+                for (int c2 = 0; c2 < 2; ++c2) {
+                    uint32_t acc[32], res[16];
+                    tmem_ld_32x32(t_addr + (uint32_t)(c2 * 32), acc);
+                    if (p.has_res) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            ld_shared_v4(sR + (uint32_t)(s * kTileBytes + half * kHalfBytes) + sw128_offset(quad * 32 + lane, c2 * 4 + c), res + 4 * c);
+                    }
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t out[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float lo = __uint_as_float(acc[c * 8 + 2 * e]), hi = __uint_as_float(acc[c * 8 + 2 * e + 1]);
+                            if (p.has_res) {
+                                lo += __uint_as_float(res[4 * c + e] << 16);
+                                hi += __uint_as_float(res[4 * c + e] & 0xffff0000u);
+                            }
+                            out[e] = pack_bf16(lo, hi);
+                        }
+                        st_shared_v4(stage + sw128_offset(lane, c2 * 4 + c), out);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&bars->acc_empty[slot]));
+                    if (p.has_res) mbar_arrive(smem_u32(&bars->r_empty[s]));
+                }
+                const int row0 = it.row0 + quad * 32;
+                if (valid >= 32) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d(&map_o.m[block0 + j], half * 64, row0, stage);
+                        bulk_commit();
+                    }
+                } else if (valid > 0) {
+                    // the item ends inside these rows: 8 lanes per row, four rows per instruction
+                    __nv_bfloat16* outp = p.out[block0 + j];
+                    const int64_t ldo = p.ldo[block0 + j];
+                    for (int r = lane >> 3; r < valid; r += 4) {
+                        uint32_t v[4];
+                        ld_shared_v4(stage + sw128_offset(r, lane & 7), v);
+                        st_global_v4(outp + (int64_t)(row0 + r) * ldo + half * 64 + (lane & 7) * 8, v);
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (lane == 0) bulk_wait_all();
+    } else {
+        // ------------------------------------------------------------------ U (warps 10..13)
+        const int quad = warp & 3;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        int u_items = 0;
+        for (int i = 0; i < items; ++i) {
+            if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
+            const int q = i % kRing;
+            if (!mbar_wait_warp(smem_u32(&bars->item_full[q]), (uint32_t)(i / kRing) & 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+            const Item it = bars->ring[q];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q]));
+            if (it.adapter < 0) continue;
+            const float scale = __ldg(p.scale + it.adapter);
+            if (!mbar_wait_warp(smem_u32(&bars->u_full), (uint32_t)u_items & 1u, p.poll_limit) ||
+                !mbar_wait_warp(smem_u32(&bars->ub_empty), ((uint32_t)u_items & 1u) ^ 1u, p.poll_limit)) {
+                raise_timeout(bars, p.status);
+                break;
+            }
+            ++u_items;
+            tc_fence_after();
+            for (int c = 0; c < rank16 / 16; ++c) {            // 16 columns of U: one K step of the second product
+                uint32_t f[16], b[8];
+                tmem_ld_32x8(tmem + lanes + (uint32_t)(kColU + c * 16), f);
+                tmem_ld_32x8(tmem + lanes + (uint32_t)(kColU + c * 16 + 8), f + 8);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    // columns beyond the rank (a rank of 8, 24, ... inside a step of 16) are zero, whatever the unused
+                    // rows of A's buffer held
+                    const bool in = c * 16 + 2 * e < p.rank;
+                    b[e] = in ? pack_bf16(__uint_as_float(f[2 * e]) * scale, __uint_as_float(f[2 * e + 1]) * scale) : 0u;
+                }
+                tmem_st_32x8(tmem + lanes + (uint32_t)(kColUb + c * 8), b);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->u_ready));
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------------
+#define CHECK(expr) do { dg4_status _s = (expr); if (_s != DG4_OK) return _s; } while (0)
+
+constexpr int kSmemLimit = 232448;                // what one CTA may hold
+
+std::mutex g_mu;
+bool g_attr_set[64] = {};
+int g_sm_count[64] = {};
+
+struct Call {
+    const void* X; int64_t ldx;
+    const void* W;
+    const dg4_adapters* ad;
+    const dg4_segments* seg;
+    const void* R; int64_t ldr;
+    void* out[3]; int64_t ldo[3];
+    int n_out;
+};
+
+dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
+    int dev = 0;
+    DG4_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
+    {
+        std::lock_guard<std::mutex> lock(g_mu);
+        if (!g_attr_set[dev]) {
+            DG4_CUDA_TRY(cudaFuncSetAttribute(adapter_proj_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
+            DG4_CUDA_TRY(cudaDeviceGetAttribute(&g_sm_count[dev], cudaDevAttrMultiProcessorCount, dev));
+            g_attr_set[dev] = true;
+        }
+    }
+    Params p;
+    p.seg_ptr = c.seg ? c.seg->seg_ptr : nullptr;
+    p.seg_id = c.seg ? c.seg->seg_id : nullptr;
+    p.n_seg = c.seg ? c.seg->n_seg : 1;
+    p.n = g->n; p.n_adapters = c.ad->n_adapters; p.rank = c.ad->rank; p.scale = c.ad->scale;
+    p.n_out = c.n_out; p.has_res = c.R != nullptr;
+    p.status = g->dev_status; p.poll_limit = dg4i_poll_limit();
+    const int blocks = c.n_out / 128, sms = g_sm_count[dev];
+    // items: at most one per full tile and one ragged one per request
+    const int64_t most = (int64_t)g->n / kTileM + p.n_seg;
+    const bool split = most * blocks <= sms;
+    p.nb = split ? 1 : blocks;
+    int off = p.nb * kTileBytes;
+    p.off_a = off; off += kABytes;
+    p.off_b = off; off += p.nb * kHalfBytes;
+    p.off_stage = off; off += kEpiWarps * 4096;
+    const int per_stage = kTileBytes * (p.has_res ? 2 : 1), tail = (int)sizeof(Bars) + 1024;
+    p.stages = off + kMaxStages * per_stage + tail <= kSmemLimit ? kMaxStages : 1;
+    p.off_x = off; off += p.stages * kTileBytes;
+    p.off_r = off; off += p.has_res ? p.stages * kTileBytes : 0;
+    p.off_bar = off; off += tail;                 // 1024 of it: the base is aligned by hand
+    CUtensorMap map_x, map_w, map_r, map_a, map_b;
+    OutMaps map_o;
+    CHECK(dg4i_make_row_map(&map_w, c.W, c.n_out, 128, 128));
+    CHECK(dg4i_make_row_map(&map_x, c.X, g->n, c.ldx, 128));
+    map_r = map_x;
+    if (c.R) CHECK(dg4i_make_row_map(&map_r, c.R, g->n, c.ldr, 128));
+    CHECK(dg4i_make_row_map(&map_a, c.ad->A, (int64_t)c.ad->n_adapters * c.ad->rank, 128, c.ad->rank));
+    CHECK(dg4i_make_map(&map_b, c.ad->B, c.ad->rank, (int64_t)c.ad->n_adapters * c.n_out, c.ad->rank, 128));
+    for (int j = 0; j < 3; ++j) {
+        map_o.m[j] = map_x;
+        p.out[j] = nullptr; p.ldo[j] = 0;
+        if (j < blocks) {
+            CHECK(dg4i_make_row_map(&map_o.m[j], c.out[j], g->n, c.ldo[j], 32));
+            p.out[j] = (__nv_bfloat16*)c.out[j]; p.ldo[j] = c.ldo[j];
+        }
+    }
+    const dim3 grid((unsigned)(most < sms ? most : sms), (unsigned)(blocks / p.nb));
+    adapter_proj_kernel<<<grid, kThreads, off, st>>>(map_x, map_w, map_r, map_a, map_b, map_o, p);
+    dg4i_count_launch();
+    DG4_CUDA_TRY(cudaGetLastError());
+    return DG4_OK;
+}
+
+dg4_status check_adapters(const dg4_adapters* ad, int n_out) {
+    if (!ad) DG4_FAIL(DG4_ERR_INVALID_ARG, "null adapters");
+    if (ad->n_adapters < 1) DG4_FAIL(DG4_ERR_INVALID_ARG, "the number of adapters (%d) is below one", ad->n_adapters);
+    if (ad->rank < 8 || ad->rank > kRankMax || ad->rank % 8 != 0)
+        DG4_FAIL(DG4_ERR_UNSUPPORTED, "rank = %d: must be a multiple of 8 up to %d", ad->rank, kRankMax);
+    if ((int64_t)ad->n_adapters * n_out > 0x7fffffff)
+        DG4_FAIL(DG4_ERR_UNSUPPORTED, "%d adapters are too many", ad->n_adapters);
+    CHECK(dg4i_check_tensor("A", ad->A, 128, 2, 128));
+    CHECK(dg4i_check_tensor("B", ad->B, ad->rank, 2, ad->rank));
+    if (!ad->scale || ((uintptr_t)ad->scale & 3u)) DG4_FAIL(DG4_ERR_INVALID_ARG, "the adapters' scale is null or not 4-byte aligned");
+    return DG4_OK;
+}
+
+}  // namespace
+
+extern "C" dg4_status dg4_qkv_project_adapters(const dg4_graph* g, const dg4_desc* desc, const void* X, int64_t ldx,
+                                               const void* W_qkv, const dg4_adapters* adapters,
+                                               const dg4_segments* segments, void* Q, int64_t ldq, void* K, int64_t ldk,
+                                               void* V, int64_t ldv, void* stream) {
+    CHECK(dg4i_check_device(g));
+    CHECK(dg4i_check_desc(desc, true));
+    CHECK(dg4i_check_tensor("X", X, ldx, 2, 128));
+    CHECK(dg4i_check_tensor("W_qkv", W_qkv, 128, 2, 128));
+    CHECK(check_adapters(adapters, 384));
+    if (segments) CHECK(dg4i_check_segments(segments));
+    CHECK(dg4i_check_tensor("Q", Q, ldq, 2, 128));
+    CHECK(dg4i_check_tensor("K", K, ldk, 2, 128));
+    CHECK(dg4i_check_tensor("V", V, ldv, 2, 128));
+    Call c = {X, ldx, W_qkv, adapters, segments, nullptr, 0, {Q, K, V}, {ldq, ldk, ldv}, 384};
+    return launch(g, c, (cudaStream_t)stream);
+}
+
+extern "C" dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_desc* desc, const void* O, int64_t ldo,
+                                               const void* W_o, const dg4_adapters* adapters,
+                                               const dg4_segments* segments, const void* H_res, int64_t ldh, void* H_out,
+                                               int64_t ldho, void* stream) {
+    CHECK(dg4i_check_device(g));
+    CHECK(dg4i_check_desc(desc, true));
+    CHECK(dg4i_check_tensor("O", O, ldo, 2, 128));
+    CHECK(dg4i_check_tensor("W_o", W_o, 128, 2, 128));
+    CHECK(check_adapters(adapters, 128));
+    if (segments) CHECK(dg4i_check_segments(segments));
+    const bool res = (desc->flags & DG4_FLAG_RESIDUAL) && H_res;
+    if (res) CHECK(dg4i_check_tensor("H_res", H_res, ldh, 2, 128));
+    CHECK(dg4i_check_tensor("H_out", H_out, ldho, 2, 128));
+    Call c = {O, ldo, W_o, adapters, segments, res ? H_res : nullptr, ldh, {H_out, nullptr, nullptr}, {ldho, 0, 0}, 128};
+    return launch(g, c, (cudaStream_t)stream);
+}

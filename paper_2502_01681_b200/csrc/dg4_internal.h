@@ -33,6 +33,7 @@ void dg4_set_error(const char* fmt, ...);
 dg4_status dg4i_check_device(const dg4_graph* g);
 dg4_status dg4i_check_desc(const dg4_desc* d, bool need_bf16);
 dg4_status dg4i_check_tensor(const char* name, const void* p, int64_t ld, int elem_size, int min_ld);
+dg4_status dg4i_check_segments(const dg4_segments* seg);          // dg4_norm_gate.cu
 // Poll limit of the bounded device-side waits (mbarrier phases, level counters) handed to every kernel launch:
 // the built-in default unless dg4_debug_set_poll_limit changed it.
 uint32_t dg4i_poll_limit();
@@ -43,6 +44,8 @@ uint32_t dg4i_poll_limit();
 // box_rows rows, 128-byte swizzle, rows past the end read as zero and are clipped on store (dg4_project.cu).
 struct CUtensorMap_st;
 dg4_status dg4i_make_row_map(CUtensorMap_st* map, const void* base, int64_t rows, int64_t ld, int box_rows);
+// The same for [rows, cols] with fewer than 64 columns: the box's columns past the end read as zero.
+dg4_status dg4i_make_map(CUtensorMap_st* map, const void* base, int cols, int64_t rows, int64_t ld, int box_rows);
 
 // ---- launch accounting (every kernel launch of the library bumps this counter) ------------------
 void dg4i_count_launch(int n = 1);

@@ -379,12 +379,12 @@ dg4_status get_encoder(EncodeTiledFn* fn) {
     return DG4_OK;
 }
 
-// [rows, 128] bf16 row-major with leading dimension ld; box = 64 columns x box_rows rows, 128-byte swizzle.
-dg4_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t ld, int box_rows = 128) {
+// [rows, cols] bf16 row-major with leading dimension ld; box = 64 columns x box_rows rows, 128-byte swizzle.
+dg4_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t ld, int box_rows = 128, int cols = 128) {
     EncodeTiledFn enc;
     dg4_status s = get_encoder(&enc);
     if (s != DG4_OK) return s;
-    cuuint64_t dims[2] = {128, (cuuint64_t)rows};
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     cuuint64_t strides[1] = {(cuuint64_t)(ld * 2)};
     cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
     cuuint32_t estr[2] = {1, 1};
@@ -399,6 +399,10 @@ dg4_status make_map(CUtensorMap* m, const void* base, int64_t rows, int64_t ld, 
 
 dg4_status dg4i_make_row_map(CUtensorMap_st* map, const void* base, int64_t rows, int64_t ld, int box_rows) {
     return make_map(map, base, rows, ld, box_rows);
+}
+
+dg4_status dg4i_make_map(CUtensorMap_st* map, const void* base, int cols, int64_t rows, int64_t ld, int box_rows) {
+    return make_map(map, base, rows, ld, box_rows, cols);
 }
 
 dg4_status dg4i_proj_launch(const dg4i_proj_args& a, cudaStream_t st) {

@@ -31,6 +31,9 @@ DG4_F32, DG4_BF16 = 0, 1
 DG4_FLAG_RESIDUAL = 1
 DG4_FLAG_LEVEL_LAUNCHES = 2
 DG4_FLAG_FUSED_LAYER = 4
+DG4_FLAG_RMS_NORM = 8
+
+DG4_KV8_ROW_BYTES = 288
 
 (DG4_ARR_NBR_PTR, DG4_ARR_NBR_IDX, DG4_ARR_LEVEL_PTR, DG4_ARR_LEVEL_NODES, DG4_ARR_PERM, DG4_ARR_CLASS_PTR,
  DG4_ARR_LEVEL_PERM, DG4_ARR_LEVEL_CLASS_PTR, DG4_ARR_NBR_PAD) = range(9)
@@ -45,6 +48,8 @@ EXPORTS = [
     "dg4_debug_set_poll_limit", "dg4_debug_override_current_device",
     "dg4_cone_update_workspace_bytes", "dg4_cone_update_fwd", "dg4_block_fwd_levelised",
     "dg4_blocks_workspace_bytes", "dg4_blocks_fwd_levelised",
+    "dg4_qkv_project_adapters", "dg4_out_project_adapters", "dg4_kv8_write", "dg4_kv8_read",
+    "dg4_sparse_attn_kv8_fwd", "dg4_norm_gate_fwd",
 ]
 
 
@@ -64,6 +69,15 @@ class dg4_graph_info_t(ctypes.Structure):
     _fields_ = [("n_nodes", ctypes.c_int64), ("n_edges", ctypes.c_int64), ("n_nbr", ctypes.c_int64),
                 ("n_levels", ctypes.c_int32), ("max_class", ctypes.c_int32), ("hops", ctypes.c_int32),
                 ("perm_chunk", ctypes.c_int32), ("n_chunks", ctypes.c_int32), ("device", ctypes.c_int32)]
+
+
+class dg4_segments(ctypes.Structure):
+    _fields_ = [("n_seg", ctypes.c_int32), ("seg_ptr", ctypes.c_void_p), ("seg_id", ctypes.c_void_p)]
+
+
+class dg4_adapters(ctypes.Structure):
+    _fields_ = [("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("A", ctypes.c_void_p),
+                ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 _lib = None
@@ -160,6 +174,19 @@ def load():
     lib.dg4_cone_update_fwd.restype = ctypes.c_int
     lib.dg4_cone_update_fwd.argtypes = [vp, dp, vp, i64, ctypes.c_int32, ctypes.POINTER(vp), ctypes.POINTER(vp),
                                         ctypes.c_int32, ctypes.c_int32, vp, ctypes.c_size_t, vp, ctypes.POINTER(i64), vp]
+    adp, sgp, i32 = ctypes.POINTER(dg4_adapters), ctypes.POINTER(dg4_segments), ctypes.c_int32
+    lib.dg4_qkv_project_adapters.restype = ctypes.c_int
+    lib.dg4_qkv_project_adapters.argtypes = [vp, dp, vp, i64, vp, adp, sgp, vp, i64, vp, i64, vp, i64, vp]
+    lib.dg4_out_project_adapters.restype = ctypes.c_int
+    lib.dg4_out_project_adapters.argtypes = [vp, dp, vp, i64, vp, adp, sgp, vp, i64, vp, i64, vp]
+    lib.dg4_kv8_write.restype = ctypes.c_int
+    lib.dg4_kv8_write.argtypes = [vp, dp, vp, i64, vp, i64, vp, i64, vp, i32, vp]
+    lib.dg4_kv8_read.restype = ctypes.c_int
+    lib.dg4_kv8_read.argtypes = [vp, dp, vp, i64, vp, i64, vp, i64, vp, i32, vp]
+    lib.dg4_sparse_attn_kv8_fwd.restype = ctypes.c_int
+    lib.dg4_sparse_attn_kv8_fwd.argtypes = [vp, dp, vp, i64, vp, i64, vp, i64, vp, i32, vp]
+    lib.dg4_norm_gate_fwd.restype = ctypes.c_int
+    lib.dg4_norm_gate_fwd.argtypes = [vp, dp, vp, i64, vp, i64, cf, vp, i32, sgp, vp, vp, vp, vp, cf, vp, i64, vp, i64, vp]
     lib.dg4_debug_set_poll_limit.restype = None
     lib.dg4_debug_set_poll_limit.argtypes = [ctypes.c_uint32]
     lib.dg4_debug_override_current_device.restype = None
@@ -195,9 +222,9 @@ def _ld(t):
 
 
 def desc(heads: int, dtype: int, scale: float, residual: bool = False, d: int = 128,
-         level_launches: bool = False, fused_layer: bool = False) -> dg4_desc:
+         level_launches: bool = False, fused_layer: bool = False, rms_norm: bool = False) -> dg4_desc:
     flags = ((DG4_FLAG_RESIDUAL if residual else 0) | (DG4_FLAG_LEVEL_LAUNCHES if level_launches else 0)
-             | (DG4_FLAG_FUSED_LAYER if fused_layer else 0))
+             | (DG4_FLAG_FUSED_LAYER if fused_layer else 0) | (DG4_FLAG_RMS_NORM if rms_norm else 0))
     return dg4_desc(d, heads, dtype, flags, float(scale))
 
 
@@ -365,6 +392,126 @@ def dg4_cone_update_fwd(g: Graph, dsc: dg4_desc, H, W_qkv_list, W_o_list, delta:
                                       _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(stored),
                                       ctypes.byref(nb), _stream(stream)))
     return int(nb.value)
+
+
+@dataclass
+class Segments:
+    """Requests of a batch: row offsets and ids (CUDA int32 tensors, kept alive here)."""
+    ptr: object
+    ids: object
+    struct: dg4_segments
+
+
+@dataclass
+class Adapters:
+    """Low-rank adapters of one projection (CUDA tensors, kept alive here)."""
+    A: object
+    B: object
+    scale: object
+    struct: dg4_adapters
+
+
+def segments(seg_ptr, seg_id) -> Segments:
+    """seg_ptr [n_seg + 1] and seg_id [n_seg], CUDA int32: see dg4_segments in dg4.h."""
+    import torch
+    for t in (seg_ptr, seg_id):
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError("segment arrays are contiguous one-dimensional CUDA int32 tensors")
+    if seg_ptr.numel() != seg_id.numel() + 1:
+        raise ValueError("seg_ptr has one entry more than seg_id")
+    return Segments(seg_ptr, seg_id, dg4_segments(seg_id.numel(), seg_ptr.data_ptr(), seg_id.data_ptr()))
+
+
+def adapters(A, B, scale) -> Adapters:
+    """A [n, rank, 128] and B [n, n_out, rank] bf16, scale [n] fp32, CUDA, contiguous: see dg4_adapters in dg4.h."""
+    import torch
+    if A.dim() != 3 or B.dim() != 3 or scale.dim() != 1 or A.shape[2] != 128 or B.shape[1] not in (128, 384) \
+            or B.shape[2] != A.shape[1] or not A.shape[0] == B.shape[0] == scale.shape[0]:
+        raise ValueError("adapters are A [n, rank, 128], B [n, 128 or 384, rank] and scale [n]")
+    if A.dtype != torch.bfloat16 or B.dtype != torch.bfloat16 or scale.dtype != torch.float32:
+        raise ValueError("adapters are bf16 with an fp32 scale")
+    if not all(t.is_cuda and t.is_contiguous() for t in (A, B, scale)):
+        raise ValueError("adapters are contiguous CUDA tensors")
+    return Adapters(A, B, scale, dg4_adapters(A.shape[0], A.shape[1], A.data_ptr(), B.data_ptr(), scale.data_ptr()))
+
+
+def _struct(x):
+    return ctypes.byref(x.struct) if x is not None else None
+
+
+def _nodes(nodes):
+    if nodes is None:
+        return None, 0
+    import torch
+    if nodes.dtype != torch.int32 or nodes.dim() != 1 or not nodes.is_contiguous() or not nodes.is_cuda:
+        raise ValueError("a node list is a contiguous one-dimensional CUDA int32 tensor")
+    return _ptr(nodes), nodes.numel()
+
+
+def _vec(t, rows=1):
+    """Pointer of an fp32 vector of 128 (or of `rows` of them), or None."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
+        raise ValueError("norm and gate vectors are contiguous CUDA fp32 tensors of 128 elements each")
+    return _ptr(t)
+
+
+def dg4_qkv_project_adapters(g: Graph, dsc: dg4_desc, X, W_qkv, ad: Adapters, seg, Q, K, V, stream=None):
+    """dg4_qkv_project with a low-rank adapter per request; seg None: all rows use adapter 0."""
+    if ad.B.shape[1] != 384:
+        raise ValueError("the adapters are not those of a QKV projection")
+    _check(load().dg4_qkv_project_adapters(g.handle, ctypes.byref(dsc), _ptr(X), _ld(X), _ptr(W_qkv), _struct(ad),
+                                           _struct(seg), _ptr(Q), _ld(Q), _ptr(K), _ld(K), _ptr(V), _ld(V),
+                                           _stream(stream)))
+
+
+def dg4_out_project_adapters(g: Graph, dsc: dg4_desc, O, W_o, ad: Adapters, seg, H_res, H_out, stream=None):
+    """dg4_out_project with a low-rank adapter per request; seg None: all rows use adapter 0."""
+    if ad.B.shape[1] != 128:
+        raise ValueError("the adapters are not those of an output projection")
+    _check(load().dg4_out_project_adapters(g.handle, ctypes.byref(dsc), _ptr(O), _ld(O), _ptr(W_o), _struct(ad),
+                                           _struct(seg), _ptr(H_res), _ld(H_res) if H_res is not None else 0,
+                                           _ptr(H_out), _ld(H_out), _stream(stream)))
+
+
+def dg4_kv8_write(g: Graph, dsc: dg4_desc, K, V, T, nodes=None, stream=None):
+    """Rows of K and V into the 8-bit table T ([n, >= 288] uint8); `nodes`: CUDA int32 list, None for all."""
+    lst, count = _nodes(nodes)
+    if nodes is not None and count == 0:
+        return
+    _check(load().dg4_kv8_write(g.handle, ctypes.byref(dsc), _ptr(K), _ld(K), _ptr(V), _ld(V), _ptr(T), _ld(T), lst,
+                                count, _stream(stream)))
+
+
+def dg4_kv8_read(g: Graph, dsc: dg4_desc, T, K, V, nodes=None, stream=None):
+    """The values the table T stands for into rows of K and V."""
+    lst, count = _nodes(nodes)
+    if nodes is not None and count == 0:
+        return
+    _check(load().dg4_kv8_read(g.handle, ctypes.byref(dsc), _ptr(T), _ld(T), _ptr(K), _ld(K), _ptr(V), _ld(V), lst,
+                               count, _stream(stream)))
+
+
+def dg4_sparse_attn_kv8_fwd(g: Graph, dsc: dg4_desc, Q, T, O, nodes=None, stream=None):
+    """dg4_sparse_attn_fwd over the 8-bit table, for all nodes or the listed ones."""
+    lst, count = _nodes(nodes)
+    if nodes is not None and count == 0:
+        return
+    _check(load().dg4_sparse_attn_kv8_fwd(g.handle, ctypes.byref(dsc), _ptr(Q), _ld(Q), _ptr(T), _ld(T), _ptr(O),
+                                          _ld(O), lst, count, _stream(stream)))
+
+
+def dg4_norm_gate_fwd(g: Graph, dsc: dg4_desc, S, R, res_scale, gate, seg, post, pre, eps, R_out, Y, stream=None):
+    """R_out = res_scale * R + gate * Norm_post(S), Y = Norm_pre(R_out).  gate [n_gates, 128] fp32 or None; post and
+    pre: (gamma, beta or None); Y and pre may be None."""
+    n_gates = 0 if gate is None else gate.numel() // 128
+    pre = pre or (None, None)
+    _check(load().dg4_norm_gate_fwd(g.handle, ctypes.byref(dsc), _ptr(S), _ld(S), _ptr(R), _ld(R), float(res_scale),
+                                    _vec(gate, n_gates), n_gates, _struct(seg), _vec(post[0]), _vec(post[1]),
+                                    _vec(pre[0]), _vec(pre[1]), float(eps), _ptr(R_out), _ld(R_out), _ptr(Y),
+                                    _ld(Y) if Y is not None else 0, _stream(stream)))
 
 
 def dg4_debug_set_poll_limit(polls: int):
