@@ -471,7 +471,8 @@ dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_desc* desc, co
  *
  * dg4_kv8_write: rows of K and V into the table.  dg4_kv8_read: the values the table stands for into rows of K and V
  * (exact in fp32; in bf16 too unless they fall below its normal range).
- *   T      device, [n, ldt] bytes, 16-byte aligned; ldt a multiple of 16, >= 288.  Must not overlap K or V
+ *   T      device, [n, ldt] bytes, 32-byte aligned; ldt a multiple of 32, 288 .. 2^31 - 1.  Must not
+ *          overlap K or V
  *   K, V   device, [n, d] of desc->dtype
  *   nodes  device, [count] int32 or NULL: the nodes whose rows are written (the rows of others stay as they are);
  *          ids outside 0 .. n - 1 are skipped, repeated ids are allowed.  NULL: all nodes (count 0 or n)

@@ -15,6 +15,11 @@ __device__ __forceinline__ Piece ld_piece_nc(const void* p) {        // read-onl
                  : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
     return r;
 }
+__device__ __forceinline__ void ld_pieces2_nc(const void* p, Piece& a, Piece& b) {   // two at once, 32-byte aligned
+    asm volatile("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(a.w[0]), "=r"(a.w[1]), "=r"(a.w[2]), "=r"(a.w[3]), "=r"(b.w[0]), "=r"(b.w[1]), "=r"(b.w[2]), "=r"(b.w[3])
+                 : "l"(p));
+}
 // L2 eviction priorities (a 64-bit policy word made once per thread): rows that are gathered again by later nodes
 // are asked to stay, data that passes through once is asked to leave first.
 __device__ __forceinline__ uint64_t l2_policy_evict_last() {

@@ -7,6 +7,8 @@
 #include "dg4_internal.h"
 #include "dg4_kv8_core.cuh"
 
+#include <atomic>
+
 namespace {
 
 using namespace attn;
@@ -66,7 +68,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(CopyArgs a) {
         const uint8_t* row = a.T + (int64_t)v * a.ldt;
         const Piece p = ld_piece_stream(row + sub * 16);
         const uint32_t pair = ld_pair(row + kCodeBytes + 2 * (sub / LPH));
-        const float sk = scale_of(pair & 255u), sv = scale_of(pair >> 8);
+        const float sk = scale_k(pair), sv = scale_v(pair);
         float k[kEl], w[kEl];
         decode4(p.w[0], k); decode4(p.w[1], k + 4);
         decode4(p.w[2], w); decode4(p.w[3], w + 4);
@@ -79,7 +81,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(CopyArgs a) {
 
 struct AttnArgs {
     const void* Q; int64_t ldq;        // bytes
-    const uint8_t* T; int64_t ldt;
+    const uint8_t* T; uint32_t ldt;
     void* O; int64_t ldo;
     const int32_t* nodes;              // nullable
     const int32_t* nbr_pad;            // fixed-width lists (two hops at most)
@@ -89,165 +91,330 @@ struct AttnArgs {
     float c;                           // scale * log2(e): scores are kept in log2 units
 };
 
-// q . (8 codes); the sum over a head's lanes and the slice's scale follow
-__device__ __forceinline__ float dot8(const float* q, const Piece& p) {
-    float k[kEl], acc = 0.f;
-    decode4(p.w[0], k); decode4(p.w[1], k + 4);
+// Attention is bound by instructions, not by bytes: a member's 256 codes cost 128 conversions to pairs of fp16 and 256
+// multiply-adds, whoever does them, and every lane that takes part pays the member's addresses, scales, exponential and
+// sums on top.  So
+//  - a row is spread over as few lanes as the heads allow: 8 lanes with two pieces (one 32-byte load) each for up to 8
+//    heads (a lane then holds 16 elements; with 8 heads that is a head, and a score needs no shuffle), 16 lanes with
+//    one piece each for 16;
+//  - for bf16 rows the multiply-adds take the fp16 codes as they are (fp16 x fp16 + fp32), which saves the 256
+//    conversions to fp32.  The query is brought to fp16 for that, times a power of two that puts the largest magnitude
+//    of its head into [2^14, 2^15): a bf16 number then fits exactly down to 2^-25 of that magnitude, and what is
+//    smaller is off by at most 2^-40 of it.  The weights are rounded to fp16 (off by at most 2^-11 of themselves,
+//    an eighth of the output's own rounding); their sum is taken in fp32 before that rounding.  fp32 rows keep query
+//    and weights in fp32.
+// A member's weight on its codes is exp2(score - max score) * (V scale), of which the scales alone may span 2^247.
+// Before it is rounded to fp16 it is therefore measured against the largest weight of the node and head, which is put
+// near 2^14 by a power of two (the other end of fp16's range, 2^-24, is then so far below that it does not matter).
+// exponent field of the power of two that puts a largest magnitude `top` into [2^14, 2^15), kept where that power and
+// its inverse (field 254 - b) are normal numbers
+__device__ __forceinline__ uint32_t lift(float top) { return min(268u - (__float_as_uint(top) >> 23), 253u); }
+
+template <bool BF16, int LANES> struct Query {
+    static constexpr int kN = 128 / LANES;
+    uint32_t h[BF16 ? kN / 2 : 1];
+    float f[BF16 ? 1 : kN];
+    float c;                                   // what makes a dot product with codes a score in log2 units
+    template <int LPH>
+    __device__ __forceinline__ void set(const float* q, float scale) {
+        if (BF16) {
+            float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < kEl; ++i) acc = fmaf(q[i], k[i], acc);
-    return acc;
-}
-__device__ __forceinline__ void add8(float weight, const Piece& p, float* acc) {
-    float w[kEl];
-    decode4(p.w[2], w); decode4(p.w[3], w + 4);
+            for (int e = 0; e < kN; ++e) top = fmaxf(top, fabsf(q[e]));
 #pragma unroll
-    for (int i = 0; i < kEl; ++i) acc[i] = fmaf(weight, w[i], acc[i]);
+            for (int o = LPH / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const uint32_t b = lift(top);
+            const float up = __uint_as_float(b << 23);
+            c = scale * __uint_as_float((254u - b) << 23);
+#pragma unroll
+            for (int e = 0; e < kN / 2; ++e) {
+                const __half2 x = __floats2half2_rn(q[2 * e] * up, q[2 * e + 1] * up);
+                h[e] = *reinterpret_cast<const uint32_t*>(&x);
+            }
+        } else {
+            c = scale;
+#pragma unroll
+            for (int e = 0; e < kN; ++e) f[e] = q[e];
+        }
+    }
+};
+
+__device__ __forceinline__ void fma_half2(uint32_t a, uint32_t b, float& lo, float& hi) {     // lo += a.lo b.lo, hi += a.hi b.hi
+    asm("{\n\t.reg .b16 al, ah, bl, bh;\n\tmov.b32 {al, ah}, %2;\n\tmov.b32 {bl, bh}, %3;\n\t"
+        "fma.rn.f32.f16 %0, al, bl, %0;\n\tfma.rn.f32.f16 %1, ah, bh, %1;\n\t}"
+        : "+f"(lo), "+f"(hi) : "r"(a), "r"(b));
 }
 
-// Lists of at most MAXN members from the fixed-width table; the walk and the prefetch of the next node's list are
-// those of the 16-bit kernel (dg4_attn.cu).
-template <bool BF16, int LPH, int MAXN>
-__global__ void __launch_bounds__(256, 3) sparse_attn_kv8_kernel(AttnArgs a) {
-    constexpr int W = MAXN + 1;
-    const int lane = threadIdx.x & 31, sub = lane & 15, grp = lane - sub;
-    const unsigned mask = 0xffffu << grp;
-    const uint32_t stride = gridDim.x * (blockDim.x / kLanes);
-    uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) / kLanes;
-    int v_next = -1, pad_next = 0;
-    if (slot < (uint32_t)a.count) {
-        v_next = a.nodes ? a.nodes[slot] : (int)slot;
-        if (sub < W && (uint32_t)v_next < (uint32_t)a.n) pad_next = a.nbr_pad[(size_t)v_next * W + sub];
+template <bool BF16, int LANES> struct Row {
+    static constexpr int kPieces = 16 / LANES, kN = 8 * kPieces;
+
+    Piece p[kPieces];
+    uint32_t pair;
+    // codes: T + this lane's pieces; exps: T + this lane's pair
+    __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* exps, uint32_t row, uint32_t ldt) {
+        const uint64_t off = (uint64_t)row * ldt;
+        if (kPieces == 2) ld_pieces2_nc(codes + off, p[0], p[kPieces - 1]);
+        else p[0] = ld_piece_nc(codes + off);
+        pair = ld_pair(exps + off);
     }
-    for (; slot < (uint32_t)a.count; slot += stride) {
-        const int v = v_next, pad = pad_next;
-        {
-            const uint32_t s2 = slot + stride;
-            if (s2 < (uint32_t)a.count) {
-                v_next = a.nodes ? a.nodes[s2] : (int)s2;
-                if (sub < W && (uint32_t)v_next < (uint32_t)a.n) pad_next = a.nbr_pad[(size_t)v_next * W + sub];
+    __device__ __forceinline__ float dot(const Query<BF16, LANES>& q) const {
+        float a = 0.f, b = 0.f;
+#pragma unroll
+        for (int i = 0; i < 2 * kPieces; ++i) {
+            const uint32_t w = p[i >> 1].w[i & 1];
+            if (BF16) {
+                uint32_t k[2];
+                decode4_half(w, k);
+                fma_half2(k[0], q.h[2 * i], a, b);
+                fma_half2(k[1], q.h[2 * i + 1], a, b);
+            } else {
+                float k[4];
+                decode4(w, k);
+#pragma unroll
+                for (int e = 0; e < 4; e += 2) {
+                    a = fmaf(q.f[4 * i + e], k[e], a);
+                    b = fmaf(q.f[4 * i + e + 1], k[e + 1], b);
+                }
             }
         }
-        if ((uint32_t)v >= (uint32_t)a.n) continue;                 // ids outside the graph are skipped
-        const int cnt = __shfl_sync(mask, pad, grp);
-        Piece kv[MAXN];
-        uint32_t pair[MAXN];
-        int u[MAXN];
-        u[0] = v;
+        return a + b;
+    }
+    __device__ __forceinline__ void add(float weight, float* acc) const {
+        const __half2 w2 = __floats2half2_rn(weight, weight);
+        const uint32_t wh = *reinterpret_cast<const uint32_t*>(&w2);
 #pragma unroll
-        for (int j = 1; j < MAXN; ++j) u[j] = __shfl_sync(mask, pad, grp + j);
-        float q[kEl];
-        load8<BF16>((const char*)a.Q + (int64_t)v * a.ldq, sub, q);
-        // the filler of a list repeats v, so every slot names a valid row and the loads need no predicate
+        for (int i = 0; i < 2 * kPieces; ++i) {
+            const uint32_t w = p[i >> 1].w[2 + (i & 1)];
+            float* o = acc + 4 * i;
+            if (BF16) {
+                uint32_t v[2];
+                decode4_half(w, v);
+                fma_half2(v[0], wh, o[0], o[1]);
+                fma_half2(v[1], wh, o[2], o[3]);
+            } else {
+                float v[4];
+                decode4(w, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(weight, v[e], o[e]);
+            }
+        }
+    }
+};
+// this lane's part of a row as it stands in memory, so that a row fetched early costs no more registers than that
+template <bool BF16, int LANES> struct RawRow {
+    static constexpr int kPieces = (BF16 ? 1 : 2) * 16 / LANES;
+    Piece p[kPieces];
+    __device__ __forceinline__ void load(const void* row, int sub) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) p[i] = ld_piece_stream((const char*)row + (sub * kPieces + i) * 16);
+    }
+    __device__ __forceinline__ void unpack(float* f) const {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) Elem<BF16>::unpack(p[i], f + i * Elem<BF16>::kPerPiece);
+    }
+};
+template <bool BF16, int LANES>
+__device__ __forceinline__ void store_row(void* row, int sub, const float* f) {
+#pragma unroll
+    for (int i = 0; i < 16 / LANES; ++i) store8<BF16>(row, sub * (16 / LANES) + i, f + 8 * i);
+}
+
+// Lists of at most MAXN members from the fixed-width table.  A group of LANES lanes takes a node; the nodes in flight
+// across the GPU are a contiguous range.  All members of a list are computed without branches inside the warp up to the
+// longest of its lists; a member beyond a node's own list weighs zero (its filler is the node's own row, so no value
+// enters that the node does not read anyway).
+// The loads run ahead of the arithmetic: lists two nodes ahead, and a member's row of the next node goes into the
+// registers of this node's as soon as that has been added up.
+template <bool BF16, int LANES, int LPH, int MAXN>
+__global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kernel(AttnArgs a) {
+    constexpr int W = MAXN + 1, N = Row<BF16, LANES>::kN;
+    const int lane = threadIdx.x & 31, sub = lane & (LANES - 1), grp = lane - sub;
+    const uint32_t stride = gridDim.x * (blockDim.x / LANES);
+    uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) / 32 * (32 / LANES) + lane / LANES;
+    uint32_t base = slot - lane / LANES;                                      // the warp's first slot
+    const uint8_t* codes = a.T + sub * (256 / LANES);
+    const uint8_t* exps = a.T + kCodeBytes + 2 * (sub / LPH);
+    auto node_of = [&](uint32_t s) {
+        int v = -1;
+        if (s < (uint32_t)a.count) v = a.nodes ? a.nodes[s] : (int)s;
+        return (uint32_t)v < (uint32_t)a.n ? v : -1;                          // ids outside the graph are skipped
+    };
+    auto list_of = [&](int v) { return sub < W && v >= 0 ? a.nbr_pad[(size_t)v * W + sub] : 0; };
+    Row<BF16, LANES> row[MAXN];
+    RawRow<BF16, LANES> raw;
+    int v = node_of(slot), pad = list_of(v);
+    int v1 = node_of(slot + stride), pad1 = list_of(v1);
+    raw.load((const char*)a.Q + (int64_t)max(v, 0) * a.ldq, sub);
+#pragma unroll
+    for (int j = 0; j < MAXN; ++j)
+        row[j].load(codes, exps, (uint32_t)(j ? __shfl_sync(0xffffffffu, pad, grp + j) : max(v, 0)), a.ldt);
+    for (; base < (uint32_t)a.count; base += stride, slot += stride) {
+        const int cnt = __shfl_sync(0xffffffffu, pad, grp);
+        const int most = __reduce_max_sync(0xffffffffu, cnt);
+        const bool more = base + stride < (uint32_t)a.count;                  // the warp has another round
+        const int v2 = node_of(slot + 2 * stride), pad2 = list_of(v2);
+        float acc[N];
+        raw.unpack(acc);
+        Query<BF16, LANES> q;
+        q.template set<LPH>(acc, a.c);
+        if (more) raw.load((const char*)a.Q + (int64_t)max(v1, 0) * a.ldq, sub);
+        float s[MAXN], m = -INFINITY, z = 0.f, top = 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = 0.f;
 #pragma unroll
         for (int j = 0; j < MAXN; ++j) {
-            const uint8_t* row = a.T + (int64_t)u[j] * a.ldt;
-            kv[j] = ld_piece_nc(row + sub * 16);
-            pair[j] = ld_pair(row + kCodeBytes + 2 * (sub / LPH));
-        }
-        float acc[kEl];
+            s[j] = -INFINITY;
+            if (j < most) {
+                float dot = row[j].dot(q);
 #pragma unroll
-        for (int i = 0; i < kEl; ++i) acc[i] = 0.f;
-        if (cnt <= 1) {                                             // softmax over one member: weight exactly 1
-            add8(scale_of(pair[0] >> 8), kv[0], acc);
-        } else {
-            float s[MAXN], m = -INFINITY, z = 0.f;
-#pragma unroll
-            for (int j = 0; j < MAXN; ++j) {
-                float dot = j < cnt ? dot8(q, kv[j]) : 0.f;
-#pragma unroll
-                for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(mask, dot, o);
-                s[j] = j < cnt ? dot * scale_of(pair[j] & 255u) * a.c : -INFINITY;
+                for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                if (j < cnt) s[j] = dot * q.c * scale_k(row[j].pair);
+                if (j == 0 && cnt <= 1) s[0] = 0.f;                           // softmax over one member: weight exactly 1
                 m = fmaxf(m, s[j]);
             }
-#pragma unroll
-            for (int j = 0; j < MAXN; ++j) {
-                if (j < cnt) {
-                    const float p = fast_exp2(s[j] - m);
-                    z += p;
-                    add8(p * scale_of(pair[j] >> 8), kv[j], acc);
-                }
-            }
-            const float inv = fast_rcp(z);
-#pragma unroll
-            for (int i = 0; i < kEl; ++i) acc[i] *= inv;
         }
-        store8<BF16>((char*)a.O + (int64_t)v * a.ldo, sub, acc);
+#pragma unroll
+        for (int j = 0; j < MAXN; ++j) {
+            if (j < most) {
+                const float p = fast_exp2(s[j] - m);
+                z += p;
+                s[j] = p * scale_v(row[j].pair);                              // from here on the weight on the codes
+                top = fmaxf(top, s[j]);
+            }
+        }
+        const uint32_t b = BF16 ? lift(top) : 127u;
+        const float up = __uint_as_float(b << 23), down = __uint_as_float((254u - b) << 23);
+#pragma unroll
+        for (int j = 0; j < MAXN; ++j) {
+            if (j < most) row[j].add(BF16 ? s[j] * up : s[j], acc);
+            const int u = j ? __shfl_sync(0xffffffffu, pad1, grp + j) : max(v1, 0);
+            if (more) row[j].load(codes, exps, (uint32_t)u, a.ldt);
+        }
+        const float inv = cnt <= 1 ? 1.f : fast_rcp(z);
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = BF16 ? acc[e] * inv * down : acc[e] * inv;
+        if (v >= 0) store_row<BF16, LANES>((char*)a.O + (int64_t)v * a.ldo, sub, acc);
+        v = v1; pad = pad1;
+        v1 = v2; pad1 = pad2;
     }
 }
 
-// Wider cones (3 to 8 hops, lists of up to 511 members): one warp per node, the half-warps take alternate members,
-// four in flight each; online softmax (running maximum and sum in 32 bits) per half, merged at the end.
-template <bool BF16, int LPH>
-__global__ void __launch_bounds__(256, 3) sparse_attn_kv8_wide_kernel(AttnArgs a) {
-    constexpr int UN = 4;
-    const int lane = threadIdx.x & 31, sub = lane & 15, half = lane >> 4;
-    const unsigned hmask = 0xffffu << (lane - sub);
+// Wider cones (3 to 8 hops, lists of up to 511 members): one warp per node, its groups of LANES lanes take alternate
+// members, UN in flight each; online softmax (running maximum and sum in 32 bits) per group, merged at the end.
+// For bf16 rows the sums are measured against a running reference of their own: the largest logarithm of a weight on
+// the codes, score + log2(V scale), less 14.  What its rounding does (2^-18 in the exponent) is far below that of the
+// fp16 weights.
+// The loads run ahead of the arithmetic: the next batch of members (of this node, or the first one of the next node)
+// goes into the registers of the present one as soon as that has been added up, the member ids a chunk of 32 ahead.
+template <bool BF16, int LANES, int LPH>
+__global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a) {
+    constexpr int GROUPS = 32 / LANES, UN = 4, BATCH = GROUPS * UN, N = Row<BF16, LANES>::kN;
+    const int lane = threadIdx.x & 31, sub = lane & (LANES - 1), grp = lane / LANES;
     const uint32_t warps = gridDim.x * (blockDim.x >> 5);
-    for (uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) >> 5; slot < (uint32_t)a.count; slot += warps) {
-        const int v = a.nodes ? a.nodes[slot] : (int)slot;
-        if ((uint32_t)v >= (uint32_t)a.n) continue;
-        const int beg = a.nbr_ptr[v];
-        const int cnt = a.nbr_ptr[v + 1] - beg;
-        float q[kEl], acc[kEl], m = -INFINITY, z = 0.f;
-        load8<BF16>((const char*)a.Q + (int64_t)v * a.ldq, sub, q);
+    const uint8_t* codes = a.T + sub * (256 / LANES);
+    const uint8_t* exps = a.T + kCodeBytes + 2 * (sub / LPH);
+    uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
+    // the node after next: id (-1: none), list bounds, first 32 members
+    int v1 = -1, beg1 = 0, cnt1 = 0, u1 = 0;
+    auto fetch = [&]() {
+        v1 = -1;
+        for (; slot < (uint32_t)a.count && v1 < 0; slot += warps) {
+            const int v = a.nodes ? a.nodes[slot] : (int)slot;
+            if ((uint32_t)v < (uint32_t)a.n) v1 = v;                          // ids outside the graph are skipped
+        }
+        if (v1 >= 0) {
+            beg1 = a.nbr_ptr[v1];
+            cnt1 = a.nbr_ptr[v1 + 1] - beg1;
+            u1 = lane < cnt1 ? a.nbr_idx[beg1 + lane] : 0;
+        }
+    };
+    // exp2(x - ref) where ref = -inf stands for "nothing seen yet": measured against 0 then, so that scores of -inf
+    // weigh nothing instead of inf - inf
+    auto finite = [](float ref) { return ref == -INFINITY ? 0.f : ref; };
+    Row<BF16, LANES> row[UN];
+    RawRow<BF16, LANES> raw;
+    fetch();
+    int v = v1, beg = beg1, cnt = cnt1, ids = u1;                             // ids: the chunk of 32 members being read
+    if (v < 0) return;
+    raw.load((const char*)a.Q + (int64_t)v * a.ldq, sub);
+    // members past the end are stood in for by the last one, which is not added again (it may be NaN: not even 0 * it)
 #pragma unroll
-        for (int i = 0; i < kEl; ++i) acc[i] = 0.f;
-        for (int base = 0; base < cnt; base += 32) {
-            const int my_u = base + lane < cnt ? a.nbr_idx[beg + base + lane] : -1;
-            const int chunk = cnt - base < 32 ? cnt - base : 32;
-            for (int t = 0; t < chunk; t += 2 * UN) {
-                Piece kv[UN];
-                uint32_t pair[UN];
-                float s[UN], m_new = m;
-                int u[UN];
+    for (int i = 0; i < UN; ++i)
+        row[i].load(codes, exps, (uint32_t)__shfl_sync(0xffffffffu, ids, min(GROUPS * i + grp, min(cnt, 32) - 1)), a.ldt);
+    fetch();
+    while (v >= 0) {
+        float acc[N], m = -INFINITY, mw = -INFINITY, z = 0.f;
+        raw.unpack(acc);
+        Query<BF16, LANES> q;
+        q.template set<LPH>(acc, a.c);
+        if (v1 >= 0) raw.load((const char*)a.Q + (int64_t)v1 * a.ldq, sub);
 #pragma unroll
-                for (int i = 0; i < UN; ++i) {
-                    const int j = t + 2 * i + half;
-                    u[i] = __shfl_sync(0xffffffffu, my_u, j & 31);
-                    if (j >= chunk) u[i] = -1;
+        for (int e = 0; e < N; ++e) acc[e] = 0.f;
+        int ids_next = 32 + lane < cnt ? a.nbr_idx[beg + 32 + lane] : 0;      // the chunk after `ids`
+        for (int t = 0; t < cnt; t += BATCH) {
+            float s[UN], m_new = m, mw_new = mw;
+#pragma unroll
+            for (int i = 0; i < UN; ++i) {
+                float dot = row[i].dot(q);
+#pragma unroll
+                for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                s[i] = t + GROUPS * i + grp < cnt ? dot * q.c * scale_k(row[i].pair) : -INFINITY;
+                if (i == 0 && cnt == 1 && grp == 0) s[0] = 0.f;               // softmax over one member: weight exactly 1
+                m_new = fmaxf(m_new, s[i]);
+                if (BF16) mw_new = fmaxf(mw_new, s[i] + log2_scale_v(row[i].pair) - 14.f);
+            }
+            const float ref = finite(m_new), keep = fast_exp2(m - ref);       // one rescale per batch; 0 for the first
+            const float ref_w = finite(mw_new), keep_w = BF16 ? fast_exp2(mw - ref_w) : keep;
+            z *= keep;
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] *= keep_w;
+            m = m_new;
+            mw = mw_new;
+            // where the next batch comes from
+            int next = t + BATCH, from = ids, left = cnt;
+            const bool same = next < cnt;
+            if (same) {
+                if ((next & 31) == 0) {
+                    from = ids = ids_next;
+                    ids_next = next + 32 + lane < cnt ? a.nbr_idx[beg + next + 32 + lane] : 0;
                 }
+                left = cnt - (next & ~31);
+            } else {
+                from = u1;
+                left = cnt1;
+                next = 0;
+            }
+            const bool more = same || v1 >= 0;
 #pragma unroll
-                for (int i = 0; i < UN; ++i) {
-                    if (u[i] >= 0) {
-                        const uint8_t* row = a.T + (int64_t)u[i] * a.ldt;
-                        kv[i] = ld_piece_nc(row + sub * 16);
-                        pair[i] = ld_pair(row + kCodeBytes + 2 * (sub / LPH));
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < UN; ++i) {
-                    float dot = u[i] >= 0 ? dot8(q, kv[i]) : 0.f;
-#pragma unroll
-                    for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(hmask, dot, o);
-                    s[i] = u[i] >= 0 ? dot * scale_of(pair[i] & 255u) * a.c : -INFINITY;
-                    m_new = fmaxf(m_new, s[i]);
-                }
-                if (u[0] >= 0) {                                    // a batch's first slot is its lowest position
-                    // scores of -inf alone: measured against 0 they weigh nothing, instead of inf - inf
-                    const float ref = m_new == -INFINITY ? 0.f : m_new;
-                    const float keep = fast_exp2(m - ref);          // 0 for the first batch
-                    z *= keep;
-#pragma unroll
-                    for (int e = 0; e < kEl; ++e) acc[e] *= keep;
-#pragma unroll
-                    for (int i = 0; i < UN; ++i) {
-                        if (u[i] >= 0) {
-                            const float p = fast_exp2(s[i] - ref);
-                            z += p;
-                            add8(p * scale_of(pair[i] >> 8), kv[i], acc);
-                        }
-                    }
-                    m = m_new;
-                }
+            for (int i = 0; i < UN; ++i) {
+                const float p = fast_exp2(s[i] - ref);
+                z += p;
+                const float w = BF16 ? fast_exp2(s[i] + log2_scale_v(row[i].pair) - ref_w) : p * scale_v(row[i].pair);
+                if (t + GROUPS * i + grp < cnt) row[i].add(w, acc);
+                const int u = __shfl_sync(0xffffffffu, from, min((next & 31) + GROUPS * i + grp, min(left, 32) - 1) & 31);
+                if (more) row[i].load(codes, exps, (uint32_t)u, a.ldt);
             }
         }
-        const float m2 = __shfl_xor_sync(0xffffffffu, m, 16), z2 = __shfl_xor_sync(0xffffffffu, z, 16);
-        const float mm = fmaxf(m, m2);
-        const float w1 = m == -INFINITY ? 0.f : fast_exp2(m - mm), w2 = m2 == -INFINITY ? 0.f : fast_exp2(m2 - mm);
-        const float inv = cnt == 1 ? 1.f : fast_rcp(z * w1 + z2 * w2);
+        if (!BF16) mw = m;
 #pragma unroll
-        for (int e = 0; e < kEl; ++e) acc[e] = (acc[e] * w1 + __shfl_xor_sync(0xffffffffu, acc[e], 16) * w2) * inv;
-        if (half == 0) store8<BF16>((char*)a.O + (int64_t)v * a.ldo, sub, acc);
+        for (int o = LANES; o < 32; o <<= 1) {                                // merge the groups
+            const float m2 = __shfl_xor_sync(0xffffffffu, m, o), z2 = __shfl_xor_sync(0xffffffffu, z, o);
+            const float mw2 = __shfl_xor_sync(0xffffffffu, mw, o);
+            const float mm = fmaxf(m, m2), mmw = fmaxf(mw, mw2);
+            z = z * fast_exp2(m - finite(mm)) + z2 * fast_exp2(m2 - finite(mm));
+            const float w1 = fast_exp2(mw - finite(mmw)), w2 = fast_exp2(mw2 - finite(mmw));
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] = acc[e] * w1 + __shfl_xor_sync(0xffffffffu, acc[e], o) * w2;
+            m = mm;
+            mw = mmw;
+        }
+        // the two references differ by at most some 2^150: that power is put on in two halves
+        const float inv = fast_rcp(z), half = BF16 ? fast_exp2(0.5f * (finite(mw) - finite(m))) : 1.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] = BF16 ? acc[e] * half * inv * half : acc[e] * inv;
+        if (grp == 0) store_row<BF16, LANES>((char*)a.O + (int64_t)v * a.ldo, sub, acc);
+        v = v1; beg = beg1; cnt = cnt1; ids = u1;
+        fetch();
     }
 }
 
@@ -257,15 +424,22 @@ __global__ void __launch_bounds__(256, 3) sparse_attn_kv8_wide_kernel(AttnArgs a
 #define CHECK(expr) do { dg4_status _s = (expr); if (_s != DG4_OK) return _s; } while (0)
 
 // grid: as many blocks as the work needs, at most what the device holds at once
-template <typename Kernel, typename Args>
-dg4_status launch(Kernel kernel, const Args& args, int64_t per_block, cudaStream_t st) {
-    int dev = 0, sms = 0, per_sm = 0;
+template <auto kKernel, typename Args>
+dg4_status launch(const Args& args, int64_t per_block, cudaStream_t st) {
+    static std::atomic<int> resident[64];      // blocks of this kernel the device holds, 0 = not asked yet
+    int dev = 0;
     DG4_CUDA_TRY(cudaGetDevice(&dev));
-    DG4_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    DG4_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, 256, 0));
+    if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
+    int most = resident[dev].load(std::memory_order_relaxed);
+    if (most == 0) {
+        int sms = 0, per_sm = 0;
+        DG4_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        DG4_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kKernel, 256, 0));
+        most = sms * (per_sm > 0 ? per_sm : 1);
+        resident[dev].store(most, std::memory_order_relaxed);
+    }
     const int64_t needed = ((int64_t)args.count + per_block - 1) / per_block;
-    const int64_t resident = (int64_t)sms * (per_sm > 0 ? per_sm : 1);
-    kernel<<<(unsigned)(needed < resident ? needed : resident), 256, 0, st>>>(args);
+    kKernel<<<(unsigned)(needed < most ? needed : most), 256, 0, st>>>(args);
     dg4i_count_launch();
     DG4_CUDA_TRY(cudaGetLastError());
     return DG4_OK;
@@ -273,7 +447,10 @@ dg4_status launch(Kernel kernel, const Args& args, int64_t per_block, cudaStream
 
 dg4_status check_table(const dg4_desc* d, const void* T, int64_t ldt) {
     if (d->heads > 16) DG4_FAIL(DG4_ERR_UNSUPPORTED, "heads = %d: the 8-bit table has at most 16", d->heads);
-    return dg4i_check_tensor("T", T, ldt, 1, DG4_KV8_ROW_BYTES);
+    if (ldt > 0x7fffffff) DG4_FAIL(DG4_ERR_UNSUPPORTED, "the table's rows are %lld bytes apart: 2^31 - 1 at most", (long long)ldt);
+    CHECK(dg4i_check_tensor("T", T, ldt, 1, DG4_KV8_ROW_BYTES));
+    if ((((uintptr_t)T) | (uintptr_t)ldt) & 31u) DG4_FAIL(DG4_ERR_INVALID_ARG, "the table or its row distance is not a multiple of 32 bytes");
+    return DG4_OK;
 }
 
 dg4_status check_nodes(const dg4_graph* g, const int32_t* nodes, int32_t count) {
@@ -293,10 +470,12 @@ dg4_status check_nodes(const dg4_graph* g, const int32_t* nodes, int32_t count) 
         default: return LAUNCH(BF16, 16, ##__VA_ARGS__);                                     \
     }
 
-#define WRITE(BF16, LPH) launch(kv8_write_kernel<BF16, LPH>, a, 256 / kLanes, st)
-#define READ(BF16, LPH) launch(kv8_read_kernel<BF16, LPH>, a, 256 / kLanes, st)
-#define ATTN(BF16, LPH, MAXN) launch(sparse_attn_kv8_kernel<BF16, LPH, MAXN>, a, 256 / kLanes, st)
-#define ATTN_WIDE(BF16, LPH) launch(sparse_attn_kv8_wide_kernel<BF16, LPH>, a, 256 / 32, st)
+#define WRITE(BF16, LPH) launch<kv8_write_kernel<BF16, LPH>>(a, 256 / kLanes, st)
+#define READ(BF16, LPH) launch<kv8_read_kernel<BF16, LPH>>(a, 256 / kLanes, st)
+// LPH counts lanes of 8 elements: with two pieces per lane a head spans half as many
+#define ATTN(BF16, LPH, MAXN) \
+    launch<sparse_attn_kv8_kernel<BF16, LPH == 1 ? 16 : 8, LPH == 1 ? 1 : LPH / 2, MAXN>>(a, LPH == 1 ? 16 : 32, st)
+#define ATTN_WIDE(BF16, LPH) launch<sparse_attn_kv8_wide_kernel<BF16, LPH == 1 ? 16 : 8, LPH == 1 ? 1 : LPH / 2>>(a, 8, st)
 
 dg4_status copy_call(const dg4_graph* g, const dg4_desc* desc, const void* K, int64_t ldk, const void* V, int64_t ldv,
                      const void* T, int64_t ldt, const int32_t* nodes, int32_t count, bool write, void* stream) {
@@ -348,7 +527,7 @@ extern "C" dg4_status dg4_sparse_attn_kv8_fwd(const dg4_graph* g, const dg4_desc
     CHECK(check_nodes(g, nodes, count));
     if (nodes && O == Q) DG4_FAIL(DG4_ERR_INVALID_ARG, "O may not be Q for a list of nodes (one that is named twice would be read after it was written)");
     AttnArgs a;
-    a.Q = Q; a.ldq = ldq * es; a.T = (const uint8_t*)T; a.ldt = ldt; a.O = O; a.ldo = ldo * es;
+    a.Q = Q; a.ldq = ldq * es; a.T = (const uint8_t*)T; a.ldt = (uint32_t)ldt; a.O = O; a.ldo = ldo * es;
     a.nodes = nodes; a.count = nodes ? count : g->n; a.n = g->n;
     a.nbr_pad = g->nbr_pad; a.nbr_ptr = g->nbr_ptr; a.nbr_idx = g->nbr_idx;
     a.c = desc->scale * 1.4426950408889634f;

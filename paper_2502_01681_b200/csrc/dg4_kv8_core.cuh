@@ -51,8 +51,13 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
     const int b = (int)((top + 0x1fffffu) >> 23) - 8;
     return (uint32_t)(b > 0 ? b : 0);
 }
-// 2^(b - 127); 2^-127 is subnormal in fp32, 255 gives an infinity (which a NaN code turns into NaN)
-__device__ __forceinline__ float scale_of(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x00400000u); }
+// 2^(b - 127) of the K byte (low) and of the V byte (high) of a head's pair.  2^-127 (b = 0) is subnormal in fp32 and
+// has the pattern 0x00400000, below that of every b > 0, so a maximum puts it in; 255 gives an infinity, which the NaN
+// codes that go with it turn into NaN.
+__device__ __forceinline__ float scale_k(uint32_t pair) { return __uint_as_float(max((pair << 23) & 0x7f800000u, 0x00400000u)); }
+__device__ __forceinline__ float scale_v(uint32_t pair) { return __uint_as_float(max((pair << 15) & 0x7f800000u, 0x00400000u)); }
+// log2 of the V scale: the byte becomes the low mantissa bits of 2^23 + b
+__device__ __forceinline__ float log2_scale_v(uint32_t pair) { return __uint_as_float(0x4b000000u | (pair >> 8)) - 8388735.f; }
 
 // 8 values -> 8 codes.  The slice's scale is 2^(b - 127), so the factor 2^(127 - b) has the exponent field 254 - b;
 // b <= 247 for a finite slice, so the factor is a normal number and the product is exact (or far below e4m3's range).
@@ -71,13 +76,16 @@ __device__ __forceinline__ void encode8(const float* f, uint32_t b, uint32_t* ou
     }
 }
 
-// 4 codes -> 4 floats (every e4m3 number is an fp16 number)
-__device__ __forceinline__ void decode4(uint32_t w, float* f) {
-    uint32_t lo, hi;
+// 4 codes -> 2 pairs of fp16 (every e4m3 number is an fp16 number), or 4 floats
+__device__ __forceinline__ void decode4_half(uint32_t w, uint32_t* h) {
     asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
-        : "=r"(lo), "=r"(hi) : "r"(w));
-    const float2 x = __half22float2(*reinterpret_cast<__half2*>(&lo));
-    const float2 y = __half22float2(*reinterpret_cast<__half2*>(&hi));
+        : "=r"(h[0]), "=r"(h[1]) : "r"(w));
+}
+__device__ __forceinline__ void decode4(uint32_t w, float* f) {
+    uint32_t h[2];
+    decode4_half(w, h);
+    const float2 x = __half22float2(*reinterpret_cast<__half2*>(&h[0]));
+    const float2 y = __half22float2(*reinterpret_cast<__half2*>(&h[1]));
     f[0] = x.x; f[1] = x.y; f[2] = y.x; f[3] = y.y;
 }
 

@@ -208,12 +208,13 @@ def _i32(a):
 def _stream(stream):
     if stream is None:
         import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-    return ctypes.c_void_p(int(getattr(stream, "cuda_stream", stream)))     # a raw handle or a torch stream
+        # the raw handle, without a stream object around it: 0.4 instead of 3.6 us of a call that takes about 8
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return int(getattr(stream, "cuda_stream", stream))                      # a raw handle or a torch stream
 
 
 def _ptr(t):
-    return ctypes.c_void_p(t.data_ptr()) if t is not None else None
+    return t.data_ptr() if t is not None else None
 
 
 def _ld(t):

@@ -315,7 +315,7 @@ def hard_rows(seed, n, dtype):
 def test_kv8_codes_are_the_definition_bit_for_bit(heads, n, dtype):
     g = edgeless(n)
     k, v = hard_rows(1, n, dtype), hard_rows(2, n, dtype).flip(0).contiguous()
-    t = torch.full((n, 304), 9, dtype=torch.uint8, device="cuda")
+    t = torch.full((n, 320), 9, dtype=torch.uint8, device="cuda")
     dg4.dg4_kv8_write(g, desc(heads, dtype), k, v, t)
     want, vals = table_ref(k, v, heads)
     assert torch.equal(t[:, :288].cpu(), want)
@@ -378,6 +378,12 @@ def attn_ref(q, k, v, lists, heads, scale, nodes, dtype):
             # exponential and the reciprocal are good to 2^-21; sums over the members
             ds = (128 / heads + 8) * U32 * (scale * (kk.abs() @ qq.abs())).max() + 4 * U32 * s.abs().max()
             rel = 2 * (2 * ds + 2.0 ** -21) + (2 * len(u) + 8) * U32
+            if dtype == BF16:
+                # the query in fp16 is exact down to 2^-25 of its largest element and off by 2^-40 of that below it
+                rel += 4 * scale * 2.0 ** -40 * float((kk.abs().sum(1) * qq.abs().max()).max())
+                # each weight is rounded to fp16: half a step of 2^-11 relative to it; the exponents' own rounding in
+                # the wide form: half a step of a number below 128 + |score| in log2 units, three times
+                rel += 2.0 ** -11 + 3 * 2.0 ** -24 * (128 + 2 * s.abs().max())
             o[r, at] = p @ vv
             mag = p @ vv.abs()
             tol[r, at] = rel * mag * 1.01 + HALF[dtype] * (o[r, at].abs() + rel * mag) + 1e-300
@@ -661,7 +667,7 @@ def test_refusals():
     f = torch.float32
     refused(uns, dg4.dg4_kv8_write, g, desc(32, f), x.float(), x.float(), t)
     refused(inv, dg4.dg4_kv8_write, g, desc(), x, x, torch.zeros((n, 272), dtype=torch.uint8, device="cuda"))
-    refused(inv, dg4.dg4_kv8_read, g, desc(), torch.zeros((n, 296), dtype=torch.uint8, device="cuda"), q, k)
+    refused(inv, dg4.dg4_kv8_read, g, desc(), torch.zeros((n, 304), dtype=torch.uint8, device="cuda"), q, k)
     refused(inv, dg4.dg4_sparse_attn_kv8_fwd, g, desc(), x, t, x, i32([0]))
     refused(inv, dg4.dg4_sparse_attn_kv8_fwd, g, desc(), x, torch.zeros(n * 288 + 8, dtype=torch.uint8, device="cuda")[8:].view(n, 288), q)
     one = (torch.ones(128, device="cuda"), None)
