@@ -46,7 +46,15 @@ constexpr int kTmemCols = 512;
 constexpr int kColU = kSlots * 128;               // U in fp32: 64 columns
 constexpr int kColUb = kColU + 64;                // U in bf16: 32 columns
 constexpr int kRankMax = 64;
-constexpr int kABytes = kRankMax * 256;           // A_a: two halves of rank rows x 128 bytes
+
+// The adapter's place in shared memory, for ranks up to 64 and up to 32: A_a is two halves of RANK rows x 128 bytes,
+// B_a per column block 128 rows of RANK columns (128-byte or 64-byte swizzle; the columns past the rank are zero).  The
+// smaller place leaves room for a second X stage beside the whole of W_qkv.
+template <int RANK> struct Place {
+    static constexpr int kA = RANK * 256, kAHalf = kA / 2;
+    static constexpr int kB = 128 * RANK * 2;
+    __device__ static __forceinline__ uint64_t b_desc(uint32_t addr) { return RANK == 64 ? smem_desc_sw128(addr) : smem_desc_sw64(addr); }
+};
 
 struct Item {
     int32_t row0, rows;
@@ -186,10 +194,12 @@ __device__ __forceinline__ void find_items(const Params& p, Bars* bars) {
     }
 }
 
+template <int RANK>
 __global__ void __launch_bounds__(kThreads, 1)
 adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                     const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_a,
                     const __grid_constant__ CUtensorMap map_b, const __grid_constant__ OutMaps map_o, Params p) {
+    using P = Place<RANK>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + p.off_bar);
@@ -267,10 +277,10 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     // the previous adapter's last products (load index `loads` - 1) must have read it
                     if (!mbar_wait(smem_u32(&bars->ad_empty), ((uint32_t)loads & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
                     const uint32_t ad = smem_u32(&bars->ad_full);
-                    mbar_expect_tx(ad, (uint32_t)(p.rank * 256 + nb * kHalfBytes));
-                    for (int h = 0; h < 2; ++h) tma_load_2d(sA + h * (kABytes / 2), &map_a, h * 64, it.adapter * p.rank, ad);
+                    mbar_expect_tx(ad, (uint32_t)(p.rank * 256 + nb * P::kB));
+                    for (int h = 0; h < 2; ++h) tma_load_2d(sA + h * P::kAHalf, &map_a, h * 64, it.adapter * p.rank, ad);
                     for (int j = 0; j < nb; ++j)
-                        tma_load_2d(sB + j * kHalfBytes, &map_b, 0, it.adapter * p.n_out + (block0 + j) * 128, ad);
+                        tma_load_2d(sB + j * P::kB, &map_b, 0, it.adapter * p.n_out + (block0 + j) * 128, ad);
                     ++loads;
                     held = it.adapter;
                 }
@@ -306,7 +316,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
                         mma_bf16(tmem + kColU, smem_desc_sw128(x_base + (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32)),
-                                 smem_desc_sw128(sA + (uint32_t)((ks >> 2) * (kABytes / 2) + (ks & 3) * 32)), idesc_u, ks > 0 ? 1u : 0u);
+                                 smem_desc_sw128(sA + (uint32_t)((ks >> 2) * P::kAHalf + (ks & 3) * 32)), idesc_u, ks > 0 ? 1u : 0u);
                     mma_commit(smem_u32(&bars->u_full));
                 }
                 for (int j = 0; j < nb; ++j) {
@@ -332,7 +342,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                         const int slot = (block + j) % kSlots;
                         for (int ks = 0; ks < rank16 / 16; ++ks)
                             mma_bf16_ta(tmem + (uint32_t)(slot * 128), tmem + (uint32_t)(kColUb + ks * 8),
-                                        smem_desc_sw128(sB + (uint32_t)(j * kHalfBytes + ks * 32)), idesc, 1u);
+                                        P::b_desc(sB + (uint32_t)(j * P::kB + ks * 32)), idesc, 1u);
                         mma_commit(smem_u32(&bars->acc_full[slot]));
                     }
                     mma_commit(smem_u32(&bars->ub_empty));
@@ -476,10 +486,6 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
 
 constexpr int kSmemLimit = 232448;                // what one CTA may hold
 
-std::mutex g_mu;
-bool g_attr_set[64] = {};
-int g_sm_count[64] = {};
-
 struct Call {
     const void* X; int64_t ldx;
     const void* W;
@@ -490,16 +496,21 @@ struct Call {
     int n_out;
 };
 
+template <int RANK>
 dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
+    using P = Place<RANK>;
+    static std::mutex mu;
+    static bool attr_set[64] = {};
+    static int sm_count[64] = {};
     int dev = 0;
     DG4_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
     {
-        std::lock_guard<std::mutex> lock(g_mu);
-        if (!g_attr_set[dev]) {
-            DG4_CUDA_TRY(cudaFuncSetAttribute(adapter_proj_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
-            DG4_CUDA_TRY(cudaDeviceGetAttribute(&g_sm_count[dev], cudaDevAttrMultiProcessorCount, dev));
-            g_attr_set[dev] = true;
+        std::lock_guard<std::mutex> lock(mu);
+        if (!attr_set[dev]) {
+            DG4_CUDA_TRY(cudaFuncSetAttribute(adapter_proj_kernel<RANK>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
+            DG4_CUDA_TRY(cudaDeviceGetAttribute(&sm_count[dev], cudaDevAttrMultiProcessorCount, dev));
+            attr_set[dev] = true;
         }
     }
     Params p;
@@ -509,14 +520,14 @@ dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
     p.n = g->n; p.n_adapters = c.ad->n_adapters; p.rank = c.ad->rank; p.scale = c.ad->scale;
     p.n_out = c.n_out; p.has_res = c.R != nullptr;
     p.status = g->dev_status; p.poll_limit = dg4i_poll_limit();
-    const int blocks = c.n_out / 128, sms = g_sm_count[dev];
+    const int blocks = c.n_out / 128, sms = sm_count[dev];
     // items: at most one per full tile and one ragged one per request
     const int64_t most = (int64_t)g->n / kTileM + p.n_seg;
     const bool split = most * blocks <= sms;
     p.nb = split ? 1 : blocks;
     int off = p.nb * kTileBytes;
-    p.off_a = off; off += kABytes;
-    p.off_b = off; off += p.nb * kHalfBytes;
+    p.off_a = off; off += P::kA;
+    p.off_b = off; off += p.nb * P::kB;
     p.off_stage = off; off += kEpiWarps * 4096;
     const int per_stage = kTileBytes * (p.has_res ? 2 : 1), tail = (int)sizeof(Bars) + 1024;
     p.stages = off + kMaxStages * per_stage + tail <= kSmemLimit ? kMaxStages : 1;
@@ -530,7 +541,7 @@ dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
     map_r = map_x;
     if (c.R) CHECK(dg4i_make_row_map(&map_r, c.R, g->n, c.ldr, 128));
     CHECK(dg4i_make_row_map(&map_a, c.ad->A, (int64_t)c.ad->n_adapters * c.ad->rank, 128, c.ad->rank));
-    CHECK(dg4i_make_map(&map_b, c.ad->B, c.ad->rank, (int64_t)c.ad->n_adapters * c.n_out, c.ad->rank, 128));
+    CHECK(dg4i_make_map(&map_b, c.ad->B, c.ad->rank, (int64_t)c.ad->n_adapters * c.n_out, c.ad->rank, 128, RANK));
     for (int j = 0; j < 3; ++j) {
         map_o.m[j] = map_x;
         p.out[j] = nullptr; p.ldo[j] = 0;
@@ -540,10 +551,14 @@ dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
         }
     }
     const dim3 grid((unsigned)(most < sms ? most : sms), (unsigned)(blocks / p.nb));
-    adapter_proj_kernel<<<grid, kThreads, off, st>>>(map_x, map_w, map_r, map_a, map_b, map_o, p);
+    adapter_proj_kernel<RANK><<<grid, kThreads, off, st>>>(map_x, map_w, map_r, map_a, map_b, map_o, p);
     dg4i_count_launch();
     DG4_CUDA_TRY(cudaGetLastError());
     return DG4_OK;
+}
+
+dg4_status launch_rank(const dg4_graph* g, const Call& c, cudaStream_t st) {
+    return c.ad->rank <= 32 ? launch<32>(g, c, st) : launch<64>(g, c, st);
 }
 
 dg4_status check_adapters(const dg4_adapters* ad, int n_out) {
@@ -575,7 +590,7 @@ extern "C" dg4_status dg4_qkv_project_adapters(const dg4_graph* g, const dg4_des
     CHECK(dg4i_check_tensor("K", K, ldk, 2, 128));
     CHECK(dg4i_check_tensor("V", V, ldv, 2, 128));
     Call c = {X, ldx, W_qkv, adapters, segments, nullptr, 0, {Q, K, V}, {ldq, ldk, ldv}, 384};
-    return launch(g, c, (cudaStream_t)stream);
+    return launch_rank(g, c, (cudaStream_t)stream);
 }
 
 extern "C" dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_desc* desc, const void* O, int64_t ldo,
@@ -592,5 +607,5 @@ extern "C" dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_des
     if (res) CHECK(dg4i_check_tensor("H_res", H_res, ldh, 2, 128));
     CHECK(dg4i_check_tensor("H_out", H_out, ldho, 2, 128));
     Call c = {O, ldo, W_o, adapters, segments, res ? H_res : nullptr, ldh, {H_out, nullptr, nullptr}, {ldho, 0, 0}, 128};
-    return launch(g, c, (cudaStream_t)stream);
+    return launch_rank(g, c, (cudaStream_t)stream);
 }

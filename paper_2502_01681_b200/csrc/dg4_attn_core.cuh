@@ -60,6 +60,11 @@ __device__ __forceinline__ void st_piece_stream(void* p, const Piece& v) {
                  :: "l"(p), "r"(v.w[0]), "r"(v.w[1]), "r"(v.w[2]), "r"(v.w[3]) : "memory");
 }
 
+__device__ __forceinline__ void st_pieces2_stream(void* p, const Piece& a, const Piece& b) {       // 32-byte aligned
+    asm volatile("st.global.cs.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "l"(p), "r"(a.w[0]), "r"(a.w[1]), "r"(a.w[2]), "r"(a.w[3]), "r"(b.w[0]), "r"(b.w[1]), "r"(b.w[2]), "r"(b.w[3]) : "memory");
+}
+
 __device__ __forceinline__ float fast_exp2(float x) {      // 2^x, relative error about 2^-22
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

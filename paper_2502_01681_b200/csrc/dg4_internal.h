@@ -44,8 +44,9 @@ uint32_t dg4i_poll_limit();
 // box_rows rows, 128-byte swizzle, rows past the end read as zero and are clipped on store (dg4_project.cu).
 struct CUtensorMap_st;
 dg4_status dg4i_make_row_map(CUtensorMap_st* map, const void* base, int64_t rows, int64_t ld, int box_rows);
-// The same for [rows, cols] with fewer than 64 columns: the box's columns past the end read as zero.
-dg4_status dg4i_make_map(CUtensorMap_st* map, const void* base, int cols, int64_t rows, int64_t ld, int box_rows);
+// The same for [rows, cols] with boxes of box_cols = 64 columns, or of 32 with a 64-byte swizzle; a box's columns past
+// the end read as zero.
+dg4_status dg4i_make_map(CUtensorMap_st* map, const void* base, int cols, int64_t rows, int64_t ld, int box_rows, int box_cols);
 
 // ---- launch accounting (every kernel launch of the library bumps this counter) ------------------
 void dg4i_count_launch(int n = 1);

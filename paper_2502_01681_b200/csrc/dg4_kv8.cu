@@ -6,8 +6,7 @@
 
 #include "dg4_internal.h"
 #include "dg4_kv8_core.cuh"
-
-#include <atomic>
+#include "dg4_launch.cuh"
 
 namespace {
 
@@ -19,7 +18,8 @@ struct CopyArgs {
     void* V; int64_t ldv;
     uint8_t* T; int64_t ldt;
     const int32_t* nodes;              // nullable
-    int32_t count, n, heads;
+    int32_t count, n;
+    int32_t wide;                      // fp32 rows: bases and row distances are multiples of 32 bytes
 };
 
 // Largest magnitude bit pattern over the lanes of a head (LPH adjacent lanes): magnitudes of floats order like
@@ -34,27 +34,65 @@ __device__ __forceinline__ uint32_t slice_top(const float* f, unsigned mask) {
     return top;
 }
 
+// 8 elements of K and of V as they stand in memory.  fp32 rows whose 32 bytes per lane are aligned to that move with one
+// instruction (`wide`, the same for the whole launch).
+template <bool BF16> struct RawKV {
+    static constexpr int kPieces = BF16 ? 1 : 2;
+    Piece k[kPieces], v[kPieces];
+    __device__ __forceinline__ void load(const CopyArgs& a, int row, int sub) {
+        const char* pk = (const char*)a.K + (int64_t)row * a.ldk + sub * 16 * kPieces;
+        const char* pv = (const char*)a.V + (int64_t)row * a.ldv + sub * 16 * kPieces;
+        if (BF16) {
+            k[0] = ld_piece_stream(pk);
+            v[0] = ld_piece_stream(pv);
+        } else if (a.wide) {
+            ld_pieces2_nc(pk, k[0], k[kPieces - 1]);
+            ld_pieces2_nc(pv, v[0], v[kPieces - 1]);
+        } else {
+            k[0] = ld_piece_stream(pk); k[kPieces - 1] = ld_piece_stream(pk + 16);
+            v[0] = ld_piece_stream(pv); v[kPieces - 1] = ld_piece_stream(pv + 16);
+        }
+    }
+};
+
+// The id of the row a slot stands for, -1 for none (ids outside the table are skipped)
+__device__ __forceinline__ int row_of(const CopyArgs& a, uint32_t slot) {
+    int v = -1;
+    if (slot < (uint32_t)a.count) v = a.nodes ? a.nodes[slot] : (int)slot;
+    return (uint32_t)v < (uint32_t)a.n ? v : -1;
+}
+
+// In both kernels the next row's loads are in flight while this row is worked on and stored.
 template <bool BF16, int LPH>
 __global__ void __launch_bounds__(256) kv8_write_kernel(CopyArgs a) {
     const int lane = threadIdx.x & 31, sub = lane & 15, grp = lane - sub;
     const unsigned mask = 0xffffu << grp;
     const uint32_t stride = gridDim.x * (blockDim.x / kLanes);
-    for (uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) / kLanes; slot < (uint32_t)a.count; slot += stride) {
-        const int v = a.nodes ? a.nodes[slot] : (int)slot;
-        if ((uint32_t)v >= (uint32_t)a.n) continue;                 // ids outside the table are skipped
+    uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) / kLanes;
+    RawKV<BF16> raw;
+    int row_next = row_of(a, slot);
+    if (row_next >= 0) raw.load(a, row_next, sub);
+    for (; slot < (uint32_t)a.count; slot += stride) {
+        const int row = row_next;
         float k[kEl], w[kEl];
-        load8<BF16>((const char*)a.K + (int64_t)v * a.ldk, sub, k);
-        load8<BF16>((const char*)a.V + (int64_t)v * a.ldv, sub, w);
+#pragma unroll
+        for (int i = 0; i < RawKV<BF16>::kPieces; ++i) {
+            Elem<BF16>::unpack(raw.k[i], k + 4 * i);
+            Elem<BF16>::unpack(raw.v[i], w + 4 * i);
+        }
+        row_next = row_of(a, slot + stride);
+        if (row_next >= 0) raw.load(a, row_next, sub);
+        if (row < 0) continue;
         const uint32_t bk = scale_byte(slice_top<LPH>(k, mask)), bv = scale_byte(slice_top<LPH>(w, mask));
         Piece p;
         encode8(k, bk, p.w);
         encode8(w, bv, p.w + 2);
-        uint8_t* row = a.T + (int64_t)v * a.ldt;
-        *reinterpret_cast<Piece*>(row + sub * 16) = p;
+        uint8_t* t = a.T + (int64_t)row * a.ldt;
+        *reinterpret_cast<Piece*>(t + sub * 16) = p;
         // lane l writes the pair of head l (held by the lanes of that head), the lanes beyond the heads write zero
         const uint32_t mine = bk | (bv << 8);
         const uint32_t pair = __shfl_sync(mask, mine, grp + ((sub * LPH) & 15));
-        *reinterpret_cast<uint16_t*>(row + kCodeBytes + 2 * sub) = (uint16_t)(sub < 16 / LPH ? pair : 0u);
+        *reinterpret_cast<uint16_t*>(t + kCodeBytes + 2 * sub) = (uint16_t)(sub < 16 / LPH ? pair : 0u);
     }
 }
 
@@ -62,20 +100,40 @@ template <bool BF16, int LPH>
 __global__ void __launch_bounds__(256) kv8_read_kernel(CopyArgs a) {
     const int sub = threadIdx.x & 15;
     const uint32_t stride = gridDim.x * (blockDim.x / kLanes);
-    for (uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) / kLanes; slot < (uint32_t)a.count; slot += stride) {
-        const int v = a.nodes ? a.nodes[slot] : (int)slot;
-        if ((uint32_t)v >= (uint32_t)a.n) continue;
-        const uint8_t* row = a.T + (int64_t)v * a.ldt;
-        const Piece p = ld_piece_stream(row + sub * 16);
-        const uint32_t pair = ld_pair(row + kCodeBytes + 2 * (sub / LPH));
+    uint32_t slot = (blockIdx.x * blockDim.x + threadIdx.x) / kLanes;
+    Piece p_next;
+    uint32_t pair_next = 0;
+    int row_next = -1;
+    auto fetch = [&](uint32_t at) {
+        row_next = row_of(a, at);
+        if (row_next >= 0) {
+            const uint8_t* t = a.T + (int64_t)row_next * a.ldt;
+            p_next = ld_piece_stream(t + sub * 16);
+            pair_next = ld_pair(t + kCodeBytes + 2 * (sub / LPH));
+        }
+    };
+    fetch(slot);
+    for (; slot < (uint32_t)a.count; slot += stride) {
+        const int row = row_next;
+        const Piece p = p_next;
+        const uint32_t pair = pair_next;
+        fetch(slot + stride);
+        if (row < 0) continue;
         const float sk = scale_k(pair), sv = scale_v(pair);
         float k[kEl], w[kEl];
         decode4(p.w[0], k); decode4(p.w[1], k + 4);
         decode4(p.w[2], w); decode4(p.w[3], w + 4);
 #pragma unroll
         for (int i = 0; i < kEl; ++i) { k[i] *= sk; w[i] *= sv; }
-        store8<BF16>((char*)a.K + (int64_t)v * a.ldk, sub, k);
-        store8<BF16>((char*)a.V + (int64_t)v * a.ldv, sub, w);
+        char* pk = (char*)a.K + (int64_t)row * a.ldk;
+        char* pv = (char*)a.V + (int64_t)row * a.ldv;
+        if (!BF16 && a.wide) {
+            st_pieces2_stream(pk + sub * 32, Elem<BF16>::pack(k), Elem<BF16>::pack(k + 4));
+            st_pieces2_stream(pv + sub * 32, Elem<BF16>::pack(w), Elem<BF16>::pack(w + 4));
+        } else {
+            store8<BF16>(pk, sub, k);
+            store8<BF16>(pv, sub, w);
+        }
     }
 }
 
@@ -423,23 +481,12 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
 // ---------------------------------------------------------------------------------------------------
 #define CHECK(expr) do { dg4_status _s = (expr); if (_s != DG4_OK) return _s; } while (0)
 
-// grid: as many blocks as the work needs, at most what the device holds at once
 template <auto kKernel, typename Args>
 dg4_status launch(const Args& args, int64_t per_block, cudaStream_t st) {
-    static std::atomic<int> resident[64];      // blocks of this kernel the device holds, 0 = not asked yet
-    int dev = 0;
-    DG4_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
-    int most = resident[dev].load(std::memory_order_relaxed);
-    if (most == 0) {
-        int sms = 0, per_sm = 0;
-        DG4_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-        DG4_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kKernel, 256, 0));
-        most = sms * (per_sm > 0 ? per_sm : 1);
-        resident[dev].store(most, std::memory_order_relaxed);
-    }
+    int resident;
+    CHECK(dg4i_resident_blocks<kKernel>(256, &resident));
     const int64_t needed = ((int64_t)args.count + per_block - 1) / per_block;
-    kKernel<<<(unsigned)(needed < most ? needed : most), 256, 0, st>>>(args);
+    kKernel<<<(unsigned)(needed < resident ? needed : resident), 256, 0, st>>>(args);
     dg4i_count_launch();
     DG4_CUDA_TRY(cudaGetLastError());
     return DG4_OK;
@@ -490,7 +537,8 @@ dg4_status copy_call(const dg4_graph* g, const dg4_desc* desc, const void* K, in
     a.K = const_cast<void*>(K); a.ldk = ldk * es;
     a.V = const_cast<void*>(V); a.ldv = ldv * es;
     a.T = (uint8_t*)const_cast<void*>(T); a.ldt = ldt;
-    a.nodes = nodes; a.count = nodes ? count : g->n; a.n = g->n; a.heads = desc->heads;
+    a.nodes = nodes; a.count = nodes ? count : g->n; a.n = g->n;
+    a.wide = (((uintptr_t)K | (uintptr_t)V | (uintptr_t)a.ldk | (uintptr_t)a.ldv) & 31u) == 0;
     if (a.count == 0) return DG4_OK;
     const cudaStream_t st = (cudaStream_t)stream;
     if (write) {

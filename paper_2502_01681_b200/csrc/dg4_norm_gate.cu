@@ -4,19 +4,25 @@
 // and the two stores of a row stays in registers in 32 bits (Y is computed from the unrounded R'), so a bf16 row
 // costs 512 bytes in and 512 out, which is the bound: the arithmetic is some 20 operations per element.
 //
-// 16 lanes per row, 8 elements per lane; a warp walks chunks of up to 32 consecutive rows, its two halves on
-// alternate rows (fewer rows per chunk when there are not enough for every resident warp: two rows one after the
-// other cost twice a row's latency).  The request of a chunk's first row is found by a 16-way search over the offsets (each step one load and one
-// ballot), after that only when a row passes the end of its request.  Mean and variance are taken in two passes over
-// the registers, so a large common offset of a row does not cancel in the variance.
+// 8 lanes per row, 16 elements per lane, four consecutive rows per warp: a row's four sums then take 3 shuffles each for
+// four rows at once, and the arithmetic runs on pairs (packed fp32 instructions).  The norm vectors lie in shared memory
+// in the order the lanes read them, the gate in registers.  A warp walks chunks of up to 16 consecutive rows (32: 168 us, 8: 164, 4: 167); the next
+// four rows are loaded while four are worked on.  The request of a row is found by a 32-way search over the offsets
+// (each step one load and one ballot), only when the four rows leave the request last found; where they belong to
+// several requests, each row's lanes search for their own.  Mean and variance are taken in two passes over the
+// registers, so a large common offset of a row does not cancel in the variance.
 
 #include "dg4_internal.h"
-#include "dg4_kv8_core.cuh"
+#include "dg4_attn_core.cuh"
+#include "dg4_launch.cuh"
 
 namespace {
 
-constexpr int kMaxChunk = 32;              // rows a warp takes at a time, at most
-constexpr int kEl = 8;
+constexpr int kMaxChunk = 16;              // rows a warp takes at a time, at most
+constexpr int kRows = 4;                    // rows of a warp at a time
+constexpr int kLanes = 8;                   // lanes per row
+constexpr int kEl = 128 / kLanes;           // elements per lane
+constexpr int kPairs = kEl / 2;
 
 struct NormArgs {
     const void* S; int64_t lds;            // bytes
@@ -30,47 +36,89 @@ struct NormArgs {
     float res_scale, eps;
 };
 
-__device__ __forceinline__ void load_vec(const float* p, int sub, float fill, float* f) {
-    if (p) {
-        const float4 a = *reinterpret_cast<const float4*>(p + sub * kEl), b = *reinterpret_cast<const float4*>(p + sub * kEl + 4);
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    } else {
+// pairs of fp32 numbers in one 64-bit register, and the packed instructions on them
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ void split(Pair p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair c; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(a), "l"(b)); return c; }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair c; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(a), "l"(b)); return c; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+
+// Which four elements of a row the i-th quadruple of a lane is (counted in quadruples): a lane's loads are 16 bytes, 8
+// lanes side by side, so bf16 rows give it two neighbouring quadruples at a time and fp32 rows one.
+template <bool BF16> __device__ __forceinline__ int quad_of(int i, int sub) {
+    return BF16 ? 2 * (sub + kLanes * (i >> 1)) + (i & 1) : sub + kLanes * i;
+}
+
+// a lane's 16 elements of a row as they stand in memory, streamed
+template <bool BF16> struct Raw {
+    static constexpr int kPieces = BF16 ? 2 : 4;
+    attn::Piece p[kPieces];
+    __device__ __forceinline__ void load(const char* row, int sub) {
 #pragma unroll
-        for (int i = 0; i < kEl; ++i) f[i] = fill;
+        for (int i = 0; i < kPieces; ++i) p[i] = attn::ld_piece_stream(row + (sub + kLanes * i) * 16);
     }
-}
-
-__device__ __forceinline__ float row_sum(float x, unsigned mask) {
+    __device__ __forceinline__ Pair get(int i) const {               // pair i of the lane's 8
+        if (BF16) {
+            const uint32_t w = p[i >> 2].w[i & 3];
+            return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        }
+        return pair(__uint_as_float(p[BF16 ? 0 : i >> 1].w[2 * (i & 1)]), __uint_as_float(p[BF16 ? 0 : i >> 1].w[2 * (i & 1) + 1]));
+    }
+    __device__ static __forceinline__ void store(char* row, int sub, const Pair* x) {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(mask, x, o);
-    return x;
+        for (int i = 0; i < kPieces; ++i) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < kPairs / kPieces; ++e) split(x[i * (kPairs / kPieces) + e], f[2 * e], f[2 * e + 1]);
+            attn::st_piece_stream(row + (sub + kLanes * i) * 16, attn::Elem<BF16>::pack(f));
+        }
+    }
+};
+
+__device__ __forceinline__ float row_sum(const Pair* x) {            // over the 8 lanes of a row
+    const Pair t = add2(add2(add2(x[0], x[1]), add2(x[2], x[3])), add2(add2(x[4], x[5]), add2(x[6], x[7])));
+    float a, b;
+    split(t, a, b);
+    a += b;
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    return a;
 }
 
-// x := Norm(x) * gamma + beta for the row that the 16 lanes hold
+// x := Norm(x) * gamma + beta; v: gamma and beta as this lane reads them, quadruple after quadruple
 template <bool RMS>
-__device__ __forceinline__ void norm_row(float* x, const float* gamma, const float* beta, float eps, unsigned mask) {
+__device__ __forceinline__ void norm_row(Pair* x, const float4* gamma, const float4* beta, float eps) {
     if (!RMS) {
-        float s = 0.f;
+        const float mean = row_sum(x) * (1.f / 128.f);
+        const Pair m = pair(-mean, -mean);
 #pragma unroll
-        for (int i = 0; i < kEl; ++i) s += x[i];
-        const float mean = row_sum(s, mask) * (1.f / 128.f);
-#pragma unroll
-        for (int i = 0; i < kEl; ++i) x[i] -= mean;
+        for (int i = 0; i < kPairs; ++i) x[i] = add2(x[i], m);
     }
-    float q = 0.f;
+    Pair q[kPairs];
 #pragma unroll
-    for (int i = 0; i < kEl; ++i) q = fmaf(x[i], x[i], q);
-    const float inv = rsqrtf(row_sum(q, mask) * (1.f / 128.f) + eps);
+    for (int i = 0; i < kPairs; ++i) q[i] = mul2(x[i], x[i]);
+    const float inv = rsqrtf(row_sum(q) * (1.f / 128.f) + eps);
+    const Pair s = pair(inv, inv);
 #pragma unroll
-    for (int i = 0; i < kEl; ++i) x[i] = fmaf(x[i] * inv, gamma[i], beta[i]);
+    for (int i = 0; i < kPairs; i += 2) {
+        const float4 g = gamma[i / 2 * kLanes], b = beta[i / 2 * kLanes];
+        x[i] = fma2(mul2(x[i], s), pair(g.x, g.y), pair(b.x, b.y));
+        x[i + 1] = fma2(mul2(x[i + 1], s), pair(g.z, g.w), pair(b.z, b.w));
+    }
 }
 
-// The request of a row: the last s with seg_ptr[s] <= row, -1 if there is none.  All 16 lanes of `mask` call it.
-__device__ __forceinline__ int find_segment(const int32_t* seg_ptr, int n_seg, int row, int sub, unsigned mask) {
+// The request of a row: the last s with seg_ptr[s] <= row, -1 if there is none.  The lanes of `mask` call it together,
+// `ways` of them (a power of two), `me` counting them from 0.
+__device__ __forceinline__ int find_segment(const int32_t* seg_ptr, int n_seg, int row, int me, int ways, unsigned mask) {
     int lo = 0, hi = n_seg;                // entries below lo are <= row, entries from hi on are > row
     while (lo < hi) {
-        const int step = (hi - lo + 15) >> 4;
-        const int64_t at = (int64_t)lo + (int64_t)(sub + 1) * step - 1;
+        const int step = (int)(((uint32_t)(hi - lo) + ways - 1) / ways);
+        const int64_t at = (int64_t)lo + (int64_t)(me + 1) * step - 1;
         const bool below = at < hi && seg_ptr[at] <= row;
         const int c = __popc(__ballot_sync(mask, below) & mask);
         const int64_t next = (int64_t)lo + (int64_t)(c + 1) * step - 1;
@@ -81,46 +129,76 @@ __device__ __forceinline__ int find_segment(const int32_t* seg_ptr, int n_seg, i
 }
 
 template <bool BF16, bool RMS>
-__global__ void __launch_bounds__(256) norm_gate_kernel(NormArgs a) {
-    const int lane = threadIdx.x & 31, sub = lane & 15, half = lane >> 4;
-    const unsigned mask = 0xffffu << (lane - sub);
-    float post_g[kEl], post_b[kEl], pre_g[kEl], pre_b[kEl], gate[kEl];
-    load_vec(a.post_gamma, sub, 1.f, post_g);
-    load_vec(a.post_beta, sub, 0.f, post_b);
-    load_vec(a.Y ? a.pre_gamma : nullptr, sub, 1.f, pre_g);
-    load_vec(a.Y ? a.pre_beta : nullptr, sub, 0.f, pre_b);
-    load_vec(a.seg_ptr ? nullptr : a.gate, sub, 1.f, gate);
-    const int64_t chunks = ((int64_t)a.n + a.chunk - 1) / a.chunk;
-    const int64_t warps = (int64_t)gridDim.x * (blockDim.x >> 5);
-    for (int64_t chunk = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; chunk < chunks; chunk += warps) {
-        int end = a.seg_ptr ? -1 : a.n;    // rows below `end` belong to the request whose gate is held
-        bool covered = true;
-        for (int i = half; i < a.chunk; i += 2) {
-            const int64_t row = chunk * a.chunk + i;
-            if (row >= a.n) break;
-            if (row >= end) {
-                const int s = find_segment(a.seg_ptr, a.n_seg, (int)row, sub, mask);
-                covered = s >= 0 && row < a.seg_ptr[s + 1];
-                end = s + 1 <= a.n_seg ? a.seg_ptr[s + 1] : a.n;
-                if (end <= row) end = a.n;                      // behind the last request: nothing more is written
-                if (covered) {
-                    const int id = a.seg_id[s];
-                    load_vec((uint32_t)id < (uint32_t)a.n_gates && a.gate ? a.gate + (int64_t)id * 128 : nullptr, sub, 1.f, gate);
-                }
-            }
-            if (!covered) continue;
-            float x[kEl], r[kEl];
-            kv8::load8<BF16>((const char*)a.S + row * a.lds, sub, x);
-            kv8::load8<BF16>((const char*)a.R + row * a.ldr, sub, r);
-            norm_row<RMS>(x, post_g, post_b, a.eps, mask);
+__global__ void __launch_bounds__(256, 2) norm_gate_kernel(NormArgs a) {
+    __shared__ float4 vec[4][32];
+    const int lane = threadIdx.x & 31, sub = lane & (kLanes - 1), grp = lane / kLanes;
+    if (threadIdx.x < 128) {                                         // place i * 8 + sub holds quad_of(i, sub)
+        const int v = threadIdx.x >> 5, t = threadIdx.x & 31;
+        const float* p = v == 0 ? a.post_gamma : v == 1 ? a.post_beta : v == 2 ? a.pre_gamma : a.pre_beta;
+        const float fill = (v & 1) ? 0.f : 1.f;
+        if (!a.Y && v >= 2) p = nullptr;
+        vec[v][t] = p ? reinterpret_cast<const float4*>(p)[quad_of<BF16>(t / kLanes, t & (kLanes - 1))] : make_float4(fill, fill, fill, fill);
+    }
+    __syncthreads();
+    Pair gate[kPairs];
+    auto set_gate = [&](int id) {
+        const float4* p = reinterpret_cast<const float4*>(a.gate) + (int64_t)id * 32;
+        const bool has = a.gate && (uint32_t)id < (uint32_t)a.n_gates;
 #pragma unroll
-            for (int e = 0; e < kEl; ++e) x[e] = fmaf(gate[e], x[e], a.res_scale * r[e]);
-            kv8::store8<BF16>((char*)a.R_out + row * a.ldro, sub, x);
-            if (a.Y) {
-                norm_row<RMS>(x, pre_g, pre_b, a.eps, mask);
-                kv8::store8<BF16>((char*)a.Y + row * a.ldy, sub, x);
-            }
+        for (int i = 0; i < kPairs / 2; ++i) {
+            const float4 g = has ? p[quad_of<BF16>(i, sub)] : make_float4(1.f, 1.f, 1.f, 1.f);
+            gate[2 * i] = pair(g.x, g.y);
+            gate[2 * i + 1] = pair(g.z, g.w);
         }
+    };
+    const uint32_t step = gridDim.x * (blockDim.x >> 5) * a.chunk;
+    uint32_t chunk = ((blockIdx.x * blockDim.x + threadIdx.x) >> 5) * a.chunk;
+    uint32_t row0 = chunk;                                           // the first of the four rows
+    const uint32_t n = (uint32_t)a.n;
+    bool covered = true;                                             // this lane's row belongs to a request
+    uint32_t end = n;                                                // rows below it have this `gate` and `covered`
+    if (a.seg_ptr) end = 0;
+    else set_gate(0);
+    Raw<BF16> s_next, r_next;
+    auto fetch = [&](uint32_t row) {
+        if (row < n) {
+            s_next.load((const char*)a.S + (int64_t)row * a.lds, sub);
+            r_next.load((const char*)a.R + (int64_t)row * a.ldr, sub);
+        }
+    };
+    fetch(row0 + grp);
+    const Pair rs = pair(a.res_scale, a.res_scale);
+    while (row0 < n) {                                               // the whole warp
+        const uint32_t row = row0 + grp;
+        Pair x[kPairs], r[kPairs];
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) { x[i] = s_next.get(i); r[i] = r_next.get(i); }
+        uint32_t next = row0 + kRows;
+        if (next >= chunk + a.chunk) next = chunk += step;
+        fetch(next + grp);
+        if (min(row0 + kRows, n) > end) {
+            int s = find_segment(a.seg_ptr, a.n_seg, (int)row0, lane, 32, 0xffffffffu);
+            // between the end of request s and the beginning of the next non-empty one there may be rows of none
+            const int to = a.seg_ptr[s + 1];
+            end = to > (int)row0 ? (uint32_t)to : n;                 // behind the last request nothing is written
+            covered = s >= 0 && to > (int)row0;
+            if (min(row0 + kRows, n) > end) {                        // several requests: each row for itself, this once
+                s = find_segment(a.seg_ptr, a.n_seg, (int)min(row, n - 1), sub, kLanes, 0xffu << (lane - sub));
+                covered = s >= 0 && a.seg_ptr[s + 1] > (int)row;
+                end = 0;
+            }
+            if (covered) set_gate(a.seg_id[s]);
+        }
+        norm_row<RMS>(x, &vec[0][sub], &vec[1][sub], a.eps);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) x[i] = fma2(gate[i], x[i], mul2(rs, r[i]));
+        const bool writes = covered && row < n;
+        if (writes) Raw<BF16>::store((char*)a.R_out + (int64_t)row * a.ldro, sub, x);
+        if (a.Y) {
+            norm_row<RMS>(x, &vec[2][sub], &vec[3][sub], a.eps);
+            if (writes) Raw<BF16>::store((char*)a.Y + (int64_t)row * a.ldy, sub, x);
+        }
+        row0 = next;
     }
 }
 
@@ -135,13 +213,10 @@ dg4_status check_vec(const char* name, const void* p, bool optional) {
 
 template <bool BF16, bool RMS>
 dg4_status launch(NormArgs a, cudaStream_t st) {
-    int dev = 0, sms = 0, per_sm = 0;
-    DG4_CUDA_TRY(cudaGetDevice(&dev));
-    DG4_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    DG4_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, norm_gate_kernel<BF16, RMS>, 256, 0));
-    const int64_t resident = (int64_t)sms * (per_sm > 0 ? per_sm : 1);
-    const int64_t share = ((int64_t)a.n + 16 * resident - 1) / (16 * resident);      // rows of a half-warp
-    a.chunk = (int32_t)(2 * share < kMaxChunk ? 2 * share : kMaxChunk);
+    int resident;
+    CHECK((dg4i_resident_blocks<norm_gate_kernel<BF16, RMS>>(256, &resident)));
+    const int64_t share = ((int64_t)a.n + 8 * (int64_t)resident - 1) / (8 * (int64_t)resident);        // rows of a warp
+    a.chunk = (int32_t)(share < kMaxChunk ? (share + kRows - 1) / kRows * kRows : kMaxChunk);
     const int64_t needed = ((int64_t)a.n + 8 * a.chunk - 1) / (8 * a.chunk);
     norm_gate_kernel<BF16, RMS><<<(unsigned)(needed < resident ? needed : resident), 256, 0, st>>>(a);
     dg4i_count_launch();

@@ -147,6 +147,16 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t smem_addr) {
     d |= (uint64_t)2 << 61;                          // layout: 128-byte swizzle
     return d;
 }
+// The same for rows of 64 bytes (32 bf16) with the 64-byte swizzle: groups of 8 rows are 512 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t smem_addr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)1 << 16;
+    d |= (uint64_t)(512u >> 4) << 32;                // stride byte offset: 8 rows x 64 bytes
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)4 << 61;                          // layout: 64-byte swizzle
+    return d;
+}
 __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
