@@ -42,16 +42,14 @@ constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kMaxStages = 2;
 constexpr int kSlots = 3;                         // accumulator slots of 128 columns
 constexpr int kRing = 4;                          // item descriptors in flight
-constexpr int kTmemCols = 512;
-constexpr int kColU = kSlots * 128;               // U in fp32: 64 columns
-constexpr int kColUb = kColU + 64;                // U in bf16: 32 columns
+// tensor memory: U in fp32 (64 columns), U in bf16 (32), then the accumulators from column 128 on
+constexpr int kColU = 0, kColUb = 64, kColAcc = 128;
 constexpr int kRankMax = 64;
 
-// The adapter's place in shared memory, for ranks up to 64 and up to 32: A_a is two halves of RANK rows x 128 bytes,
-// B_a per column block 128 rows of RANK columns (128-byte or 64-byte swizzle; the columns past the rank are zero).  The
+// The adapter's place in shared memory, for ranks up to 64 and up to 32: A_a is two halves of rank rows x 128 bytes, B_a
+// per column block 128 rows of RANK columns (128-byte or 64-byte swizzle; the columns past the rank are zero).  The
 // smaller place leaves room for a second X stage beside the whole of W_qkv.
 template <int RANK> struct Place {
-    static constexpr int kA = RANK * 256, kAHalf = kA / 2;
     static constexpr int kB = 128 * RANK * 2;
     __device__ static __forceinline__ uint64_t b_desc(uint32_t addr) { return RANK == 64 ? smem_desc_sw128(addr) : smem_desc_sw64(addr); }
 };
@@ -62,11 +60,14 @@ struct Item {
     int32_t last;             // the next item uses another adapter (or there is none)
 };
 
+// The walk over the items of a CTA, one request after the other (the producer's state).
+struct Walk { int32_t seg, lo, hi, adapter; };
+
 struct Bars {
     uint64_t w_full;
     uint64_t a_full[kMaxStages];
     uint64_t a_empty[kMaxStages];
-    uint64_t r_empty[kMaxStages];
+    uint64_t r_full[kMaxStages], r_empty[kMaxStages];
     uint64_t acc_full[kSlots];
     uint64_t acc_empty[kSlots];
     uint64_t ad_full, ad_empty;     // the adapter in shared memory
@@ -76,7 +77,7 @@ struct Bars {
     uint32_t tmem_base;
     uint32_t abort_flag;
     int32_t my_items;               // items of this CTA, and where they begin
-    int32_t first_seg, first_tile;
+    Walk first;
     int64_t warp_sum[kThreads / 32];
     Item ring[kRing];
 };
@@ -90,6 +91,7 @@ struct Params {
     int32_t n_out;                  // rows of W
     int32_t nb;                     // column blocks per CTA (blockIdx.y picks the first one)
     int32_t stages;                 // X (and residual) stages
+    int32_t slots;                  // accumulator slots: 3, or 1 (then 256 columns of tensor memory)
     int32_t off_a, off_b, off_x, off_r, off_stage, off_bar;
     int32_t has_res;
     int32_t* status;
@@ -129,38 +131,42 @@ __device__ __forceinline__ int seg_adapter(const Params& p, int s) {
     return (uint32_t)id < (uint32_t)p.n_adapters ? id : -1;
 }
 
-// The walk over the items of a CTA, one request after the other (the producer's state).
-struct Walk {
-    int seg, lo, hi, adapter;
-    __device__ void open(const Params& p, int s, int tile) {
-        seg = s;
-        seg_rows(p, s, lo, hi);
-        lo += tile * kTileM;
-        adapter = seg_adapter(p, s);
-    }
-    __device__ void next(const Params& p) {             // to the next item, which exists
-        lo += kTileM;
-        while (lo >= hi && seg + 1 < p.n_seg) {
-            ++seg;
-            seg_rows(p, seg, lo, hi);
-            adapter = seg_adapter(p, seg);
-        }
+// A place in a ring of n and the parity of its present round (counted on: a division by a runtime n costs the waiting
+// thread some 200 clocks, 2600 per QKV item when all roles had them).
+struct Turn {
+    int at = 0;
+    uint32_t odd = 0;
+    __device__ __forceinline__ void next(int n) {
+        if (++at == n) { at = 0; odd ^= 1u; }
     }
 };
 
+__device__ __forceinline__ void walk_on(const Params& p, Walk& w) {       // to the next item, which exists
+    w.lo += kTileM;
+    while (w.lo >= w.hi && w.seg + 1 < p.n_seg) {
+        ++w.seg;
+        seg_rows(p, w.seg, w.lo, w.hi);
+        w.adapter = seg_adapter(p, w.seg);
+    }
+}
+
 // Cuts all items into one contiguous run per CTA: every thread counts the tiles of its share of the requests, the
-// CTA adds the counts up, and the thread in whose share this CTA's first item falls finds its place.
+// CTA adds the counts up, and the thread in whose share this CTA's first item falls leaves it in shared memory.
 __device__ __forceinline__ void find_items(const Params& p, Bars* bars) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int share = (p.n_seg + kThreads - 1) / kThreads;
-    const int64_t s0 = (int64_t)threadIdx.x * share;
+    // warp 0, which sets up the barriers and starts W on its way, takes the last share
+    const int place = (warp == 0 ? kThreads : (int)threadIdx.x) - 32 + (warp == 0 ? lane : 0);
+    const int64_t s0 = (int64_t)place * share;
     const int64_t s1 = min(s0 + share, (int64_t)p.n_seg);
-    int64_t sum = 0;
-    for (int64_t s = s0; s < s1; ++s) {
-        int lo, hi;
+    auto tiles_of = [&](int64_t s, int& lo, int& hi) {
         seg_rows(p, (int)s, lo, hi);
-        sum += (hi - lo + kTileM - 1) / kTileM;
-    }
+        return (int64_t)((uint32_t)(hi - lo) + kTileM - 1) / kTileM;
+    };
+    int lo = 0, hi = 0, id = -1;
+    int64_t sum = 0;
+    for (int64_t s = s0; s < s1; ++s) sum += tiles_of(s, lo, hi);
+    if (share == 1 && s0 < s1) id = seg_adapter(p, (int)s0);   // on its way with the offsets
     int64_t incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -168,34 +174,38 @@ __device__ __forceinline__ void find_items(const Params& p, Bars* bars) {
         if (lane >= o) incl += below;
     }
     if (lane == 31) bars->warp_sum[warp] = incl;
-    if (threadIdx.x == 0) { bars->my_items = 0; bars->first_seg = 0; bars->first_tile = 0; }
+    if (threadIdx.x == 0) bars->my_items = 0;
     __syncthreads();
     int64_t total = 0, before = incl - sum;
     for (int w = 0; w < kThreads / 32; ++w) {
         const int64_t x = bars->warp_sum[w];
-        if (w < warp) before += x;
+        if (warp == 0 ? w > 0 : (w > 0 && w < warp)) before += x;
         total += x;
     }
-    const int64_t begin = total * blockIdx.x / gridDim.x, end = total * (blockIdx.x + 1) / gridDim.x;
-    if (end > begin && begin >= before && begin < before + sum) {
-        bars->my_items = (int32_t)(end - begin);
-        int64_t at = before;
-        for (int64_t s = s0; s < s1; ++s) {
-            int lo, hi;
-            seg_rows(p, (int)s, lo, hi);
-            const int64_t tiles = (hi - lo + kTileM - 1) / kTileM;
-            if (begin < at + tiles) {
-                bars->first_seg = (int32_t)s;
-                bars->first_tile = (int32_t)(begin - at);
-                break;
+    // the first total % gridDim.x CTAs take one item more (32-bit division where it suffices: 64 bits take 300 clocks)
+    const int64_t each = total <= 0xffffffffll ? (int64_t)((uint32_t)total / gridDim.x) : total / gridDim.x;
+    const int64_t rest = total - each * gridDim.x, b = blockIdx.x;
+    const int64_t begin = b * each + min(b, rest), mine = each + (b < rest ? 1 : 0);
+    if (mine > 0 && begin >= before && begin < before + sum) {
+        int64_t s = s0, at = before;
+        if (share > 1) {
+            for (;; ++s) {
+                const int64_t tiles = tiles_of(s, lo, hi);
+                if (begin < at + tiles || s + 1 >= s1) break;
+                at += tiles;
             }
-            at += tiles;
+            id = seg_adapter(p, (int)s);
         }
+        bars->my_items = (int32_t)mine;
+        bars->first.seg = (int32_t)s;
+        bars->first.lo = lo + (int32_t)(begin - at) * kTileM;
+        bars->first.hi = hi;
+        bars->first.adapter = id;
     }
 }
 
 template <int RANK>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 2)
 adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                     const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_a,
                     const __grid_constant__ CUtensorMap map_b, const __grid_constant__ OutMaps map_o, Params p) {
@@ -207,25 +217,33 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int nb = p.nb, block0 = blockIdx.y * p.nb, stages = p.stages;
     const int rank16 = (p.rank + 15) & ~15;
+    const int a_half = rank16 * 128;                       // bytes of one half of A_a (a multiple of 1024)
     volatile uint32_t* abort_flag = &bars->abort_flag;
 
-    if (threadIdx.x == 0) {
-        mbar_init(smem_u32(&bars->w_full), 1);
-        for (int s = 0; s < kMaxStages; ++s) {
-            mbar_init(smem_u32(&bars->a_full[s]), 1);
-            mbar_init(smem_u32(&bars->a_empty[s]), 1);
-            mbar_init(smem_u32(&bars->r_empty[s]), kEpiWarps);
-        }
-        for (int s = 0; s < kSlots; ++s) { mbar_init(smem_u32(&bars->acc_full[s]), 1); mbar_init(smem_u32(&bars->acc_empty[s]), kEpiWarps); }
-        mbar_init(smem_u32(&bars->ad_full), 1);
-        mbar_init(smem_u32(&bars->ad_empty), 1);
-        mbar_init(smem_u32(&bars->u_full), 1);
-        mbar_init(smem_u32(&bars->u_ready), kUWarps);
-        mbar_init(smem_u32(&bars->ub_empty), 1);
-        for (int s = 0; s < kRing; ++s) { mbar_init(smem_u32(&bars->item_full[s]), 1); mbar_init(smem_u32(&bars->item_empty[s]), 1 + kEpiWarps + kUWarps); }
-        mbar_init(smem_u32(&bars->drain), 1);
-        bars->abort_flag = 0;
+    if (warp == 0) {
+        auto init = [&](uint64_t* first, int n, int arrivals) {
+            if (lane < n) mbar_init(smem_u32(first + lane), arrivals);
+        };
+        init(&bars->w_full, 1, 1);
+        init(bars->a_full, kMaxStages, 1);
+        init(bars->a_empty, kMaxStages, 1);
+        init(bars->r_full, kMaxStages, 1);
+        init(bars->r_empty, kMaxStages, kEpiWarps);
+        init(bars->acc_full, kSlots, 1);
+        init(bars->acc_empty, kSlots, kEpiWarps);
+        init(&bars->ad_full, 1, 1);
+        init(&bars->ad_empty, 1, 1);
+        init(&bars->u_full, 1, 1);
+        init(&bars->u_ready, 1, kUWarps);
+        init(&bars->ub_empty, 1, 1);
+        init(bars->item_full, kRing, 1);
+        init(bars->item_empty, kRing, 1 + kEpiWarps + kUWarps);
+        init(&bars->drain, 1, 1);
         mbar_fence_init();
+        __syncwarp();
+    }
+    if (threadIdx.x == 0) {
+        bars->abort_flag = 0;
         // W travels while the items are counted
         mbar_expect_tx(smem_u32(&bars->w_full), (uint32_t)(nb * kTileBytes));
         for (int j = 0; j < nb; ++j)
@@ -236,7 +254,8 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         tma_prefetch_desc(&map_b);
         for (int j = 0; j < nb; ++j) tma_prefetch_desc(&map_o.m[block0 + j]);
     }
-    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), kTmemCols);
+    const uint32_t tmem_cols = p.slots == 1 ? 256u : 512u;
+    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), tmem_cols);
     __syncwarp();
     find_items(p, bars);
     tc_fence_before();
@@ -248,48 +267,51 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     if (warp == 0) {
         // ------------------------------------------------------------------ producer
         if (lane == 0) {
-            int armed = 0, loads = 0;
-            Walk w;
-            if (items > 0) w.open(p, bars->first_seg, bars->first_tile);
+            int armed = 0, armed_r = 0, loads = 0;
+            Turn q, s;                                         // of the descriptors, of the stages
+            Walk w = bars->first;
             int held = -1;                                     // the adapter in shared memory, -1 = released
-            for (int i = 0; i < items && !*abort_flag; ++i) {
+            for (int i = 0; i < items && !*abort_flag; ++i, q.next(kRing), s.next(stages)) {
                 Item it;
                 it.row0 = w.lo;
                 it.rows = min(w.hi - w.lo, kTileM);
                 it.adapter = w.adapter;
-                if (i + 1 < items) w.next(p);
+                if (i + 1 < items) walk_on(p, w);
                 it.last = i + 1 == items || w.adapter != it.adapter;
-                const int q = i % kRing, s = i % stages;
-                const uint32_t ph = (uint32_t)(i / stages) & 1u;
-                if (!mbar_wait(smem_u32(&bars->item_empty[q]), ((uint32_t)(i / kRing) & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
-                bars->ring[q] = it;
-                mbar_arrive(smem_u32(&bars->item_full[q]));
-                if (!mbar_wait(smem_u32(&bars->a_empty[s]), ph ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
-                if (p.has_res && !mbar_wait(smem_u32(&bars->r_empty[s]), ph ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
-                const uint32_t bar = smem_u32(&bars->a_full[s]);
-                mbar_expect_tx(bar, (uint32_t)(p.has_res ? 2 * kTileBytes : kTileBytes));
-                for (int h = 0; h < 2; ++h) {
-                    tma_load_2d(sX + s * kTileBytes + h * kHalfBytes, &map_x, h * 64, it.row0, bar);
-                    if (p.has_res) tma_load_2d(sR + s * kTileBytes + h * kHalfBytes, &map_r, h * 64, it.row0, bar);
-                }
+                if (i >= kRing && !mbar_wait(smem_u32(&bars->item_empty[q.at]), q.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                bars->ring[q.at] = it;
+                mbar_arrive(smem_u32(&bars->item_full[q.at]));
+                if (i >= stages && !mbar_wait(smem_u32(&bars->a_empty[s.at]), s.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                mbar_expect_tx(smem_u32(&bars->a_full[s.at]), (uint32_t)kTileBytes);
+                for (int h = 0; h < 2; ++h)
+                    tma_load_2d(sX + s.at * kTileBytes + h * kHalfBytes, &map_x, h * 64, it.row0, smem_u32(&bars->a_full[s.at]));
                 armed = i + 1;
                 if (it.adapter >= 0 && it.adapter != held) {
                     // the previous adapter's last products (load index `loads` - 1) must have read it
-                    if (!mbar_wait(smem_u32(&bars->ad_empty), ((uint32_t)loads & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                    if (loads > 0 && !mbar_wait(smem_u32(&bars->ad_empty), ((uint32_t)loads & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
                     const uint32_t ad = smem_u32(&bars->ad_full);
                     mbar_expect_tx(ad, (uint32_t)(p.rank * 256 + nb * P::kB));
-                    for (int h = 0; h < 2; ++h) tma_load_2d(sA + h * P::kAHalf, &map_a, h * 64, it.adapter * p.rank, ad);
+                    for (int h = 0; h < 2; ++h) tma_load_2d(sA + h * a_half, &map_a, h * 64, it.adapter * p.rank, ad);
                     for (int j = 0; j < nb; ++j)
                         tma_load_2d(sB + j * P::kB, &map_b, 0, it.adapter * p.n_out + (block0 + j) * 128, ad);
                     ++loads;
                     held = it.adapter;
                 }
                 if (it.last) held = -1;
+                if (p.has_res) {                               // last: its buffer is given back by the epilogue, later than X's
+                    if (i >= stages && !mbar_wait(smem_u32(&bars->r_empty[s.at]), s.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                    mbar_expect_tx(smem_u32(&bars->r_full[s.at]), (uint32_t)kTileBytes);
+                    for (int h = 0; h < 2; ++h)
+                        tma_load_2d(sR + s.at * kTileBytes + h * kHalfBytes, &map_r, h * 64, it.row0, smem_u32(&bars->r_full[s.at]));
+                    armed_r = i + 1;
+                }
             }
             // leave with no copy still landing in shared memory (these waits keep the default limit)
             mbar_wait(smem_u32(&bars->w_full), 0);
             for (int i = (armed > stages ? armed - stages : 0); i < armed; ++i)
                 mbar_wait(smem_u32(&bars->a_full[i % stages]), (uint32_t)(i / stages) & 1u);
+            for (int i = (armed_r > stages ? armed_r - stages : 0); i < armed_r; ++i)
+                mbar_wait(smem_u32(&bars->r_full[i % stages]), (uint32_t)(i / stages) & 1u);
             if (loads > 0) mbar_wait(smem_u32(&bars->ad_full), (uint32_t)(loads - 1) & 1u);
         }
     } else if (warp == 1) {
@@ -298,58 +320,70 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             const uint32_t idesc = idesc_bf16_f32(128, 128), idesc_u = idesc_bf16_f32(128, rank16);
             bool ok = mbar_wait(smem_u32(&bars->w_full), 0, p.poll_limit);
             if (!ok) raise_timeout(bars, p.status);
-            int block = 0, loads = 0, u_items = 0;
+            int loads = 0, u_items = 0;
+            Turn q, s, acc;                                    // of the descriptors and stages (of the item begun last), of the slots
             bool fresh = true;                                 // the next adapter item brings a new adapter
-            for (int i = 0; i < items && ok && !*abort_flag; ++i) {
-                const int q = i % kRing, s = i % stages;
-                ok = mbar_wait(smem_u32(&bars->item_full[q]), (uint32_t)(i / kRing) & 1u, p.poll_limit);
-                if (!ok) { raise_timeout(bars, p.status); break; }
-                const Item it = bars->ring[q];
-                mbar_arrive(smem_u32(&bars->item_empty[q]));
-                const bool ad = it.adapter >= 0;
-                ok = mbar_wait(smem_u32(&bars->a_full[s]), (uint32_t)(i / stages) & 1u, p.poll_limit);
-                if (ok && ad && fresh) ok = mbar_wait(smem_u32(&bars->ad_full), (uint32_t)(loads++) & 1u, p.poll_limit);
-                if (!ok) { raise_timeout(bars, p.status); break; }
+            Item it, next;
+            // takes the item q and s point at, waits for its rows, and issues U = X A^T
+            auto begin = [&](Item& item) -> bool {
+                if (!mbar_wait(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) return false;
+                item = bars->ring[q.at];
+                mbar_arrive(smem_u32(&bars->item_empty[q.at]));
+                if (!mbar_wait(smem_u32(&bars->a_full[s.at]), s.odd, p.poll_limit)) return false;
+                if (item.adapter < 0) return true;
+                if (fresh && !mbar_wait(smem_u32(&bars->ad_full), (uint32_t)(loads++) & 1u, p.poll_limit)) return false;
+                fresh = item.last != 0;
                 tc_fence_after();
-                const uint32_t x_base = sX + s * kTileBytes;
-                if (ad) {
+                const uint32_t x_base = sX + s.at * kTileBytes;
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        mma_bf16(tmem + kColU, smem_desc_sw128(x_base + (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32)),
-                                 smem_desc_sw128(sA + (uint32_t)((ks >> 2) * P::kAHalf + (ks & 3) * 32)), idesc_u, ks > 0 ? 1u : 0u);
-                    mma_commit(smem_u32(&bars->u_full));
-                }
-                for (int j = 0; j < nb; ++j) {
-                    const int slot = (block + j) % kSlots;
-                    ok = mbar_wait(smem_u32(&bars->acc_empty[slot]), ((uint32_t)((block + j) / kSlots) & 1u) ^ 1u, p.poll_limit);
+                for (int ks = 0; ks < 8; ++ks)
+                    mma_bf16(tmem + kColU, smem_desc_sw128(x_base + (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32)),
+                             smem_desc_sw128(sA + (uint32_t)((ks >> 2) * a_half + (ks & 3) * 32)), idesc_u, ks > 0 ? 1u : 0u);
+                mma_commit(smem_u32(&bars->u_full));
+                return true;
+            };
+            if (ok && items > 0 && !(ok = begin(it))) raise_timeout(bars, p.status);
+            for (int i = 0; i < items && ok && !*abort_flag; ++i) {
+                const bool ad = it.adapter >= 0;
+                const uint32_t x_base = sX + s.at * kTileBytes;
+                tc_fence_after();
+                for (int j = 0; j < nb && ok; ++j, acc.next(p.slots)) {
+                    const int slot = acc.at;
+                    const uint32_t d = tmem + (uint32_t)(kColAcc + slot * 128), b_base = sW + j * kTileBytes;
+                    ok = mbar_wait(smem_u32(&bars->acc_empty[slot]), acc.odd ^ 1u, p.poll_limit);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t b_base = sW + j * kTileBytes;
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks) {
                         const uint32_t off = (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32);
-                        mma_bf16(tmem + (uint32_t)(slot * 128), smem_desc_sw128(x_base + off), smem_desc_sw128(b_base + off), idesc, ks > 0 ? 1u : 0u);
+                        mma_bf16(d, smem_desc_sw128(x_base + off), smem_desc_sw128(b_base + off), idesc, ks > 0 ? 1u : 0u);
                     }
-                    if (!ad) mma_commit(smem_u32(&bars->acc_full[slot]));
+                    if (ad) {
+                        if (j == 0) {
+                            ok = mbar_wait(smem_u32(&bars->u_ready), (uint32_t)(u_items++) & 1u, p.poll_limit);
+                            if (!ok) break;
+                            tc_fence_after();
+                        }
+                        for (int ks = 0; ks < rank16 / 16; ++ks)
+                            mma_bf16_ta(d, tmem + (uint32_t)(kColUb + ks * 8), P::b_desc(sB + (uint32_t)(j * P::kB + ks * 32)), idesc, 1u);
+                    }
+                    mma_commit(smem_u32(&bars->acc_full[slot]));
                 }
                 if (!ok) { raise_timeout(bars, p.status); break; }
-                mma_commit(smem_u32(&bars->a_empty[s]));
+                mma_commit(smem_u32(&bars->a_empty[s.at]));
                 if (ad) {
-                    ok = mbar_wait(smem_u32(&bars->u_ready), (uint32_t)(u_items++) & 1u, p.poll_limit);
-                    if (!ok) { raise_timeout(bars, p.status); break; }
-                    tc_fence_after();
-                    for (int j = 0; j < nb; ++j) {
-                        const int slot = (block + j) % kSlots;
-                        for (int ks = 0; ks < rank16 / 16; ++ks)
-                            mma_bf16_ta(tmem + (uint32_t)(slot * 128), tmem + (uint32_t)(kColUb + ks * 8),
-                                        P::b_desc(sB + (uint32_t)(j * P::kB + ks * 32)), idesc, 1u);
-                        mma_commit(smem_u32(&bars->acc_full[slot]));
-                    }
                     mma_commit(smem_u32(&bars->ub_empty));
-                    fresh = it.last != 0;
-                    if (fresh) mma_commit(smem_u32(&bars->ad_empty));
+                    if (it.last) mma_commit(smem_u32(&bars->ad_empty));
                 }
-                block += nb;
+                // the next item's U at once: it turns into the second product's operand while the epilogue is still
+                // emptying the accumulators of this item
+                if (i + 1 < items) {
+                    q.next(kRing);
+                    s.next(stages);
+                    ok = begin(next);
+                    if (!ok) { raise_timeout(bars, p.status); break; }
+                    it = next;
+                }
             }
             mma_commit(smem_u32(&bars->drain));                // tensor memory is freed below: every MMA must be done
             mbar_wait(smem_u32(&bars->drain), 0);
@@ -358,32 +392,32 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         // ------------------------------------------------------------------ epilogue (warps 2..9)
         const int ew = warp - 2, quad = warp & 3, half = ew >> 2;
         const uint32_t stage = base + p.off_stage + (uint32_t)(ew * 4096);
-        int block = 0;
+        Turn q, s, acc_turn;
         bool ok = true;
-        for (int i = 0; i < items && ok; ++i) {
+        for (int i = 0; i < items && ok; ++i, q.next(kRing), s.next(stages)) {
             if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
-            const int q = i % kRing, s = i % stages;
-            if (!mbar_wait_warp(smem_u32(&bars->item_full[q]), (uint32_t)(i / kRing) & 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
-            const Item it = bars->ring[q];
+            if (!mbar_wait_warp(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+            const Item it = bars->ring[q.at];
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q]));
+            if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q.at]));
             const int valid = it.rows - quad * 32;             // rows of the item among this warp's 32
-            for (int j = 0; j < nb; ++j, ++block) {
-                const int slot = block % kSlots;
-                ok = mbar_wait_warp(smem_u32(&bars->acc_full[slot]), (uint32_t)(block / kSlots) & 1u, p.poll_limit);
+            for (int j = 0; j < nb; ++j, acc_turn.next(p.slots)) {
+                const int slot = acc_turn.at;
+                ok = mbar_wait_warp(smem_u32(&bars->acc_full[slot]), acc_turn.odd, p.poll_limit);
+                if (ok && p.has_res) ok = mbar_wait_warp(smem_u32(&bars->r_full[s.at]), s.odd, p.poll_limit);
                 if (!ok) { raise_timeout(bars, p.status); break; }
                 tc_fence_after();
-                const uint32_t t_addr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(slot * 128 + half * 64);
+                const uint32_t t_addr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(kColAcc + slot * 128 + half * 64);
                 if (lane == 0) bulk_wait_read0();              // the previous store has read the staging rows
                 __syncwarp();
 #pragma unroll 1
-                for (int c2 = 0; c2 < 2; ++c2) {
+                for (int c2 = 0; c2 < (valid > 0 ? 2 : 0); ++c2) {
                     uint32_t acc[32], res[16];
                     tmem_ld_32x32(t_addr + (uint32_t)(c2 * 32), acc);
                     if (p.has_res) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            ld_shared_v4(sR + (uint32_t)(s * kTileBytes + half * kHalfBytes) + sw128_offset(quad * 32 + lane, c2 * 4 + c), res + 4 * c);
+                            ld_shared_v4(sR + (uint32_t)(s.at * kTileBytes + half * kHalfBytes) + sw128_offset(quad * 32 + lane, c2 * 4 + c), res + 4 * c);
                     }
                     tmem_ld_wait();
 #pragma unroll
@@ -405,7 +439,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(smem_u32(&bars->acc_empty[slot]));
-                    if (p.has_res) mbar_arrive(smem_u32(&bars->r_empty[s]));
+                    if (p.has_res) mbar_arrive(smem_u32(&bars->r_empty[s.at]));
                 }
                 const int row0 = it.row0 + quad * 32;
                 if (valid >= 32) {
@@ -434,13 +468,13 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         const int quad = warp & 3;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         int u_items = 0;
-        for (int i = 0; i < items; ++i) {
+        Turn q;
+        for (int i = 0; i < items; ++i, q.next(kRing)) {
             if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
-            const int q = i % kRing;
-            if (!mbar_wait_warp(smem_u32(&bars->item_full[q]), (uint32_t)(i / kRing) & 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
-            const Item it = bars->ring[q];
+            if (!mbar_wait_warp(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+            const Item it = bars->ring[q.at];
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q]));
+            if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q.at]));
             if (it.adapter < 0) continue;
             const float scale = __ldg(p.scale + it.adapter);
             if (!mbar_wait_warp(smem_u32(&bars->u_full), (uint32_t)u_items & 1u, p.poll_limit) ||
@@ -475,7 +509,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, kTmemCols);
+        tmem_dealloc(tmem, tmem_cols);
     }
 }
 
@@ -523,14 +557,19 @@ dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
     const int blocks = c.n_out / 128, sms = sm_count[dev];
     // items: at most one per full tile and one ragged one per request
     const int64_t most = (int64_t)g->n / kTileM + p.n_seg;
-    const bool split = most * blocks <= sms;
+    // Column blocks to different CTAs where the device holds all of them at once: two to an SM if two fit.  64 requests
+    // of one row: 11.7 us with a CTA per request, see the figure beside it for this form.
+    const int per_stage = kTileBytes * (c.R ? 2 : 1), tail = (int)sizeof(Bars) + 1024;
+    const int a_bytes = ((c.ad->rank + 15) & ~15) * 256;
+    const int one = kTileBytes + a_bytes + P::kB + kEpiWarps * 4096 + per_stage + tail;       // shared memory of such a CTA
+    const bool split = blocks > 1 && most * blocks <= sms * (2 * (one + 1024) <= 233472 ? 2 : 1);
     p.nb = split ? 1 : blocks;
+    p.slots = split ? 1 : kSlots;
     int off = p.nb * kTileBytes;
-    p.off_a = off; off += P::kA;
+    p.off_a = off; off += a_bytes;
     p.off_b = off; off += p.nb * P::kB;
     p.off_stage = off; off += kEpiWarps * 4096;
-    const int per_stage = kTileBytes * (p.has_res ? 2 : 1), tail = (int)sizeof(Bars) + 1024;
-    p.stages = off + kMaxStages * per_stage + tail <= kSmemLimit ? kMaxStages : 1;
+    p.stages = !split && off + kMaxStages * per_stage + tail <= kSmemLimit ? kMaxStages : 1;
     p.off_x = off; off += p.stages * kTileBytes;
     p.off_r = off; off += p.has_res ? p.stages * kTileBytes : 0;
     p.off_bar = off; off += tail;                 // 1024 of it: the base is aligned by hand
