@@ -28,7 +28,7 @@
 #include "dg4_internal.h"
 #include "dg4_sm100.cuh"
 
-#include <mutex>
+#include <atomic>
 
 namespace {
 
@@ -40,17 +40,24 @@ constexpr int kTileM = 128;
 constexpr int kHalfBytes = 128 * 128;             // a 128-row x 64-column bf16 box
 constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kMaxStages = 2;
-constexpr int kSlots = 3;                         // accumulator slots of 128 columns
+constexpr int kSlots = 3;                         // accumulators of 128 columns, at most
 constexpr int kRing = 4;                          // item descriptors in flight
-// tensor memory: U in fp32 (64 columns), U in bf16 (32), then the accumulators from column 128 on
-constexpr int kColU = 0, kColUb = 64, kColAcc = 128;
 constexpr int kRankMax = 64;
 
-// The adapter's place in shared memory, for ranks up to 64 and up to 32: A_a is two halves of rank rows x 128 bytes, B_a
-// per column block 128 rows of RANK columns (128-byte or 64-byte swizzle; the columns past the rank are zero).  The
-// smaller place leaves room for a second X stage beside the whole of W_qkv.
-template <int RANK> struct Place {
+// Where things lie, for ranks up to RANK = 32 or 64 and NB = 3 or 1 column blocks per CTA.
+// Shared memory: the rows of A_a stand directly in front of those of W in each half of K (128-byte rows, 128-byte
+// swizzle), so ONE product makes U and the first column block: X is read once for both, and its N (128 + the rank) costs
+// little more than 128.  B_a per column block 128 rows of RANK columns (128-byte or 64-byte swizzle; the columns past
+// the rank are zero).
+// Tensor memory: U (fp32) directly in front of the first block's accumulator, accordingly.  With NB = 1 that pair stands
+// there two or three times, so that the next item's product need not wait for this one's second product.
+template <int RANK, int NB> struct Place {
     static constexpr int kB = 128 * RANK * 2;
+    static constexpr int kSets = NB == 3 ? 1 : RANK == 64 ? 2 : 3;      // at most (few requests: one)
+    static constexpr int kSetCols = RANK + 128;
+    static constexpr int kColUb = NB == 3 ? 448 : kSets * kSetCols;     // U in bf16: RANK / 2 columns
+    static_assert(RANK + NB * 128 <= 448 && kColUb + RANK / 2 <= 512, "tensor memory columns");
+    static_assert(kSetCols + RANK / 2 <= 256, "tensor memory columns of a CTA with one set");
     __device__ static __forceinline__ uint64_t b_desc(uint32_t addr) { return RANK == 64 ? smem_desc_sw128(addr) : smem_desc_sw64(addr); }
 };
 
@@ -89,10 +96,10 @@ struct Params {
     __nv_bfloat16* out[3]; int64_t ldo[3];
     int32_t n, n_seg, n_adapters, rank;
     int32_t n_out;                  // rows of W
-    int32_t nb;                     // column blocks per CTA (blockIdx.y picks the first one)
     int32_t stages;                 // X (and residual) stages
-    int32_t slots;                  // accumulator slots: 3, or 1 (then 256 columns of tensor memory)
-    int32_t off_a, off_b, off_x, off_r, off_stage, off_bar;
+    int32_t slots;                  // accumulators: 3 (NB = 3), or the number of sets (one: 256 columns of tensor memory)
+    int32_t col_ub;
+    int32_t off_b, off_x, off_r, off_stage, off_bar;
     int32_t has_res;
     int32_t* status;
     uint32_t poll_limit;
@@ -204,20 +211,21 @@ __device__ __forceinline__ void find_items(const Params& p, Bars* bars) {
     }
 }
 
-template <int RANK>
+template <int RANK, int NB>
 __global__ void __launch_bounds__(kThreads, 2)
 adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                     const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_a,
                     const __grid_constant__ CUtensorMap map_b, const __grid_constant__ OutMaps map_o, Params p) {
-    using P = Place<RANK>;
+    using P = Place<RANK, NB>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + p.off_bar);
-    const uint32_t sW = base, sA = base + p.off_a, sB = base + p.off_b, sX = base + p.off_x, sR = base + p.off_r;
+    const uint32_t sW = base, sB = base + p.off_b, sX = base + p.off_x, sR = base + p.off_r;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int nb = p.nb, block0 = blockIdx.y * p.nb, stages = p.stages;
+    const int block0 = blockIdx.y * NB, stages = p.stages;
     const int rank16 = (p.rank + 15) & ~15;
     const int a_half = rank16 * 128;                       // bytes of one half of A_a (a multiple of 1024)
+    const int w_half = a_half + NB * kHalfBytes;           // and of A_a and W together
     volatile uint32_t* abort_flag = &bars->abort_flag;
 
     if (warp == 0) {
@@ -245,14 +253,14 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     if (threadIdx.x == 0) {
         bars->abort_flag = 0;
         // W travels while the items are counted
-        mbar_expect_tx(smem_u32(&bars->w_full), (uint32_t)(nb * kTileBytes));
-        for (int j = 0; j < nb; ++j)
+        mbar_expect_tx(smem_u32(&bars->w_full), (uint32_t)(NB * kTileBytes));
+        for (int j = 0; j < NB; ++j)
             for (int h = 0; h < 2; ++h)
-                tma_load_2d(sW + (j * 2 + h) * kHalfBytes, &map_w, h * 64, (block0 + j) * 128, smem_u32(&bars->w_full));
+                tma_load_2d(sW + h * w_half + a_half + j * kHalfBytes, &map_w, h * 64, (block0 + j) * 128, smem_u32(&bars->w_full));
         tma_prefetch_desc(&map_x);
         tma_prefetch_desc(&map_a);
         tma_prefetch_desc(&map_b);
-        for (int j = 0; j < nb; ++j) tma_prefetch_desc(&map_o.m[block0 + j]);
+        for (int j = 0; j < NB; ++j) tma_prefetch_desc(&map_o.m[block0 + j]);
     }
     const uint32_t tmem_cols = p.slots == 1 ? 256u : 512u;
     if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), tmem_cols);
@@ -278,28 +286,28 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 it.adapter = w.adapter;
                 if (i + 1 < items) walk_on(p, w);
                 it.last = i + 1 == items || w.adapter != it.adapter;
-                if (i >= kRing && !mbar_wait(smem_u32(&bars->item_empty[q.at]), q.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                if (i >= kRing && !mbar_wait_relaxed(smem_u32(&bars->item_empty[q.at]), q.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
                 bars->ring[q.at] = it;
                 mbar_arrive(smem_u32(&bars->item_full[q.at]));
-                if (i >= stages && !mbar_wait(smem_u32(&bars->a_empty[s.at]), s.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                if (i >= stages && !mbar_wait_relaxed(smem_u32(&bars->a_empty[s.at]), s.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
                 mbar_expect_tx(smem_u32(&bars->a_full[s.at]), (uint32_t)kTileBytes);
                 for (int h = 0; h < 2; ++h)
                     tma_load_2d(sX + s.at * kTileBytes + h * kHalfBytes, &map_x, h * 64, it.row0, smem_u32(&bars->a_full[s.at]));
                 armed = i + 1;
                 if (it.adapter >= 0 && it.adapter != held) {
                     // the previous adapter's last products (load index `loads` - 1) must have read it
-                    if (loads > 0 && !mbar_wait(smem_u32(&bars->ad_empty), ((uint32_t)loads & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                    if (loads > 0 && !mbar_wait_relaxed(smem_u32(&bars->ad_empty), ((uint32_t)loads & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
                     const uint32_t ad = smem_u32(&bars->ad_full);
-                    mbar_expect_tx(ad, (uint32_t)(p.rank * 256 + nb * P::kB));
-                    for (int h = 0; h < 2; ++h) tma_load_2d(sA + h * a_half, &map_a, h * 64, it.adapter * p.rank, ad);
-                    for (int j = 0; j < nb; ++j)
+                    mbar_expect_tx(ad, (uint32_t)(p.rank * 256 + NB * P::kB));
+                    for (int h = 0; h < 2; ++h) tma_load_2d(sW + h * w_half, &map_a, h * 64, it.adapter * p.rank, ad);
+                    for (int j = 0; j < NB; ++j)
                         tma_load_2d(sB + j * P::kB, &map_b, 0, it.adapter * p.n_out + (block0 + j) * 128, ad);
                     ++loads;
                     held = it.adapter;
                 }
                 if (it.last) held = -1;
                 if (p.has_res) {                               // last: its buffer is given back by the epilogue, later than X's
-                    if (i >= stages && !mbar_wait(smem_u32(&bars->r_empty[s.at]), s.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                    if (i >= stages && !mbar_wait_relaxed(smem_u32(&bars->r_empty[s.at]), s.odd ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
                     mbar_expect_tx(smem_u32(&bars->r_full[s.at]), (uint32_t)kTileBytes);
                     for (int h = 0; h < 2; ++h)
                         tma_load_2d(sR + s.at * kTileBytes + h * kHalfBytes, &map_r, h * 64, it.row0, smem_u32(&bars->r_full[s.at]));
@@ -317,74 +325,99 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         if (lane == 0) {
-            const uint32_t idesc = idesc_bf16_f32(128, 128), idesc_u = idesc_bf16_f32(128, rank16);
-            bool ok = mbar_wait(smem_u32(&bars->w_full), 0, p.poll_limit);
-            if (!ok) raise_timeout(bars, p.status);
+            const uint32_t idesc = idesc_bf16_f32(128, 128), idesc_first = idesc_bf16_f32(128, rank16 + 128),
+                           idesc_two = idesc_bf16_f32(128, 256);
+            bool ok = mbar_wait_relaxed(smem_u32(&bars->w_full), 0, p.poll_limit);
             int loads = 0, u_items = 0;
-            Turn q, s, acc;                                    // of the descriptors and stages (of the item begun last), of the slots
+            Turn q, s, acc;                                    // of the descriptors, the stages, the accumulators
             bool fresh = true;                                 // the next adapter item brings a new adapter
-            Item it, next;
-            // takes the item q and s point at, waits for its rows, and issues U = X A^T
-            auto begin = [&](Item& item) -> bool {
-                if (!mbar_wait(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) return false;
-                item = bars->ring[q.at];
-                mbar_arrive(smem_u32(&bars->item_empty[q.at]));
-                if (!mbar_wait(smem_u32(&bars->a_full[s.at]), s.odd, p.poll_limit)) return false;
-                if (item.adapter < 0) return true;
-                if (fresh && !mbar_wait(smem_u32(&bars->ad_full), (uint32_t)(loads++) & 1u, p.poll_limit)) return false;
-                fresh = item.last != 0;
-                tc_fence_after();
-                const uint32_t x_base = sX + s.at * kTileBytes;
+            bool owed = false, owed_last = false;              // NB = 1: the second product of the item before
+            int owed_slot = 0;
+            // d = X * (rows of A_a and W from row0 on)^T over K = 128, as many as `id` says
+            auto product = [&](uint32_t d, uint32_t x_base, int row0, uint32_t id) {
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
-                    mma_bf16(tmem + kColU, smem_desc_sw128(x_base + (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32)),
-                             smem_desc_sw128(sA + (uint32_t)((ks >> 2) * a_half + (ks & 3) * 32)), idesc_u, ks > 0 ? 1u : 0u);
-                mma_commit(smem_u32(&bars->u_full));
+                    mma_bf16(d, smem_desc_sw128(x_base + (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32)),
+                             smem_desc_sw128(sW + (uint32_t)((ks >> 2) * w_half + row0 * 128 + (ks & 3) * 32)), id, ks > 0 ? 1u : 0u);
+            };
+            // d += U * B_a^T for the column blocks from j on
+            auto second = [&](uint32_t d, int j, uint32_t id) {
+                for (int ks = 0; ks < rank16 / 16; ++ks)
+                    mma_bf16_ta(d, tmem + (uint32_t)(p.col_ub + ks * 8), P::b_desc(sB + (uint32_t)(j * P::kB + ks * 32)), id, 1u);
+            };
+            auto u_wait = [&]() {
+                const bool r = mbar_wait_relaxed(smem_u32(&bars->u_ready), (uint32_t)(u_items++) & 1u, p.poll_limit);
+                tc_fence_after();
+                return r;
+            };
+            auto u_done = [&](bool last) {
+                mma_commit(smem_u32(&bars->ub_empty));
+                if (last) mma_commit(smem_u32(&bars->ad_empty));
+            };
+            auto settle = [&]() {                              // NB = 1: what is owed
+                if (!owed) return true;
+                owed = false;
+                if (!u_wait()) return false;
+                second(tmem + (uint32_t)(owed_slot * P::kSetCols + rank16), 0, idesc);
+                mma_commit(smem_u32(&bars->acc_full[owed_slot]));
+                u_done(owed_last);
                 return true;
             };
-            if (ok && items > 0 && !(ok = begin(it))) raise_timeout(bars, p.status);
-            for (int i = 0; i < items && ok && !*abort_flag; ++i) {
+            for (int i = 0; i < items && ok && !*abort_flag; ++i, q.next(kRing), s.next(stages)) {
+                ok = mbar_wait_relaxed(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit);
+                if (!ok) break;
+                const Item it = bars->ring[q.at];
+                mbar_arrive(smem_u32(&bars->item_empty[q.at]));
                 const bool ad = it.adapter >= 0;
-                const uint32_t x_base = sX + s.at * kTileBytes;
+                // what is owed comes first if this item cannot begin yet, or if its adapter takes the owed one's place
+                if (owed && ((ad && fresh) || !mbar_test(smem_u32(&bars->a_full[s.at]), s.odd) ||
+                             !mbar_test(smem_u32(&bars->acc_empty[acc.at]), acc.odd ^ 1u))) ok = settle();
+                ok = ok && mbar_wait_relaxed(smem_u32(&bars->a_full[s.at]), s.odd, p.poll_limit);
+                if (ok && ad && fresh) {
+                    ok = mbar_wait_relaxed(smem_u32(&bars->ad_full), (uint32_t)(loads++) & 1u, p.poll_limit);
+                }
+                if (ad) fresh = it.last != 0;
+                ok = ok && mbar_wait_relaxed(smem_u32(&bars->acc_empty[acc.at]), acc.odd ^ 1u, p.poll_limit);
+                if (!ok) break;
                 tc_fence_after();
-                for (int j = 0; j < nb && ok; ++j, acc.next(p.slots)) {
-                    const int slot = acc.at;
-                    const uint32_t d = tmem + (uint32_t)(kColAcc + slot * 128), b_base = sW + j * kTileBytes;
-                    ok = mbar_wait(smem_u32(&bars->acc_empty[slot]), acc.odd ^ 1u, p.poll_limit);
+                const uint32_t x_base = sX + s.at * kTileBytes;
+                const uint32_t d = tmem + (uint32_t)(NB == 3 ? 0 : acc.at * P::kSetCols);
+                product(ad ? d : d + rank16, x_base, ad ? 0 : rank16, ad ? idesc_first : idesc);
+                if (ad) mma_commit(smem_u32(&bars->u_full));
+                if (NB == 1) {
+                    mma_commit(smem_u32(&bars->a_empty[s.at]));
+                    ok = settle();                             // while this item's U is on its way
+                    if (ad) {
+                        owed = true; owed_last = it.last != 0; owed_slot = acc.at;
+                    } else {
+                        mma_commit(smem_u32(&bars->acc_full[acc.at]));
+                    }
+                    acc.next(p.slots);
+                } else {
+                    // the first block is finished at once, for the epilogue to go on with; the other two wait until it
+                    // has left both of their accumulators
+                    if (ad) {
+                        ok = u_wait();
+                        if (!ok) break;
+                        second(d + rank16, 0, idesc);
+                    }
+                    mma_commit(smem_u32(&bars->acc_full[0]));
+                    for (int j = 1; j < 3; ++j) ok = ok && mbar_wait_relaxed(smem_u32(&bars->acc_empty[j]), acc.odd ^ 1u, p.poll_limit);
                     if (!ok) break;
                     tc_fence_after();
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {
-                        const uint32_t off = (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32);
-                        mma_bf16(d, smem_desc_sw128(x_base + off), smem_desc_sw128(b_base + off), idesc, ks > 0 ? 1u : 0u);
-                    }
+                    product(d + rank16 + 128, x_base, rank16 + 128, idesc_two);
+                    mma_commit(smem_u32(&bars->a_empty[s.at]));
                     if (ad) {
-                        if (j == 0) {
-                            ok = mbar_wait(smem_u32(&bars->u_ready), (uint32_t)(u_items++) & 1u, p.poll_limit);
-                            if (!ok) break;
-                            tc_fence_after();
-                        }
-                        for (int ks = 0; ks < rank16 / 16; ++ks)
-                            mma_bf16_ta(d, tmem + (uint32_t)(kColUb + ks * 8), P::b_desc(sB + (uint32_t)(j * P::kB + ks * 32)), idesc, 1u);
+                        second(d + rank16 + 128, 1, idesc_two);
+                        u_done(it.last != 0);
                     }
-                    mma_commit(smem_u32(&bars->acc_full[slot]));
-                }
-                if (!ok) { raise_timeout(bars, p.status); break; }
-                mma_commit(smem_u32(&bars->a_empty[s.at]));
-                if (ad) {
-                    mma_commit(smem_u32(&bars->ub_empty));
-                    if (it.last) mma_commit(smem_u32(&bars->ad_empty));
-                }
-                // the next item's U at once: it turns into the second product's operand while the epilogue is still
-                // emptying the accumulators of this item
-                if (i + 1 < items) {
-                    q.next(kRing);
-                    s.next(stages);
-                    ok = begin(next);
-                    if (!ok) { raise_timeout(bars, p.status); break; }
-                    it = next;
+                    mma_commit(smem_u32(&bars->acc_full[1]));
+                    mma_commit(smem_u32(&bars->acc_full[2]));
+                    acc.odd ^= 1u;
                 }
             }
+            if (ok && !*abort_flag) ok = settle();
+            if (!ok) raise_timeout(bars, p.status);
             mma_commit(smem_u32(&bars->drain));                // tensor memory is freed below: every MMA must be done
             mbar_wait(smem_u32(&bars->drain), 0);
         }
@@ -396,18 +429,18 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         bool ok = true;
         for (int i = 0; i < items && ok; ++i, q.next(kRing), s.next(stages)) {
             if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
-            if (!mbar_wait_warp(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+            if (!mbar_wait_relaxed_warp(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) { raise_timeout(bars, p.status); break; }
             const Item it = bars->ring[q.at];
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q.at]));
             const int valid = it.rows - quad * 32;             // rows of the item among this warp's 32
-            for (int j = 0; j < nb; ++j, acc_turn.next(p.slots)) {
+            for (int j = 0; j < NB; ++j, acc_turn.next(p.slots)) {
                 const int slot = acc_turn.at;
-                ok = mbar_wait_warp(smem_u32(&bars->acc_full[slot]), acc_turn.odd, p.poll_limit);
-                if (ok && p.has_res) ok = mbar_wait_warp(smem_u32(&bars->r_full[s.at]), s.odd, p.poll_limit);
+                ok = mbar_wait_relaxed_warp(smem_u32(&bars->acc_full[slot]), acc_turn.odd, p.poll_limit);
+                if (ok && p.has_res) ok = mbar_wait_relaxed_warp(smem_u32(&bars->r_full[s.at]), s.odd, p.poll_limit);
                 if (!ok) { raise_timeout(bars, p.status); break; }
                 tc_fence_after();
-                const uint32_t t_addr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(kColAcc + slot * 128 + half * 64);
+                const uint32_t t_addr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(rank16 + slot * (NB == 3 ? 128 : P::kSetCols) + half * 64);
                 if (lane == 0) bulk_wait_read0();              // the previous store has read the staging rows
                 __syncwarp();
 #pragma unroll 1
@@ -468,26 +501,27 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         const int quad = warp & 3;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         int u_items = 0;
-        Turn q;
-        for (int i = 0; i < items; ++i, q.next(kRing)) {
+        Turn q, set;
+        for (int i = 0; i < items; ++i, q.next(kRing), set.next(NB == 3 ? 1 : p.slots)) {
             if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
-            if (!mbar_wait_warp(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+            if (!mbar_wait_relaxed_warp(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) { raise_timeout(bars, p.status); break; }
             const Item it = bars->ring[q.at];
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q.at]));
             if (it.adapter < 0) continue;
             const float scale = __ldg(p.scale + it.adapter);
-            if (!mbar_wait_warp(smem_u32(&bars->u_full), (uint32_t)u_items & 1u, p.poll_limit) ||
-                !mbar_wait_warp(smem_u32(&bars->ub_empty), ((uint32_t)u_items & 1u) ^ 1u, p.poll_limit)) {
+            if (!mbar_wait_relaxed_warp(smem_u32(&bars->u_full), (uint32_t)u_items & 1u, p.poll_limit) ||
+                !mbar_wait_relaxed_warp(smem_u32(&bars->ub_empty), ((uint32_t)u_items & 1u) ^ 1u, p.poll_limit)) {
                 raise_timeout(bars, p.status);
                 break;
             }
             ++u_items;
             tc_fence_after();
+            const uint32_t u = tmem + lanes + (uint32_t)(NB == 3 ? 0 : set.at * P::kSetCols);
             for (int c = 0; c < rank16 / 16; ++c) {            // 16 columns of U: one K step of the second product
                 uint32_t f[16], b[8];
-                tmem_ld_32x8(tmem + lanes + (uint32_t)(kColU + c * 16), f);
-                tmem_ld_32x8(tmem + lanes + (uint32_t)(kColU + c * 16 + 8), f + 8);
+                tmem_ld_32x8(u + (uint32_t)(c * 16), f);
+                tmem_ld_32x8(u + (uint32_t)(c * 16 + 8), f + 8);
                 tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -496,7 +530,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     const bool in = c * 16 + 2 * e < p.rank;
                     b[e] = in ? pack_bf16(__uint_as_float(f[2 * e]) * scale, __uint_as_float(f[2 * e + 1]) * scale) : 0u;
                 }
-                tmem_st_32x8(tmem + lanes + (uint32_t)(kColUb + c * 8), b);
+                tmem_st_32x8(tmem + lanes + (uint32_t)(p.col_ub + c * 8), b);
             }
             tmem_st_wait();
             tc_fence_before();
@@ -530,22 +564,21 @@ struct Call {
     int n_out;
 };
 
-template <int RANK>
-dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
-    using P = Place<RANK>;
-    static std::mutex mu;
-    static bool attr_set[64] = {};
-    static int sm_count[64] = {};
+// bytes of shared memory in front of the X stages: W and A_a, B_a, the staging rows
+int fixed_bytes(int nb, int rank, int place_rank) {
+    return nb * kTileBytes + ((rank + 15) & ~15) * 256 + nb * 128 * place_rank * 2 + kEpiWarps * 4096;
+}
+constexpr int kTail = (int)sizeof(Bars) + 1024;         // 1024: the base is aligned by hand
+
+template <int RANK, int NB>
+dg4_status launch_place(const dg4_graph* g, const Call& c, int sms, int64_t most, bool split, cudaStream_t st) {
+    using P = Place<RANK, NB>;
+    static std::atomic<bool> attr_set[64];
     int dev = 0;
     DG4_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
-    {
-        std::lock_guard<std::mutex> lock(mu);
-        if (!attr_set[dev]) {
-            DG4_CUDA_TRY(cudaFuncSetAttribute(adapter_proj_kernel<RANK>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
-            DG4_CUDA_TRY(cudaDeviceGetAttribute(&sm_count[dev], cudaDevAttrMultiProcessorCount, dev));
-            attr_set[dev] = true;
-        }
+    if (!attr_set[dev].load(std::memory_order_relaxed)) {
+        DG4_CUDA_TRY(cudaFuncSetAttribute(adapter_proj_kernel<RANK, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit));
+        attr_set[dev].store(true, std::memory_order_relaxed);
     }
     Params p;
     p.seg_ptr = c.seg ? c.seg->seg_ptr : nullptr;
@@ -554,50 +587,58 @@ dg4_status launch(const dg4_graph* g, const Call& c, cudaStream_t st) {
     p.n = g->n; p.n_adapters = c.ad->n_adapters; p.rank = c.ad->rank; p.scale = c.ad->scale;
     p.n_out = c.n_out; p.has_res = c.R != nullptr;
     p.status = g->dev_status; p.poll_limit = dg4i_poll_limit();
-    const int blocks = c.n_out / 128, sms = sm_count[dev];
-    // items: at most one per full tile and one ragged one per request
-    const int64_t most = (int64_t)g->n / kTileM + p.n_seg;
-    // Column blocks to different CTAs where the device holds all of them at once: two to an SM if two fit.  64 requests
-    // of one row: 11.7 us with a CTA per request, see the figure beside it for this form.
-    const int per_stage = kTileBytes * (c.R ? 2 : 1), tail = (int)sizeof(Bars) + 1024;
-    const int a_bytes = ((c.ad->rank + 15) & ~15) * 256;
-    const int one = kTileBytes + a_bytes + P::kB + kEpiWarps * 4096 + per_stage + tail;       // shared memory of such a CTA
-    const bool split = blocks > 1 && most * blocks <= sms * (2 * (one + 1024) <= 233472 ? 2 : 1);
-    p.nb = split ? 1 : blocks;
-    p.slots = split ? 1 : kSlots;
-    int off = p.nb * kTileBytes;
-    p.off_a = off; off += a_bytes;
-    p.off_b = off; off += p.nb * P::kB;
-    p.off_stage = off; off += kEpiWarps * 4096;
-    p.stages = !split && off + kMaxStages * per_stage + tail <= kSmemLimit ? kMaxStages : 1;
+    p.slots = NB == 3 ? 3 : split ? 1 : P::kSets;
+    p.col_ub = NB == 1 && split ? P::kSetCols : P::kColUb;
+    const int per_stage = kTileBytes * (p.has_res ? 2 : 1);
+    int off = fixed_bytes(NB, p.rank, RANK);
+    p.off_stage = off - kEpiWarps * 4096;
+    p.off_b = p.off_stage - NB * P::kB;
+    p.stages = !split && off + kMaxStages * per_stage + kTail <= kSmemLimit ? kMaxStages : 1;
     p.off_x = off; off += p.stages * kTileBytes;
     p.off_r = off; off += p.has_res ? p.stages * kTileBytes : 0;
-    p.off_bar = off; off += tail;                 // 1024 of it: the base is aligned by hand
+    p.off_bar = off; off += kTail;
     CUtensorMap map_x, map_w, map_r, map_a, map_b;
     OutMaps map_o;
     CHECK(dg4i_make_row_map(&map_w, c.W, c.n_out, 128, 128));
     CHECK(dg4i_make_row_map(&map_x, c.X, g->n, c.ldx, 128));
     map_r = map_x;
     if (c.R) CHECK(dg4i_make_row_map(&map_r, c.R, g->n, c.ldr, 128));
-    CHECK(dg4i_make_row_map(&map_a, c.ad->A, (int64_t)c.ad->n_adapters * c.ad->rank, 128, c.ad->rank));
-    CHECK(dg4i_make_map(&map_b, c.ad->B, c.ad->rank, (int64_t)c.ad->n_adapters * c.n_out, c.ad->rank, 128, RANK));
+    CHECK(dg4i_make_row_map(&map_a, c.ad->A, (int64_t)p.n_adapters * p.rank, 128, p.rank));
+    CHECK(dg4i_make_map(&map_b, c.ad->B, p.rank, (int64_t)p.n_adapters * c.n_out, p.rank, 128, RANK));
     for (int j = 0; j < 3; ++j) {
         map_o.m[j] = map_x;
         p.out[j] = nullptr; p.ldo[j] = 0;
-        if (j < blocks) {
+        if (j < c.n_out / 128) {
             CHECK(dg4i_make_row_map(&map_o.m[j], c.out[j], g->n, c.ldo[j], 32));
             p.out[j] = (__nv_bfloat16*)c.out[j]; p.ldo[j] = c.ldo[j];
         }
     }
-    const dim3 grid((unsigned)(most < sms ? most : sms), (unsigned)(blocks / p.nb));
-    adapter_proj_kernel<RANK><<<grid, kThreads, off, st>>>(map_x, map_w, map_r, map_a, map_b, map_o, p);
+    const dim3 grid((unsigned)(most < sms ? most : sms), (unsigned)(c.n_out / 128 / NB));
+    adapter_proj_kernel<RANK, NB><<<grid, kThreads, off, st>>>(map_x, map_w, map_r, map_a, map_b, map_o, p);
     dg4i_count_launch();
     DG4_CUDA_TRY(cudaGetLastError());
     return DG4_OK;
 }
 
+template <int RANK>
 dg4_status launch_rank(const dg4_graph* g, const Call& c, cudaStream_t st) {
-    return c.ad->rank <= 32 ? launch<32>(g, c, st) : launch<64>(g, c, st);
+    static std::atomic<int> sm_count[64];
+    int dev = 0;
+    DG4_CUDA_TRY(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
+    int sms = sm_count[dev].load(std::memory_order_relaxed);
+    if (sms == 0) {
+        DG4_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        sm_count[dev].store(sms, std::memory_order_relaxed);
+    }
+    // items: at most one per full tile and one ragged one per request
+    const int64_t most = (int64_t)g->n / kTileM + (c.seg ? c.seg->n_seg : 1);
+    if (c.n_out == 128) return launch_place<RANK, 1>(g, c, sms, most, false, st);
+    // Column blocks to different CTAs (of one item at most) where the device holds them all at once, two to an SM if two
+    // fit: each then fetches a third of W and ends with one block's epilogue instead of three.
+    const int one = fixed_bytes(1, c.ad->rank, RANK) + kTileBytes + kTail;
+    const bool split = most * 3 <= sms * (2 * (one + 1024) <= 233472 ? 2 : 1);
+    return split ? launch_place<RANK, 1>(g, c, sms, most, true, st) : launch_place<RANK, 3>(g, c, sms, most, false, st);
 }
 
 dg4_status check_adapters(const dg4_adapters* ad, int n_out) {
@@ -629,7 +670,7 @@ extern "C" dg4_status dg4_qkv_project_adapters(const dg4_graph* g, const dg4_des
     CHECK(dg4i_check_tensor("K", K, ldk, 2, 128));
     CHECK(dg4i_check_tensor("V", V, ldv, 2, 128));
     Call c = {X, ldx, W_qkv, adapters, segments, nullptr, 0, {Q, K, V}, {ldq, ldk, ldv}, 384};
-    return launch_rank(g, c, (cudaStream_t)stream);
+    return adapters->rank <= 32 ? launch_rank<32>(g, c, (cudaStream_t)stream) : launch_rank<64>(g, c, (cudaStream_t)stream);
 }
 
 extern "C" dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_desc* desc, const void* O, int64_t ldo,
@@ -646,5 +687,5 @@ extern "C" dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_des
     if (res) CHECK(dg4i_check_tensor("H_res", H_res, ldh, 2, 128));
     CHECK(dg4i_check_tensor("H_out", H_out, ldho, 2, 128));
     Call c = {O, ldo, W_o, adapters, segments, res ? H_res : nullptr, ldh, {H_out, nullptr, nullptr}, {ldho, 0, 0}, 128};
-    return launch_rank(g, c, (cudaStream_t)stream);
+    return adapters->rank <= 32 ? launch_rank<32>(g, c, (cudaStream_t)stream) : launch_rank<64>(g, c, (cudaStream_t)stream);
 }

@@ -81,6 +81,7 @@ class dg4_adapters(ctypes.Structure):
 
 
 _lib = None
+torch = None          # imported with the library; an import statement in every call would cost 0.4 us of some 7
 
 
 def library_path() -> str:
@@ -89,9 +90,10 @@ def library_path() -> str:
 
 def load():
     """Loads libdg4.so (building it with nvcc if it is missing or stale).  Raises if that is impossible."""
-    global _lib
+    global _lib, torch
     if _lib is not None:
         return _lib
+    import torch
     path = _build.LIB
     if _build.needs_build():
         path = _build.build()
@@ -207,7 +209,6 @@ def _i32(a):
 
 def _stream(stream):
     if stream is None:
-        import torch
         # the raw handle, without a stream object around it: 0.4 instead of 3.6 us of a call that takes about 8
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return int(getattr(stream, "cuda_stream", stream))                      # a raw handle or a torch stream
@@ -218,8 +219,9 @@ def _ptr(t):
 
 
 def _ld(t):
-    assert t.dim() == 2 and t.stride(1) == 1, "tensors are [rows, d] with unit inner stride"
-    return int(t.stride(0))
+    s = t.stride()
+    assert len(s) == 2 and s[1] == 1, "tensors are [rows, d] with unit inner stride"
+    return s[0]
 
 
 def desc(heads: int, dtype: int, scale: float, residual: bool = False, d: int = 128,
@@ -414,7 +416,7 @@ class Adapters:
 
 def segments(seg_ptr, seg_id) -> Segments:
     """seg_ptr [n_seg + 1] and seg_id [n_seg], CUDA int32: see dg4_segments in dg4.h."""
-    import torch
+    load()
     for t in (seg_ptr, seg_id):
         if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
             raise ValueError("segment arrays are contiguous one-dimensional CUDA int32 tensors")
@@ -425,7 +427,7 @@ def segments(seg_ptr, seg_id) -> Segments:
 
 def adapters(A, B, scale) -> Adapters:
     """A [n, rank, 128] and B [n, n_out, rank] bf16, scale [n] fp32, CUDA, contiguous: see dg4_adapters in dg4.h."""
-    import torch
+    load()
     if A.dim() != 3 or B.dim() != 3 or scale.dim() != 1 or A.shape[2] != 128 or B.shape[1] not in (128, 384) \
             or B.shape[2] != A.shape[1] or not A.shape[0] == B.shape[0] == scale.shape[0]:
         raise ValueError("adapters are A [n, rank, 128], B [n, 128 or 384, rank] and scale [n]")
@@ -443,7 +445,7 @@ def _struct(x):
 def _nodes(nodes):
     if nodes is None:
         return None, 0
-    import torch
+    load()
     if nodes.dtype != torch.int32 or nodes.dim() != 1 or not nodes.is_contiguous() or not nodes.is_cuda:
         raise ValueError("a node list is a contiguous one-dimensional CUDA int32 tensor")
     return _ptr(nodes), nodes.numel()
@@ -453,7 +455,6 @@ def _vec(t, rows=1):
     """Pointer of an fp32 vector of 128 (or of `rows` of them), or None."""
     if t is None:
         return None
-    import torch
     if t.dtype != torch.float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
         raise ValueError("norm and gate vectors are contiguous CUDA fp32 tensors of 128 elements each")
     return _ptr(t)
@@ -507,9 +508,10 @@ def dg4_sparse_attn_kv8_fwd(g: Graph, dsc: dg4_desc, Q, T, O, nodes=None, stream
 def dg4_norm_gate_fwd(g: Graph, dsc: dg4_desc, S, R, res_scale, gate, seg, post, pre, eps, R_out, Y, stream=None):
     """R_out = res_scale * R + gate * Norm_post(S), Y = Norm_pre(R_out).  gate [n_gates, 128] fp32 or None; post and
     pre: (gamma, beta or None); Y and pre may be None."""
+    lib = load()
     n_gates = 0 if gate is None else gate.numel() // 128
     pre = pre or (None, None)
-    _check(load().dg4_norm_gate_fwd(g.handle, ctypes.byref(dsc), _ptr(S), _ld(S), _ptr(R), _ld(R), float(res_scale),
+    _check(lib.dg4_norm_gate_fwd(g.handle, ctypes.byref(dsc), _ptr(S), _ld(S), _ptr(R), _ld(R), float(res_scale),
                                     _vec(gate, n_gates), n_gates, _struct(seg), _vec(post[0]), _vec(post[1]),
                                     _vec(pre[0]), _vec(pre[1]), float(eps), _ptr(R_out), _ld(R_out), _ptr(Y),
                                     _ld(Y) if Y is not None else 0, _stream(stream)))
@@ -580,7 +582,7 @@ def dg4_blocks_fwd_levelised(g: Graph, dsc: dg4_desc, H, blocks, eps, workspace,
 
 def dg4_graph_partition(g: Graph, delta: int):
     """Algorithm 1: returns (roots, group_ptr) as CUDA int32 tensors (roots trimmed to their number)."""
-    import torch
+    load()
     roots = torch.empty(g.n, dtype=torch.int32, device="cuda")
     group_ptr = torch.empty(int(g.info.n_levels) + 1, dtype=torch.int32, device="cuda")
     m = ctypes.c_int64(0)
