@@ -172,7 +172,7 @@ template <bool BF16, int LANES> struct Query {
     static constexpr int kN = 128 / LANES;
     uint32_t h[BF16 ? kN / 2 : 1];
     float f[BF16 ? 1 : kN];
-    float c;                                   // what makes a dot product with codes a score in log2 units
+    float c;                                   // what makes a dot product with codes times `scale` a score in log2 units
     template <int LPH>
     __device__ __forceinline__ void set(const float* q, float scale) {
         if (BF16) {
@@ -183,7 +183,7 @@ template <bool BF16, int LANES> struct Query {
             for (int o = LPH / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             const uint32_t b = lift(top);
             const float up = __uint_as_float(b << 23);
-            c = scale * __uint_as_float((254u - b) << 23);
+            c = 0.5f * scale * __uint_as_float((254u - b) << 23);
 #pragma unroll
             for (int e = 0; e < kN / 2; ++e) {
                 const __half2 x = __floats2half2_rn(q[2 * e] * up, q[2 * e + 1] * up);
@@ -208,12 +208,16 @@ template <bool BF16, int LANES> struct Row {
 
     Piece p[kPieces];
     uint32_t pair;
+    // bf16 rows: twice the scale (two instructions fewer), put right in the query's factor and at the end
+    __device__ static __forceinline__ float k_scale(uint32_t pair) { return BF16 ? twice_scale_k(pair) : scale_k(pair); }
+    __device__ static __forceinline__ float v_scale(uint32_t pair) { return BF16 ? twice_scale_v(pair) : scale_v(pair); }
     // codes: T + this lane's pieces; exps: T + this lane's pair
     __device__ __forceinline__ void load(const uint8_t* codes, const uint8_t* exps, uint32_t row, uint32_t ldt) {
-        const uint64_t off = (uint64_t)row * ldt;
-        if (kPieces == 2) ld_pieces2_nc(codes + off, p[0], p[kPieces - 1]);
-        else p[0] = ld_piece_nc(codes + off);
-        pair = ld_pair(exps + off);
+        // one wide multiply-add per address
+        const uint64_t pc = (uint64_t)row * ldt + (uint64_t)codes, pe = (uint64_t)row * ldt + (uint64_t)exps;
+        if (kPieces == 2) ld_pieces2_nc((const void*)pc, p[0], p[kPieces - 1]);
+        else p[0] = ld_piece_nc((const void*)pc);
+        pair = ld_pair((const void*)pe);
     }
     __device__ __forceinline__ float dot(const Query<BF16, LANES>& q) const {
         float a = 0.f, b = 0.f;
@@ -278,9 +282,10 @@ __device__ __forceinline__ void store_row(void* row, int sub, const float* f) {
 }
 
 // Lists of at most MAXN members from the fixed-width table.  A group of LANES lanes takes a node; the nodes in flight
-// across the GPU are a contiguous range.  All members of a list are computed without branches inside the warp up to the
-// longest of its lists; a member beyond a node's own list weighs zero (its filler is the node's own row, so no value
-// enters that the node does not read anyway).
+// across the GPU are a contiguous range.  All MAXN members are computed without a branch, so that their chains of
+// dependent instructions overlap (229 us on 1.01M two-hop cones; 244 with a branch around the members beyond the longest
+// list of the warp); a member beyond a node's own list weighs zero (its filler is the node's own row, so no value enters
+// that the node does not read anyway).
 // The loads run ahead of the arithmetic: lists two nodes ahead, and a member's row of the next node goes into the
 // registers of this node's as soon as that has been added up.
 template <bool BF16, int LANES, int LPH, int MAXN>
@@ -308,7 +313,7 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
         row[j].load(codes, exps, (uint32_t)(j ? __shfl_sync(0xffffffffu, pad, grp + j) : max(v, 0)), a.ldt);
     for (; base < (uint32_t)a.count; base += stride, slot += stride) {
         const int cnt = __shfl_sync(0xffffffffu, pad, grp);
-        const int most = __reduce_max_sync(0xffffffffu, cnt);
+        __syncwarp();          // keeps the loads of one round and the arithmetic of the next apart (without: 301 us)
         const bool more = base + stride < (uint32_t)a.count;                  // the warp has another round
         const int v2 = node_of(slot + 2 * stride), pad2 = list_of(v2);
         float acc[N];
@@ -321,30 +326,25 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
         for (int e = 0; e < N; ++e) acc[e] = 0.f;
 #pragma unroll
         for (int j = 0; j < MAXN; ++j) {
-            s[j] = -INFINITY;
-            if (j < most) {
-                float dot = row[j].dot(q);
+            float dot = row[j].dot(q);
 #pragma unroll
-                for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                if (j < cnt) s[j] = dot * q.c * scale_k(row[j].pair);
-                if (j == 0 && cnt <= 1) s[0] = 0.f;                           // softmax over one member: weight exactly 1
-                m = fmaxf(m, s[j]);
-            }
+            for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+            s[j] = j < cnt ? dot * q.c * row[j].k_scale(row[j].pair) : -INFINITY;
+            if (j == 0 && cnt <= 1) s[0] = 0.f;                               // softmax over one member: weight exactly 1
+            m = fmaxf(m, s[j]);
         }
 #pragma unroll
         for (int j = 0; j < MAXN; ++j) {
-            if (j < most) {
-                const float p = fast_exp2(s[j] - m);
-                z += p;
-                s[j] = p * scale_v(row[j].pair);                              // from here on the weight on the codes
-                top = fmaxf(top, s[j]);
-            }
+            const float p = fast_exp2(s[j] - m);
+            z += p;
+            s[j] = p * row[j].v_scale(row[j].pair);                           // from here on the weight on the codes
+            top = fmaxf(top, s[j]);
         }
         const uint32_t b = BF16 ? lift(top) : 127u;
-        const float up = __uint_as_float(b << 23), down = __uint_as_float((254u - b) << 23);
+        const float up = __uint_as_float(b << 23), down = 0.5f * __uint_as_float((254u - b) << 23);
 #pragma unroll
         for (int j = 0; j < MAXN; ++j) {
-            if (j < most) row[j].add(BF16 ? s[j] * up : s[j], acc);
+            row[j].add(BF16 ? s[j] * up : s[j], acc);
             const int u = j ? __shfl_sync(0xffffffffu, pad1, grp + j) : max(v1, 0);
             if (more) row[j].load(codes, exps, (uint32_t)u, a.ldt);
         }
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
 // Wider cones (3 to 8 hops, lists of up to 511 members): one warp per node, its groups of LANES lanes take alternate
 // members, UN in flight each; online softmax (running maximum and sum in 32 bits) per group, merged at the end.
 // For bf16 rows the sums are measured against a running reference of their own: the largest logarithm of a weight on
-// the codes, score + log2(V scale), less 14.  What its rounding does (2^-18 in the exponent) is far below that of the
+// the codes, score + log2(V scale), which is put at 14.  What its rounding does (2^-18 in the exponent) is far below that of the
 // fp16 weights.
 // The loads run ahead of the arithmetic: the next batch of members (of this node, or the first one of the next node)
 // goes into the registers of the present one as soon as that has been added up, the member ids a chunk of 32 ahead.
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
     int v = v1, beg = beg1, cnt = cnt1, ids = u1;                             // ids: the chunk of 32 members being read
     if (v < 0) return;
     raw.load((const char*)a.Q + (int64_t)v * a.ldq, sub);
-    // members past the end are stood in for by the last one, which is not added again (it may be NaN: not even 0 * it)
+    // members past the end are stood in for by the last one, which is not added again
 #pragma unroll
     for (int i = 0; i < UN; ++i)
         row[i].load(codes, exps, (uint32_t)__shfl_sync(0xffffffffu, ids, min(GROUPS * i + grp, min(cnt, 32) - 1)), a.ldt);
@@ -410,16 +410,16 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
         for (int e = 0; e < N; ++e) acc[e] = 0.f;
         int ids_next = 32 + lane < cnt ? a.nbr_idx[beg + 32 + lane] : 0;      // the chunk after `ids`
         for (int t = 0; t < cnt; t += BATCH) {
-            float s[UN], m_new = m, mw_new = mw;
+            float s[UN], lw[UN], m_new = m, mw_new = mw;
 #pragma unroll
             for (int i = 0; i < UN; ++i) {
                 float dot = row[i].dot(q);
 #pragma unroll
                 for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                s[i] = t + GROUPS * i + grp < cnt ? dot * q.c * scale_k(row[i].pair) : -INFINITY;
+                s[i] = t + GROUPS * i + grp < cnt ? dot * q.c * row[i].k_scale(row[i].pair) : -INFINITY;
                 if (i == 0 && cnt == 1 && grp == 0) s[0] = 0.f;               // softmax over one member: weight exactly 1
                 m_new = fmaxf(m_new, s[i]);
-                if (BF16) mw_new = fmaxf(mw_new, s[i] + log2_scale_v(row[i].pair) - 14.f);
+                if (BF16) mw_new = fmaxf(mw_new, lw[i] = s[i] + log2_scale_v(row[i].pair));
             }
             const float ref = finite(m_new), keep = fast_exp2(m - ref);       // one rescale per batch; 0 for the first
             const float ref_w = finite(mw_new), keep_w = BF16 ? fast_exp2(mw - ref_w) : keep;
@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
             for (int i = 0; i < UN; ++i) {
                 const float p = fast_exp2(s[i] - ref);
                 z += p;
-                const float w = BF16 ? fast_exp2(s[i] + log2_scale_v(row[i].pair) - ref_w) : p * scale_v(row[i].pair);
+                const float w = BF16 ? fast_exp2(lw[i] - (ref_w - 14.f)) : p * scale_v(row[i].pair);
                 if (t + GROUPS * i + grp < cnt) row[i].add(w, acc);
                 const int u = __shfl_sync(0xffffffffu, from, min((next & 31) + GROUPS * i + grp, min(left, 32) - 1) & 31);
                 if (more) row[i].load(codes, exps, (uint32_t)u, a.ldt);
@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
             mw = mmw;
         }
         // the two references differ by at most some 2^150: that power is put on in two halves
-        const float inv = fast_rcp(z), half = BF16 ? fast_exp2(0.5f * (finite(mw) - finite(m))) : 1.f;
+        const float inv = fast_rcp(z), half = BF16 ? fast_exp2(0.5f * (finite(mw) - 14.f - finite(m))) : 1.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] = BF16 ? acc[e] * half * inv * half : acc[e] * inv;
         if (grp == 0) store_row<BF16, LANES>((char*)a.O + (int64_t)v * a.ldo, sub, acc);
