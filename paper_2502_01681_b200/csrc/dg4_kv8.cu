@@ -282,10 +282,11 @@ __device__ __forceinline__ void store_row(void* row, int sub, const float* f) {
 }
 
 // Lists of at most MAXN members from the fixed-width table.  A group of LANES lanes takes a node; the nodes in flight
-// across the GPU are a contiguous range.  All MAXN members are computed without a branch, so that their chains of
-// dependent instructions overlap (229 us on 1.01M two-hop cones; 244 with a branch around the members beyond the longest
-// list of the warp); a member beyond a node's own list weighs zero (its filler is the node's own row, so no value enters
-// that the node does not read anyway).
+// across the GPU are a contiguous range.  A member beyond a node's own list weighs zero (its filler is the node's own
+// row, so no value enters that the node does not read anyway).  The scores come in two runs without a branch inside, the
+// first three members and the others, so that their chains of dependent instructions overlap; the sums skip what lies
+// beyond the longest list of the warp (1.01M two-hop cones: 216 us, under sustained load 248; with a branch at every
+// member 244, with none 229 and 262).
 // The loads run ahead of the arithmetic: lists two nodes ahead, and a member's row of the next node goes into the
 // registers of this node's as soon as that has been added up.
 template <bool BF16, int LANES, int LPH, int MAXN>
@@ -313,7 +314,7 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
         row[j].load(codes, exps, (uint32_t)(j ? __shfl_sync(0xffffffffu, pad, grp + j) : max(v, 0)), a.ldt);
     for (; base < (uint32_t)a.count; base += stride, slot += stride) {
         const int cnt = __shfl_sync(0xffffffffu, pad, grp);
-        __syncwarp();          // keeps the loads of one round and the arithmetic of the next apart (without: 301 us)
+        const int most = __reduce_max_sync(0xffffffffu, cnt);                 // the longest list of the warp
         const bool more = base + stride < (uint32_t)a.count;                  // the warp has another round
         const int v2 = node_of(slot + 2 * stride), pad2 = list_of(v2);
         float acc[N];
@@ -326,10 +327,13 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
         for (int e = 0; e < N; ++e) acc[e] = 0.f;
 #pragma unroll
         for (int j = 0; j < MAXN; ++j) {
-            float dot = row[j].dot(q);
+            s[j] = -INFINITY;
+            if (j < 3 || most > 3) {
+                float dot = row[j].dot(q);
 #pragma unroll
-            for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-            s[j] = j < cnt ? dot * q.c * row[j].k_scale(row[j].pair) : -INFINITY;
+                for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                if (j < cnt) s[j] = dot * q.c * row[j].k_scale(row[j].pair);
+            }
             if (j == 0 && cnt <= 1) s[0] = 0.f;                               // softmax over one member: weight exactly 1
             m = fmaxf(m, s[j]);
         }
@@ -344,7 +348,7 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
         const float up = __uint_as_float(b << 23), down = 0.5f * __uint_as_float((254u - b) << 23);
 #pragma unroll
         for (int j = 0; j < MAXN; ++j) {
-            row[j].add(BF16 ? s[j] * up : s[j], acc);
+            if (j < most) row[j].add(BF16 ? s[j] * up : s[j], acc);
             const int u = j ? __shfl_sync(0xffffffffu, pad1, grp + j) : max(v1, 0);
             if (more) row[j].load(codes, exps, (uint32_t)u, a.ldt);
         }
