@@ -3,23 +3,32 @@
 // K = 128, bf16 operands, fp32 accumulation in tensor memory.  U's rounding is that of any tensor-core operand: it
 // perturbs the adapter's contribution by at most 2^-8 of itself, as the rounding of y does to y.
 //
-// The work is cut into items: up to 128 consecutive rows of ONE request.  An item multiplies with its own adapter
-// only, and only its own rows are stored, so nothing is masked and no request's infinities or NaNs can meet
-// another's rows (0 * inf in a masked product would).  Each CTA takes a contiguous run of items, so neighbouring items mostly
-// share their adapter, which is fetched into shared memory only when it changes.
+// The work is cut into items: up to 128 consecutive rows of ONE request.  An item multiplies with its own adapter only,
+// and only its own rows are stored, so nothing is masked and no request's infinities or NaNs can meet another's rows
+// (0 * inf in a masked product would).  Each CTA takes a contiguous run of items, so neighbouring items mostly share
+// their adapter, which is fetched into shared memory only when it changes.
 //
 // One persistent CTA per SM, fourteen warps:
-//   warp 0       producer: W once, the item's rows of X (and of the residual) by TMA, the adapter when it changes; it
+//   warp 0       producer: W once, the item's rows of X by TMA, the adapter when it changes, the residual's rows (on a
+//                barrier of their own: their buffer comes back from the epilogue, later than X's from the products); it
 //                alone walks the requests and passes each item on in a small ring of descriptors;
-//   warp 1       owns tensor memory, issues tcgen05.mma: U = X A^T first, then the base product of every 128-column
-//                block, then, once U stands in tensor memory as bf16, the products U B^T on top of the base blocks
-//                (A operand from tensor memory, B from shared memory);
+//   warp 1       owns tensor memory, issues tcgen05.mma: U and the first 128-column block as one product; once U stands
+//                in tensor memory as bf16, U B^T on top of the block (A operand from tensor memory); with three blocks
+//                the other two as one 256-column product, in the same two steps;
 //   warps 2-9    epilogue: each owns 32 rows x 64 columns of a block; tensor memory -> bf16 -> its own 4 KB of
 //                staging -> TMA store, or 16-byte stores where the item ends inside the 32 rows;
-//   warps 10-13  U: tensor memory -> * scale -> bf16 -> tensor memory, while the base products run.
-// Bound by HBM: a QKV row is 256 bytes in, 768 out, and 98 + 1 r kflop (58 % of the machine's ratio at rank 64).
-// With few items (decoding: one row per request) the column blocks of an item go to different CTAs instead, so that
-// each fetches a third of W.
+//   warps 10-13  U: tensor memory -> * scale -> bf16 -> tensor memory, while other products run.
+// One block per CTA (the output projection): the next item's first product goes before this item's second one, which
+// waits for U.  Few items (decoding: one row per request): an item's three column blocks go to different CTAs, two to an
+// SM, so that each fetches a third of W and has one block's epilogue.
+//
+// Bound by HBM, and under sustained load by power: a QKV row is 256 bytes in, 768 out, and 98 + r kflop.  1.01M rows,
+// rank 16, 200 requests: 186 us = 5.6 TB/s (86 % of the measured copy rate; the plain projection takes 185), sustained
+// 202 us, the SM clock falling from 1.97 to 1.5 GHz at 1 kW.  That is why the waits are suspended ones and the products
+// few and wide: a product of N columns reads the same 128 rows of X from shared memory whatever N is, so U apart and
+// three blocks apart (36 instructions of N <= 128 per item instead of 19) took 219 us.  Rank 64: 246 us, one X stage
+// beside W_qkv (rows stored from registers, without staging, made room for two and took 400).  Output projection with
+// residual, rank 64: 130 us = 6.0 TB/s, sustained 137.  64 requests of one row each: 8.3 us a call.
 //
 // Every mbarrier wait is bounded.  On expiry the kernel records DG4_ERR_TIMEOUT and raises an abort flag; every warp
 // leaves at its next item at the latest, without meeting others.  Then the producer waits for the copies it has started,

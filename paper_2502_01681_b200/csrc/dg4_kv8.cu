@@ -1,8 +1,9 @@
 // The 8-bit K | V table: writing rows, reading them back, and sparse attention over it.
 //
-// All three are bound by memory, so each row passes through registers once: 16 lanes per row (two rows per warp),
-// 8 elements of K and of V per lane (see dg4_kv8_core.cuh for the row).  A written row costs 512 + 288 bytes in
-// bf16; a gathered neighbour costs 288 bytes instead of 512.
+// Writing and reading are bound by HBM: 16 lanes per row (two rows per warp), 8 elements of K and of V per lane (see
+// dg4_kv8_core.cuh for the row); each row passes through registers once, 512 + 288 bytes in bf16.  1.01M rows written
+// and read back: 278 us, 5.8 TB/s (90 % of the measured copy rate); 250 007 fp32 rows: 111 us.
+// The attention gathers 288 bytes per member instead of 512 and is bound by instructions (see there).
 
 #include "dg4_internal.h"
 #include "dg4_kv8_core.cuh"

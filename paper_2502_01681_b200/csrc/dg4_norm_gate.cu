@@ -2,12 +2,13 @@
 //     R' = res_scale * R + gate * Norm_post(S),      Y = Norm_pre(R'),
 // S the sub-layer's output, R the residual stream, the gate a vector per request.  Everything between the two loads
 // and the two stores of a row stays in registers in 32 bits (Y is computed from the unrounded R'), so a bf16 row
-// costs 512 bytes in and 512 out, which is the bound: the arithmetic is some 20 operations per element.
+// costs 512 bytes in and 512 out, which is the bound: 1.01M rows in 164 us, 6.3 TB/s (98 % of the measured copy rate).
 //
-// 8 lanes per row, 16 elements per lane, four consecutive rows per warp: a row's four sums then take 3 shuffles each for
-// four rows at once, and the arithmetic runs on pairs (packed fp32 instructions).  The norm vectors lie in shared memory
-// in the order the lanes read them, the gate in registers.  A warp walks chunks of up to 16 consecutive rows (32: 168 us, 8: 164, 4: 167); the next
-// four rows are loaded while four are worked on.  The request of a row is found by a 32-way search over the offsets
+// 8 lanes per row, 16 elements per lane, four consecutive rows per warp: each sum over a row takes 3 shuffles for four
+// rows at once, and the arithmetic runs on pairs (packed fp32 instructions).  The norm vectors lie in shared memory in
+// the order the lanes read them, the gate in registers.  A warp walks chunks of up to 16 consecutive rows (chunks of 32:
+// 168 us, of 8: 164, of 4: 167); the next four rows are loaded while four are worked on.  (16 lanes per row and the
+// vectors in registers: 224 us; a warp per row: 230.)  The request of a row is found by a 32-way search over the offsets
 // (each step one load and one ballot), only when the four rows leave the request last found; where they belong to
 // several requests, each row's lanes search for their own.  Mean and variance are taken in two passes over the
 // registers, so a large common offset of a row does not cancel in the variance.

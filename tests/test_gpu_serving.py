@@ -226,23 +226,32 @@ def test_wild_offsets_stay_inside_the_tensors():
     assert dg4.dg4_graph_poll_status(g) == 0
 
 
-def test_adapter_waits_that_run_out_are_reported_and_leave_the_device_usable():
-    n = 20000
-    g = edgeless(n)
-    x, w, ad = normal(1, (n, 128)), normal(2, (384, 128), 0.1), make_adapters(3, 3, 16, 384)
-    seg = dg4.segments(i32([0, 100, 9000, n]), i32([0, 1, 2]))
-    out = [torch.empty((n, 128), dtype=BF16, device="cuda") for _ in range(3)]
+@pytest.mark.parametrize("n,rank,out_only", [(200000, 16, False), (200000, 64, False), (300, 16, False), (200000, 16, True), (200000, 64, True)])
+def test_adapter_waits_that_run_out_are_reported_and_leave_the_device_usable(n, rank, out_only):
+    g, n_out = edgeless(n), 128 if out_only else 384
+    ptr, ids = [0, n // 50, n // 2, n], [0, 1, 2]
+    x, w, ad, res = normal(1, (n, 128)), normal(2, (n_out, 128), 0.1), make_adapters(3, 3, rank, n_out), normal(9, (n, 128))
+    seg = dg4.segments(i32(ptr), i32(ids))
+    out = [torch.empty((n, 128), dtype=BF16, device="cuda") for _ in range(n_out // 128)]
+
+    def call(graph):
+        if out_only:
+            dg4.dg4_out_project_adapters(graph, desc(residual=True), x, w, ad, seg, res, *out)
+        else:
+            dg4.dg4_qkv_project_adapters(graph, desc(), x, w, ad, seg, *out)
+
     dg4.dg4_debug_set_poll_limit(1)
     try:
-        dg4.dg4_qkv_project_adapters(g, desc(), x, w, ad, seg, *out)
+        call(g)
         torch.cuda.synchronize()
     finally:
         dg4.dg4_debug_set_poll_limit(0)
-    assert dg4.dg4_graph_poll_status(g) == dg4.DG4_ERR_TIMEOUT
+    # one poll of a suspended wait lasts up to 640 ns, so the waits of a call with one item per CTA may all be over in it
+    assert dg4.dg4_graph_poll_status(g) in ((dg4.DG4_ERR_TIMEOUT,) if n > 1000 else (0, dg4.DG4_ERR_TIMEOUT))
     g2 = edgeless(n)
-    dg4.dg4_qkv_project_adapters(g2, desc(), x, w, ad, seg, *out)
+    call(g2)
     assert dg4.dg4_graph_poll_status(g2) == 0
-    y, tol, _ = project_ref(x, w, ad, [0, 100, 9000, n], [0, 1, 2])
+    y, tol, _ = project_ref(x, w, ad, ptr, ids, res if out_only else None)
     for j, t in enumerate(out):
         within(t, y[:, j * 128:(j + 1) * 128], tol[:, j * 128:(j + 1) * 128], j)
 
@@ -637,6 +646,71 @@ def test_two_streams_at_once_give_the_same_bits():
             dg4.dg4_qkv_project_adapters(g, desc(), x, w, ad, seg, *out, stream=st)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for p, q in zip(want, got) for a, b in zip(p, q))
+
+
+def test_small_calls_on_three_streams_at_once():
+    n = 96                                                       # column blocks on different CTAs, two to an SM
+    g = edgeless(n)
+    w, wo = normal(2, (384, 128), 0.1), normal(3, (128, 128), 0.1)
+    ad, ado = make_adapters(4, 96, 16, 384), make_adapters(7, 96, 16, 128)
+    seg = dg4.segments(i32(range(n + 1)), i32((i * 37) % 97 - 1 for i in range(n)))
+    xs = [normal(20 + i, (n, 128)) for i in range(3)]
+    new = lambda: [torch.zeros((n, 128), dtype=BF16, device="cuda") for _ in range(4)]  # noqa: E731
+    want, got, streams = [new() for _ in xs], [new() for _ in xs], [torch.cuda.Stream() for _ in xs]
+
+    def call(x, y, stream):
+        dg4.dg4_qkv_project_adapters(g, desc(), x, w, ad, seg, *y[:3], stream=stream)
+        dg4.dg4_out_project_adapters(g, desc(residual=True), x, wo, ado, seg, x, y[3], stream=stream)
+
+    for x, y in zip(xs, want):
+        call(x, y, None)
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for x, y, st in zip(xs, got, streams):
+            call(x, y, st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for p, q in zip(want, got) for a, b in zip(p, q))
+    assert dg4.dg4_graph_poll_status(g) == 0
+
+
+def test_a_captured_call_reads_the_requests_and_lists_of_its_replay():
+    n = 2000
+    g, lists = circuit(12, 20, n - 20, 2)
+    x, w, ad = normal(1, (n, 128)), normal(2, (384, 128), 0.1), make_adapters(3, 3, 16, 384)
+    ptr, ids, nodes = i32([0, 500, n]), i32([0, 1]), i32([3, 4, 5, 6])
+    seg = dg4.segments(ptr, ids)
+    gate, post = normal(5, (3, 128), 0.7, torch.float32), vectors(6)
+    q, k, v, o, r2 = (torch.zeros((n, 128), dtype=BF16, device="cuda") for _ in range(5))
+    t = torch.zeros((n, 288), dtype=torch.uint8, device="cuda")
+
+    def step():
+        dg4.dg4_qkv_project_adapters(g, desc(), x, w, ad, seg, q, k, v)
+        dg4.dg4_kv8_write(g, desc(), k, v, t, nodes)
+        dg4.dg4_sparse_attn_kv8_fwd(g, desc(), q, t, o, nodes)
+        dg4.dg4_norm_gate_fwd(g, desc(), o, x, 1.0, gate, seg, post, None, 1e-5, r2, None)
+
+    step()
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for p, i, u in (([0, 1, 2], [2, 2], [0, 1, 2, 1999]), ([7, 1400, 1999], [-1, 0], [1999, 1998, 0, -1]), ([n, n, n], [0, 1], [-1, -1, -1, -1])):
+        ptr.copy_(i32(p)), ids.copy_(i32(i)), nodes.copy_(i32(u))
+        for a in (q, k, v, o, r2, t):
+            a.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [a.clone() for a in (q, k, v, o, r2, t)]
+        for a in (q, k, v, o, r2, t):
+            a.zero_()
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (q, k, v, o, r2, t)))
+        y, tol, seen = project_ref(x, w, ad, p, i)
+        within(q[seen.cuda()], y[seen, :128], tol[seen, :128])
+        assert bool((q[~seen.cuda()] == 0).all()) and bool((r2[~seen.cuda()] == 0).all())
 
 
 # ---------------------------------------------------------------------------------------------------
