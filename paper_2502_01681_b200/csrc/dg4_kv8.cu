@@ -372,6 +372,7 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
 template <bool BF16, int LANES, int LPH>
 __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a) {
     constexpr int GROUPS = 32 / LANES, UN = 4, BATCH = GROUPS * UN, N = Row<BF16, LANES>::kN;
+    static_assert(32 % BATCH == 0, "a batch lies in one chunk of member ids");
     const int lane = threadIdx.x & 31, sub = lane & (LANES - 1), grp = lane / LANES;
     const uint32_t warps = gridDim.x * (blockDim.x >> 5);
     const uint8_t* codes = a.T + sub * (256 / LANES);
