@@ -209,6 +209,25 @@ def test_strided_rows_and_interleaved_outputs():
     assert bool((buf[:, 384:] == 3.0).all())
 
 
+def test_row_offsets_pass_32_bits():
+    n, ld = 20000, 131072                                        # 5 GB from the first row to the last
+    g = edgeless(n)
+    x, w, ad, res = normal(1, (n, 128)), normal(2, (128, 128), 0.1), make_adapters(3, 3, 16, 128), normal(5, (n, 128))
+    seg = dg4.segments(i32([0, 7000, n - 3]), i32([2, 0]))
+    gate, post, pre = normal(6, (3, 128), 0.7, torch.float32), vectors(7), vectors(9)
+    want, r2, y = (torch.zeros((n, 128), dtype=BF16, device="cuda") for _ in range(3))
+    dg4.dg4_out_project_adapters(g, desc(residual=True), x, w, ad, seg, res, want)
+    dg4.dg4_norm_gate_fwd(g, desc(), want, res, 0.5, gate, seg, post, pre, 1e-5, r2, y)
+    far = torch.zeros((n, ld), dtype=BF16, device="cuda")
+    a, b, c, d, e = (far[:, 256 * i: 256 * i + 128] for i in range(5))
+    a.copy_(x), b.copy_(res)
+    dg4.dg4_out_project_adapters(g, desc(residual=True), a, w, ad, seg, b, c)
+    dg4.dg4_norm_gate_fwd(g, desc(), c, b, 0.5, gate, seg, post, pre, 1e-5, d, e)
+    torch.cuda.synchronize()
+    assert torch.equal(c, want) and torch.equal(d, r2) and torch.equal(e, y)
+    assert not bool(far[:, 128:256].any()) and not bool(far[:, 1152:2048].any())
+
+
 def test_wild_offsets_stay_inside_the_tensors():
     n = 640
     g = edgeless(n)
