@@ -46,7 +46,7 @@ def test_node_lists_and_vectors_are_checked_before_the_library_is_reached():
     for bad in (torch.zeros(3, dtype=torch.int64), torch.zeros(3, dtype=torch.int32), torch.zeros((2, 2), dtype=torch.int32)):
         for call in (dg4.dg4_kv8_write, dg4.dg4_kv8_read, dg4.dg4_sparse_attn_kv8_fwd):
             with pytest.raises(ValueError):
-                call(None, None, None, None, *([None] if call is not dg4.dg4_sparse_attn_kv8_fwd else []), bad)
+                call(None, None, None, None, None, nodes=bad)
     from types import SimpleNamespace
     with pytest.raises(ValueError):
         dg4.dg4_norm_gate_fwd(SimpleNamespace(handle=None), dg4.desc(8, dg4.DG4_BF16, 0.25), torch.zeros((1, 128)), torch.zeros((1, 128)), 1.0, torch.ones((1, 128)), None,
