@@ -23,12 +23,12 @@
 // SM, so that each fetches a third of W and has one block's epilogue.
 //
 // Bound by HBM, and under sustained load by power: a QKV row is 256 bytes in, 768 out, and 98 + r kflop.  1.01M rows,
-// rank 16, 200 requests: 186 us = 5.6 TB/s (86 % of the measured copy rate; the plain projection takes 185), sustained
-// 202 us, the SM clock falling from 1.97 to 1.5 GHz at 1 kW.  That is why the waits are suspended ones and the products
+// rank 16, 200 requests: 189 us = 5.5 TB/s (85 % of the measured copy rate; the plain projection takes 185), sustained
+// 195 us, the SM clock falling from 1.97 to 1.5 GHz at 1 kW.  That is why the waits are suspended ones and the products
 // few and wide: a product of N columns reads the same 128 rows of X from shared memory whatever N is, so U apart and
-// three blocks apart (36 instructions of N <= 128 per item instead of 19) took 219 us.  Rank 64: 246 us, one X stage
+// three blocks apart (36 instructions of N <= 128 per item instead of 19) took 219 us.  Rank 64: 240 us, one X stage
 // beside W_qkv (rows stored from registers, without staging, made room for two and took 400).  Output projection with
-// residual, rank 64: 130 us = 6.0 TB/s, sustained 137.  64 requests of one row each: 8.3 us a call.
+// residual, rank 64: 130 us = 6.0 TB/s, sustained 137.  64 requests of one row each: 7.4 us a call, 2 048 of them 36.
 //
 // Every mbarrier wait is bounded.  On expiry the kernel records DG4_ERR_TIMEOUT and raises an abort flag; every warp
 // leaves at its next item at the latest, without meeting others.  Then the producer waits for the copies it has started,
@@ -86,7 +86,8 @@ struct Bars {
     uint64_t r_full[kMaxStages], r_empty[kMaxStages];
     uint64_t acc_full[kSlots];
     uint64_t acc_empty[kSlots];
-    uint64_t ad_full, ad_empty;     // the adapter in shared memory
+    uint64_t la_full, la_empty;     // A_a in shared memory (read by the first product)
+    uint64_t lb_full, lb_empty;     // B_a in shared memory (read by the second one)
     uint64_t u_full, u_ready, ub_empty;
     uint64_t item_full[kRing], item_empty[kRing];
     uint64_t drain;
@@ -221,7 +222,7 @@ __device__ __forceinline__ void find_items(const Params& p, Bars* bars) {
 }
 
 template <int RANK, int NB>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, NB == 3 ? 1 : 2)
 adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                     const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_a,
                     const __grid_constant__ CUtensorMap map_b, const __grid_constant__ OutMaps map_o, Params p) {
@@ -248,8 +249,10 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         init(bars->r_empty, kMaxStages, kEpiWarps);
         init(bars->acc_full, kSlots, 1);
         init(bars->acc_empty, kSlots, kEpiWarps);
-        init(&bars->ad_full, 1, 1);
-        init(&bars->ad_empty, 1, 1);
+        init(&bars->la_full, 1, 1);
+        init(&bars->la_empty, 1, 1);
+        init(&bars->lb_full, 1, 1);
+        init(&bars->lb_empty, 1, 1);
         init(&bars->u_full, 1, 1);
         init(&bars->u_ready, 1, kUWarps);
         init(&bars->ub_empty, 1, 1);
@@ -284,7 +287,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
     if (warp == 0) {
         // ------------------------------------------------------------------ producer
         if (lane == 0) {
-            int armed = 0, armed_r = 0, loads = 0;
+            int armed = 0, armed_r = 0, armed_la = 0, loads = 0;
             Turn q, s;                                         // of the descriptors, of the stages
             Walk w = bars->first;
             int held = -1;                                     // the adapter in shared memory, -1 = released
@@ -304,13 +307,17 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     tma_load_2d(sX + s.at * kTileBytes + h * kHalfBytes, &map_x, h * 64, it.row0, smem_u32(&bars->a_full[s.at]));
                 armed = i + 1;
                 if (it.adapter >= 0 && it.adapter != held) {
-                    // the previous adapter's last products (load index `loads` - 1) must have read it
-                    if (loads > 0 && !mbar_wait_relaxed(smem_u32(&bars->ad_empty), ((uint32_t)loads & 1u) ^ 1u, p.poll_limit)) { raise_timeout(bars, p.status); break; }
-                    const uint32_t ad = smem_u32(&bars->ad_full);
-                    mbar_expect_tx(ad, (uint32_t)(p.rank * 256 + NB * P::kB));
-                    for (int h = 0; h < 2; ++h) tma_load_2d(sW + h * w_half, &map_a, h * 64, it.adapter * p.rank, ad);
+                    // A_a's place is free once the previous adapter's last first product has read it, B_a's after its
+                    // last second product: A_a travels while the item before is still being finished
+                    const uint32_t free = ((uint32_t)loads & 1u) ^ 1u;
+                    if (loads > 0 && !mbar_wait_relaxed(smem_u32(&bars->la_empty), free, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                    mbar_expect_tx(smem_u32(&bars->la_full), (uint32_t)(p.rank * 256));
+                    for (int h = 0; h < 2; ++h) tma_load_2d(sW + h * w_half, &map_a, h * 64, it.adapter * p.rank, smem_u32(&bars->la_full));
+                    armed_la = loads + 1;
+                    if (loads > 0 && !mbar_wait_relaxed(smem_u32(&bars->lb_empty), free, p.poll_limit)) { raise_timeout(bars, p.status); break; }
+                    mbar_expect_tx(smem_u32(&bars->lb_full), (uint32_t)(NB * P::kB));
                     for (int j = 0; j < NB; ++j)
-                        tma_load_2d(sB + j * P::kB, &map_b, 0, it.adapter * p.n_out + (block0 + j) * 128, ad);
+                        tma_load_2d(sB + j * P::kB, &map_b, 0, it.adapter * p.n_out + (block0 + j) * 128, smem_u32(&bars->lb_full));
                     ++loads;
                     held = it.adapter;
                 }
@@ -329,7 +336,8 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 mbar_wait(smem_u32(&bars->a_full[i % stages]), (uint32_t)(i / stages) & 1u);
             for (int i = (armed_r > stages ? armed_r - stages : 0); i < armed_r; ++i)
                 mbar_wait(smem_u32(&bars->r_full[i % stages]), (uint32_t)(i / stages) & 1u);
-            if (loads > 0) mbar_wait(smem_u32(&bars->ad_full), (uint32_t)(loads - 1) & 1u);
+            if (armed_la > 0) mbar_wait(smem_u32(&bars->la_full), (uint32_t)(armed_la - 1) & 1u);
+            if (loads > 0) mbar_wait(smem_u32(&bars->lb_full), (uint32_t)(loads - 1) & 1u);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
@@ -340,8 +348,8 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             int loads = 0, u_items = 0;
             Turn q, s, acc;                                    // of the descriptors, the stages, the accumulators
             bool fresh = true;                                 // the next adapter item brings a new adapter
-            bool owed = false, owed_last = false;              // NB = 1: the second product of the item before
-            int owed_slot = 0;
+            bool owed = false, owed_last = false, owed_new = false;   // NB = 1: the second product of the item before
+            int owed_slot = 0, b_loads = 0;
             // d = X * (rows of A_a and W from row0 on)^T over K = 128, as many as `id` says
             auto product = [&](uint32_t d, uint32_t x_base, int row0, uint32_t id) {
 #pragma unroll
@@ -354,19 +362,20 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 for (int ks = 0; ks < rank16 / 16; ++ks)
                     mma_bf16_ta(d, tmem + (uint32_t)(p.col_ub + ks * 8), P::b_desc(sB + (uint32_t)(j * P::kB + ks * 32)), id, 1u);
             };
-            auto u_wait = [&]() {
-                const bool r = mbar_wait_relaxed(smem_u32(&bars->u_ready), (uint32_t)(u_items++) & 1u, p.poll_limit);
+            auto u_wait = [&](bool new_adapter) {              // what the second product needs: U, and B_a
+                bool r = mbar_wait_relaxed(smem_u32(&bars->u_ready), (uint32_t)(u_items++) & 1u, p.poll_limit);
+                if (new_adapter) r = r && mbar_wait_relaxed(smem_u32(&bars->lb_full), (uint32_t)(b_loads++) & 1u, p.poll_limit);
                 tc_fence_after();
                 return r;
             };
             auto u_done = [&](bool last) {
                 mma_commit(smem_u32(&bars->ub_empty));
-                if (last) mma_commit(smem_u32(&bars->ad_empty));
+                if (last) mma_commit(smem_u32(&bars->lb_empty));
             };
             auto settle = [&]() {                              // NB = 1: what is owed
                 if (!owed) return true;
                 owed = false;
-                if (!u_wait()) return false;
+                if (!u_wait(owed_new)) return false;
                 second(tmem + (uint32_t)(owed_slot * P::kSetCols + rank16), 0, idesc);
                 mma_commit(smem_u32(&bars->acc_full[owed_slot]));
                 u_done(owed_last);
@@ -378,13 +387,12 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 const Item it = bars->ring[q.at];
                 mbar_arrive(smem_u32(&bars->item_empty[q.at]));
                 const bool ad = it.adapter >= 0;
-                // what is owed comes first if this item cannot begin yet, or if its adapter takes the owed one's place
-                if (owed && ((ad && fresh) || !mbar_test(smem_u32(&bars->a_full[s.at]), s.odd) ||
-                             !mbar_test(smem_u32(&bars->acc_empty[acc.at]), acc.odd ^ 1u))) ok = settle();
+                const bool new_adapter = ad && fresh;
+                // what is owed comes first if this item cannot begin yet
+                if (owed && (!mbar_test(smem_u32(&bars->a_full[s.at]), s.odd) || !mbar_test(smem_u32(&bars->acc_empty[acc.at]), acc.odd ^ 1u) ||
+                             (new_adapter && !mbar_test(smem_u32(&bars->la_full), (uint32_t)loads & 1u)))) ok = settle();
                 ok = ok && mbar_wait_relaxed(smem_u32(&bars->a_full[s.at]), s.odd, p.poll_limit);
-                if (ok && ad && fresh) {
-                    ok = mbar_wait_relaxed(smem_u32(&bars->ad_full), (uint32_t)(loads++) & 1u, p.poll_limit);
-                }
+                if (new_adapter) ok = ok && mbar_wait_relaxed(smem_u32(&bars->la_full), (uint32_t)(loads++) & 1u, p.poll_limit);
                 if (ad) fresh = it.last != 0;
                 ok = ok && mbar_wait_relaxed(smem_u32(&bars->acc_empty[acc.at]), acc.odd ^ 1u, p.poll_limit);
                 if (!ok) break;
@@ -393,11 +401,12 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 const uint32_t d = tmem + (uint32_t)(NB == 3 ? 0 : acc.at * P::kSetCols);
                 product(ad ? d : d + rank16, x_base, ad ? 0 : rank16, ad ? idesc_first : idesc);
                 if (ad) mma_commit(smem_u32(&bars->u_full));
+                if (ad && it.last) mma_commit(smem_u32(&bars->la_empty));
                 if (NB == 1) {
                     mma_commit(smem_u32(&bars->a_empty[s.at]));
                     ok = settle();                             // while this item's U is on its way
                     if (ad) {
-                        owed = true; owed_last = it.last != 0; owed_slot = acc.at;
+                        owed = true; owed_last = it.last != 0; owed_new = new_adapter; owed_slot = acc.at;
                     } else {
                         mma_commit(smem_u32(&bars->acc_full[acc.at]));
                     }
@@ -406,7 +415,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     // the first block is finished at once, for the epilogue to go on with; the other two wait until it
                     // has left both of their accumulators
                     if (ad) {
-                        ok = u_wait();
+                        ok = u_wait(new_adapter);
                         if (!ok) break;
                         second(d + rank16, 0, idesc);
                     }
@@ -450,6 +459,42 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 if (!ok) { raise_timeout(bars, p.status); break; }
                 tc_fence_after();
                 const uint32_t t_addr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(rank16 + slot * (NB == 3 ? 128 : P::kSetCols) + half * 64);
+                const int row0 = it.row0 + quad * 32;
+                if (NB == 3) {
+                    // both halves at once (one CTA per SM has the registers), and the accumulator handed back before
+                    // the conversions.  A residual does not come with three blocks.
+                    uint32_t acc[64];
+                    if (valid > 0) {
+                        tmem_ld_32x32(t_addr, acc);
+                        tmem_ld_32x32(t_addr + 32, acc + 32);
+                        tmem_ld_wait();
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(smem_u32(&bars->acc_empty[slot]));
+                        bulk_wait_read0();                     // the previous store has read the staging rows
+                    }
+                    __syncwarp();
+                    __nv_bfloat16* outp = p.out[block0 + j] + (int64_t)(row0 + lane) * p.ldo[block0 + j] + half * 64;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t out[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) out[e] = pack_bf16(__uint_as_float(acc[c * 8 + 2 * e]), __uint_as_float(acc[c * 8 + 2 * e + 1]));
+                        if (valid >= 32) st_shared_v4(stage + sw128_offset(lane, c), out);
+                        else if (lane < valid) st_global_v4(outp + c * 8, out);       // the item ends inside these rows
+                    }
+                    if (valid >= 32) {
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&map_o.m[block0 + j], half * 64, row0, stage);
+                            bulk_commit();
+                        }
+                    }
+                    continue;
+                }
                 if (lane == 0) bulk_wait_read0();              // the previous store has read the staging rows
                 __syncwarp();
 #pragma unroll 1
@@ -483,7 +528,6 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                     mbar_arrive(smem_u32(&bars->acc_empty[slot]));
                     if (p.has_res) mbar_arrive(smem_u32(&bars->r_empty[s.at]));
                 }
-                const int row0 = it.row0 + quad * 32;
                 if (valid >= 32) {
                     fence_proxy_async_smem();
                     __syncwarp();
