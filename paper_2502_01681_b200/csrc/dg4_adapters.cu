@@ -51,6 +51,7 @@ constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kMaxStages = 2;
 constexpr int kSlots = 3;                         // accumulators of 128 columns, at most
 constexpr int kRing = 4;                          // item descriptors in flight
+constexpr int kUTurns = 2;                        // barriers that announce U's product, in turn
 constexpr int kRankMax = 64;
 
 // Where things lie, for ranks up to RANK = 32 or 64 and NB = 3 or 1 column blocks per CTA.
@@ -88,7 +89,11 @@ struct Bars {
     uint64_t acc_empty[kSlots];
     uint64_t la_full, la_empty;     // A_a in shared memory (read by the first product)
     uint64_t lb_full, lb_empty;     // B_a in shared memory (read by the second one)
-    uint64_t u_full, u_ready, ub_empty;
+    // U's product is done.  With one block per CTA the next item's is committed before this item's U is waited for: on
+    // one barrier a U warp that comes late for this item would find it two phases on and, by the parity, not yet done.
+    // In turn, the commit after next follows the wait for this item's U, which every U warp has passed its wait for.
+    uint64_t u_full[kUTurns];
+    uint64_t u_ready, ub_empty;
     uint64_t item_full[kRing], item_empty[kRing];
     uint64_t drain;
     uint32_t tmem_base;
@@ -253,7 +258,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         init(&bars->la_empty, 1, 1);
         init(&bars->lb_full, 1, 1);
         init(&bars->lb_empty, 1, 1);
-        init(&bars->u_full, 1, 1);
+        init(bars->u_full, kUTurns, 1);
         init(&bars->u_ready, 1, kUWarps);
         init(&bars->ub_empty, 1, 1);
         init(bars->item_full, kRing, 1);
@@ -346,7 +351,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                            idesc_two = idesc_bf16_f32(128, 256);
             bool ok = mbar_wait_relaxed(smem_u32(&bars->w_full), 0, p.poll_limit);
             int loads = 0, u_items = 0;
-            Turn q, s, acc;                                    // of the descriptors, the stages, the accumulators
+            Turn q, s, acc, u;                                 // of the descriptors, the stages, the accumulators, u_full
             bool fresh = true;                                 // the next adapter item brings a new adapter
             bool owed = false, owed_last = false, owed_new = false;   // NB = 1: the second product of the item before
             int owed_slot = 0, b_loads = 0;
@@ -400,7 +405,10 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
                 const uint32_t x_base = sX + s.at * kTileBytes;
                 const uint32_t d = tmem + (uint32_t)(NB == 3 ? 0 : acc.at * P::kSetCols);
                 product(ad ? d : d + rank16, x_base, ad ? 0 : rank16, ad ? idesc_first : idesc);
-                if (ad) mma_commit(smem_u32(&bars->u_full));
+                if (ad) {
+                    mma_commit(smem_u32(&bars->u_full[u.at]));
+                    u.next(kUTurns);
+                }
                 if (ad && it.last) mma_commit(smem_u32(&bars->la_empty));
                 if (NB == 1) {
                     mma_commit(smem_u32(&bars->a_empty[s.at]));
@@ -554,7 +562,7 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
         const int quad = warp & 3;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         int u_items = 0;
-        Turn q, set;
+        Turn q, set, full;
         for (int i = 0; i < items; ++i, q.next(kRing), set.next(NB == 3 ? 1 : p.slots)) {
             if (__any_sync(0xffffffffu, *abort_flag != 0)) break;
             if (!mbar_wait_relaxed_warp(smem_u32(&bars->item_full[q.at]), q.odd, p.poll_limit)) { raise_timeout(bars, p.status); break; }
@@ -563,12 +571,13 @@ adapter_proj_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_cons
             if (lane == 0) mbar_arrive(smem_u32(&bars->item_empty[q.at]));
             if (it.adapter < 0) continue;
             const float scale = __ldg(p.scale + it.adapter);
-            if (!mbar_wait_relaxed_warp(smem_u32(&bars->u_full), (uint32_t)u_items & 1u, p.poll_limit) ||
+            if (!mbar_wait_relaxed_warp(smem_u32(&bars->u_full[full.at]), full.odd, p.poll_limit) ||
                 !mbar_wait_relaxed_warp(smem_u32(&bars->ub_empty), ((uint32_t)u_items & 1u) ^ 1u, p.poll_limit)) {
                 raise_timeout(bars, p.status);
                 break;
             }
             ++u_items;
+            full.next(kUTurns);
             tc_fence_after();
             const uint32_t u = tmem + lanes + (uint32_t)(NB == 3 ? 0 : set.at * P::kSetCols);
             for (int c = 0; c < rank16 / 16; ++c) {            // 16 columns of U: one K step of the second product
