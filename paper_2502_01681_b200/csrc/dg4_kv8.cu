@@ -9,6 +9,8 @@
 #include "dg4_kv8_core.cuh"
 #include "dg4_launch.cuh"
 
+#include <type_traits>
+
 namespace {
 
 using namespace attn;
@@ -173,28 +175,37 @@ template <bool BF16, int LANES> struct Query {
     static constexpr int kN = 128 / LANES;
     uint32_t h[BF16 ? kN / 2 : 1];
     float f[BF16 ? 1 : kN];
-    float c;                                   // what makes a dot product with codes times `scale` a score in log2 units
+    float c;                                   // what makes a dot product with codes times the K scale a score in log2 units
+    // fp32 queries are brought down by a power of two, too, where their largest element is above 2^15 (what that takes from
+    // their small ones is below 2^-140 of the largest), so that a dot product with codes is at most 2^31 for both types.
     template <int LPH>
     __device__ __forceinline__ void set(const float* q, float scale) {
+        float top = 0.f;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) top = fmaxf(top, fabsf(q[e]));
+#pragma unroll
+        for (int o = LPH / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const uint32_t b = BF16 ? lift(top) : min(lift(top), 127u);
+        const float up = __uint_as_float(b << 23);
+        c = (BF16 ? 0.5f : 1.f) * scale * __uint_as_float((254u - b) << 23);
         if (BF16) {
-            float top = 0.f;
-#pragma unroll
-            for (int e = 0; e < kN; ++e) top = fmaxf(top, fabsf(q[e]));
-#pragma unroll
-            for (int o = LPH / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const uint32_t b = lift(top);
-            const float up = __uint_as_float(b << 23);
-            c = 0.5f * scale * __uint_as_float((254u - b) << 23);
 #pragma unroll
             for (int e = 0; e < kN / 2; ++e) {
                 const __half2 x = __floats2half2_rn(q[2 * e] * up, q[2 * e + 1] * up);
                 h[e] = *reinterpret_cast<const uint32_t*>(&x);
             }
         } else {
-            c = scale;
 #pragma unroll
-            for (int e = 0; e < kN; ++e) f[e] = q[e];
+            for (int e = 0; e < kN; ++e) f[e] = q[e] * up;
         }
+    }
+    // Score from a dot product with codes and the K scale.  Up to c = 2^96 the product with c goes first: it does not
+    // overflow (queries of 2^113 and more have a larger c).  Beyond, the product with the scale goes first: it overflows
+    // only where the score does, and what it loses to underflow is below 2^-149 c <= 2^-36 of a score.  FAR: some lane
+    // of the warp is beyond; each lane goes by its own c.
+    __device__ __forceinline__ bool is_far() const { return c > 0x1p96f; }
+    template <bool FAR> __device__ __forceinline__ float score(float dot, float k_scale) const {
+        return FAR && is_far() ? dot * k_scale * c : dot * c * k_scale;
     }
 };
 
@@ -326,17 +337,24 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
         float s[MAXN], m = -INFINITY, z = 0.f, top = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] = 0.f;
+        auto scores = [&](auto far) {
 #pragma unroll
-        for (int j = 0; j < MAXN; ++j) {
-            s[j] = -INFINITY;
-            if (j < 3 || most > 3) {
-                float dot = row[j].dot(q);
+            for (int j = 0; j < MAXN; ++j) {
+                s[j] = -INFINITY;
+                if (j < 3 || most > 3) {
+                    float dot = row[j].dot(q);
 #pragma unroll
-                for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                if (j < cnt) s[j] = dot * q.c * row[j].k_scale(row[j].pair);
+                    for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                    if (j < cnt) s[j] = q.template score<decltype(far)::value>(dot, row[j].k_scale(row[j].pair));
+                }
+                if (j == 0 && cnt <= 1) s[0] = 0.f;                           // softmax over one member: weight exactly 1
+                m = fmaxf(m, s[j]);
             }
-            if (j == 0 && cnt <= 1) s[0] = 0.f;                               // softmax over one member: weight exactly 1
-            m = fmaxf(m, s[j]);
+        };
+        scores(std::false_type());
+        if (__any_sync(0xffffffffu, q.is_far())) {
+            m = -INFINITY;
+            scores(std::true_type());
         }
 #pragma unroll
         for (int j = 0; j < MAXN; ++j) {
@@ -414,18 +432,28 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
         if (v1 >= 0) raw.load((const char*)a.Q + (int64_t)v1 * a.ldq, sub);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] = 0.f;
+        const bool far = __any_sync(0xffffffffu, q.is_far());
         int ids_next = 32 + lane < cnt ? a.nbr_idx[beg + 32 + lane] : 0;      // the chunk after `ids`
         for (int t = 0; t < cnt; t += BATCH) {
             float s[UN], lw[UN], m_new = m, mw_new = mw;
+            auto scores = [&](auto far) {
 #pragma unroll
-            for (int i = 0; i < UN; ++i) {
-                float dot = row[i].dot(q);
+                for (int i = 0; i < UN; ++i) {
+                    float dot = row[i].dot(q);
 #pragma unroll
-                for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                s[i] = t + GROUPS * i + grp < cnt ? dot * q.c * row[i].k_scale(row[i].pair) : -INFINITY;
-                if (i == 0 && cnt == 1 && grp == 0) s[0] = 0.f;               // softmax over one member: weight exactly 1
-                m_new = fmaxf(m_new, s[i]);
-                if (BF16) mw_new = fmaxf(mw_new, lw[i] = s[i] + log2_scale_v(row[i].pair));
+                    for (int o = LPH / 2; o > 0; o >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                    dot = q.template score<decltype(far)::value>(dot, row[i].k_scale(row[i].pair));
+                    s[i] = t + GROUPS * i + grp < cnt ? dot : -INFINITY;
+                    if (i == 0 && cnt == 1 && grp == 0) s[0] = 0.f;           // softmax over one member: weight exactly 1
+                    m_new = fmaxf(m_new, s[i]);
+                    if (BF16) mw_new = fmaxf(mw_new, lw[i] = s[i] + log2_scale_v(row[i].pair));
+                }
+            };
+            scores(std::false_type());
+            if (far) {
+                m_new = m;
+                mw_new = mw;
+                scores(std::true_type());
             }
             const float ref = finite(m_new), keep = fast_exp2(m - ref);       // one rescale per batch; 0 for the first
             const float ref_w = finite(mw_new), keep_w = BF16 ? fast_exp2(mw - ref_w) : keep;

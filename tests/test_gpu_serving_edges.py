@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from paper_2502_01681_b200 import dg4
-from tests.test_gpu_serving import BF16, desc, edgeless, i32, make_adapters, normal, project_ref, within
+from tests.test_gpu_serving import (BF16, attn_ref, circuit, desc, edgeless, i32, make_adapters, normal, project_ref,
+                                    table_ref, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +47,45 @@ def test_out_projection_over_thousands_of_short_requests(rank, residual):
         dg4.dg4_out_project_adapters(g, desc(residual=residual), o, w, ad, seg, res, again)
         assert torch.equal(first, again)
     assert dg4.dg4_graph_poll_status(g) == 0
+
+
+# ---------------------------------------------------------------------------------------------------
+# attention over the table
+# ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("hops,heads", [(1, 8), (2, 1), (2, 16), (3, 4), (4, 16)])
+@pytest.mark.parametrize("q_exp,k_exp", [(122, -121), (60, -60), (-118, 117)])
+def test_scores_of_ordinary_size_from_large_and_small_factors(hops, heads, dtype, q_exp, k_exp):
+    """Queries near one end of the range and keys near the other: their products are ordinary numbers."""
+    g, lists = circuit(13, 12, 150, hops)
+    n = g.n
+    q, k = normal(1, (n, 128), 2.0 ** q_exp, dtype), normal(2, (n, 128), 2.0 ** k_exp, dtype)
+    v = normal(3, (n, 128), 1.0, dtype)
+    t, o, d = torch.empty((n, 288), dtype=torch.uint8, device="cuda"), torch.empty_like(q), desc(heads, dtype)
+    dg4.dg4_kv8_write(g, d, k, v, t)
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q, t, o)
+    want, tol = attn_ref(q, *table_ref(k, v, heads)[1], lists, heads, d.scale, range(n), dtype)
+    within(o, want, tol)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("hops,heads", [(2, 8), (2, 1)])
+def test_the_largest_scores_choose_their_members(hops, heads, dtype):
+    """Scores near the top of the range: the members with the largest share the weight, whatever the distance."""
+    g, lists = circuit(14, 12, 150, hops)
+    n = g.n
+    level = torch.arange(n, device="cuda") % 7
+    k = (1.0 + level / 8.0)[:, None].expand(n, 128).to(dtype).contiguous()      # e4m3 numbers
+    q = torch.full((n, 128), 2.0 ** 117, dtype=dtype, device="cuda")            # scores of about 2^121
+    v = normal(3, (n, 128), 1.0, dtype)
+    t, o, d = torch.empty((n, 288), dtype=torch.uint8, device="cuda"), torch.empty_like(q), desc(heads, dtype)
+    dg4.dg4_kv8_write(g, d, k, v, t)
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q, t, o)
+    vals = table_ref(k, v, heads)[1][1]
+    of = level.cpu()
+    want = torch.stack([vals[u[of[u] == of[u].max()]].mean(0) for u in (torch.as_tensor(np.asarray(x, np.int64)) for x in lists)])
+    # equal weights: the sum's roundings, the weights' to fp16 (none: they are powers of two times one scale) and the output's
+    mag = torch.stack([vals[u[of[u] == of[u].max()]].abs().mean(0) for u in (torch.as_tensor(np.asarray(x, np.int64)) for x in lists)])
+    half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    rel = 2.0 ** -20 + (2.0 ** -11 if dtype == BF16 else 0.0)
+    within(o, want, rel * mag + half * (want.abs() + rel * mag) + 1e-300)
