@@ -382,9 +382,11 @@ __global__ void __launch_bounds__(256, LANES == 8 ? 2 : 3) sparse_attn_kv8_kerne
 
 // Wider cones (3 to 8 hops, lists of up to 511 members): one warp per node, its groups of LANES lanes take alternate
 // members, UN in flight each; online softmax (running maximum and sum in 32 bits) per group, merged at the end.
-// For bf16 rows the sums are measured against a running reference of their own: the largest logarithm of a weight on
-// the codes, score + log2(V scale), which is put at 14.  What its rounding does (2^-18 in the exponent) is far below that of the
-// fp16 weights.
+// For bf16 rows the sums are measured against a running reference of their own, mw: the largest logarithm of a weight on
+// the codes, which is put at 14.  These logarithms, score - m + log2(V scale), are relative to the scores' maximum m: so,
+// however large the scores are, they are numbers of a few hundred wherever a weight matters, and what their rounding does
+// (2^-17 in the exponent) is far below that of the fp16 weights.  (Against scores of 10^6 themselves an exponent would be
+// off by 2^-5.)
 // The loads run ahead of the arithmetic: the next batch of members (of this node, or the first one of the next node)
 // goes into the registers of the present one as soon as that has been added up, the member ids a chunk of 32 ahead.
 template <bool BF16, int LANES, int LPH>
@@ -435,7 +437,7 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
         const bool far = __any_sync(0xffffffffu, q.is_far());
         int ids_next = 32 + lane < cnt ? a.nbr_idx[beg + 32 + lane] : 0;      // the chunk after `ids`
         for (int t = 0; t < cnt; t += BATCH) {
-            float s[UN], lw[UN], m_new = m, mw_new = mw;
+            float s[UN], m_new = m;
             auto scores = [&](auto far) {
 #pragma unroll
                 for (int i = 0; i < UN; ++i) {
@@ -446,16 +448,21 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
                     s[i] = t + GROUPS * i + grp < cnt ? dot : -INFINITY;
                     if (i == 0 && cnt == 1 && grp == 0) s[0] = 0.f;           // softmax over one member: weight exactly 1
                     m_new = fmaxf(m_new, s[i]);
-                    if (BF16) mw_new = fmaxf(mw_new, lw[i] = s[i] + log2_scale_v(row[i].pair));
                 }
             };
             scores(std::false_type());
             if (far) {
                 m_new = m;
-                mw_new = mw;
                 scores(std::true_type());
             }
-            const float ref = finite(m_new), keep = fast_exp2(m - ref);       // one rescale per batch; 0 for the first
+            const float ref = finite(m_new), shift = m - ref, keep = fast_exp2(shift);       // one rescale per batch; 0 for the first
+            mw += shift;
+            float lw[UN], mw_new = mw;
+#pragma unroll
+            for (int i = 0; i < UN; ++i) {
+                s[i] -= ref;
+                if (BF16) mw_new = fmaxf(mw_new, lw[i] = s[i] + log2_scale_v(row[i].pair));
+            }
             const float ref_w = finite(mw_new), keep_w = BF16 ? fast_exp2(mw - ref_w) : keep;
             z *= keep;
 #pragma unroll
@@ -479,7 +486,7 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
             const bool more = same || v1 >= 0;
 #pragma unroll
             for (int i = 0; i < UN; ++i) {
-                const float p = fast_exp2(s[i] - ref);
+                const float p = fast_exp2(s[i]);
                 z += p;
                 const float w = BF16 ? fast_exp2(lw[i] - (ref_w - 14.f)) : p * scale_v(row[i].pair);
                 if (t + GROUPS * i + grp < cnt) row[i].add(w, acc);
@@ -487,18 +494,19 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
                 if (more) row[i].load(codes, exps, (uint32_t)u, a.ldt);
             }
         }
-        if (!BF16) mw = m;
         // merge the groups: maxima first, then the sums, of which each step gives one half away and keeps the other, so
         // that a lane ends with the four elements it stores (101 000 nodes, cones of five hops: 169 us; with all sums
         // exchanged at both steps 181)
-        float mm = m, mmw = mw;
+        float mm = m;
 #pragma unroll
-        for (int o = LANES; o < 32; o <<= 1) {
-            mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
-            mmw = fmaxf(mmw, __shfl_xor_sync(0xffffffffu, mmw, o));
-        }
-        const float fit = fast_exp2(mw - finite(mmw));
-        z *= fast_exp2(m - finite(mm));
+        for (int o = LANES; o < 32; o <<= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));
+        const float shift = m - finite(mm), fit_z = fast_exp2(shift);
+        mw += shift;
+        float mmw = mw;
+#pragma unroll
+        for (int o = LANES; o < 32; o <<= 1) mmw = fmaxf(mmw, __shfl_xor_sync(0xffffffffu, mmw, o));
+        const float fit = BF16 ? fast_exp2(mw - finite(mmw)) : fit_z;
+        z *= fit_z;
 #pragma unroll
         for (int o = LANES; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
 #pragma unroll
@@ -516,8 +524,8 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
                 }
             }
         }
-        // the two references differ by at most some 2^150: that power is put on in two halves
-        const float inv = fast_rcp(z), half = BF16 ? fast_exp2(0.5f * (finite(mmw) - 14.f - finite(mm))) : 1.f;
+        // what stood at 14 goes back: a power of two up to some 2^150, put on in two halves
+        const float inv = fast_rcp(z), half = BF16 ? fast_exp2(0.5f * (finite(mmw) - 14.f)) : 1.f;
         static_assert(N / GROUPS == 4, "a lane keeps four elements");
         float out[4];
 #pragma unroll

@@ -69,7 +69,7 @@ def test_scores_of_ordinary_size_from_large_and_small_factors(hops, heads, dtype
 
 
 @pytest.mark.parametrize("dtype", [BF16, torch.float32])
-@pytest.mark.parametrize("hops,heads", [(2, 8), (2, 1)])
+@pytest.mark.parametrize("hops,heads", [(2, 8), (2, 1), (3, 8)])
 def test_the_largest_scores_choose_their_members(hops, heads, dtype):
     """Scores near the top of the range: the members with the largest share the weight, whatever the distance."""
     g, lists = circuit(14, 12, 150, hops)
@@ -89,3 +89,31 @@ def test_the_largest_scores_choose_their_members(hops, heads, dtype):
     half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
     rel = 2.0 ** -20 + (2.0 ** -11 if dtype == BF16 else 0.0)
     within(o, want, rel * mag + half * (want.abs() + rel * mag) + 1e-300)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("hops,heads", [(2, 8), (3, 8), (4, 16), (5, 1)])
+@pytest.mark.parametrize("q_exp", [6, 13, 20, 60])
+def test_large_scores_cost_the_values_no_precision(q_exp, hops, heads, dtype):
+    """Scores of 10^3, 10^5, 10^7 and more, a member's values scaled by its own power of two: where a member has all the
+    weight the output is its value, however large the score is."""
+    g, lists = circuit(15, 12, 150, hops)
+    n = g.n
+    level, power = torch.arange(n, device="cuda") % 7, torch.arange(n, device="cuda") % 9 - 4
+    k = (1.0 + level / 8.0)[:, None].expand(n, 128).to(dtype).contiguous()      # e4m3 numbers
+    q = torch.full((n, 128), 2.0 ** q_exp, dtype=dtype, device="cuda")          # the dot products are exact
+    v = (normal(3, (n, 128), 1.0, torch.float32) * torch.exp2(power.float())[:, None]).to(dtype)
+    t, o, d = torch.empty((n, 288), dtype=torch.uint8, device="cuda"), torch.empty_like(q), desc(heads, dtype)
+    dg4.dg4_kv8_write(g, d, k, v, t)
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q, t, o)
+    vals = table_ref(k, v, heads)[1][1]
+    of = level.cpu()
+    best = [u[of[u] == of[u].max()] for u in (torch.as_tensor(np.asarray(x, np.int64)) for x in lists)]
+    want, mag = torch.stack([vals[u].mean(0) for u in best]), torch.stack([vals[u].abs().mean(0) for u in best])
+    # equal weights; the next member's is below 2^-40 of them (a step in k is 46 or more in log2 units, values differ by
+    # some 2^12 at most: 2^-30 in the sum).  The sum's roundings, the weights' to fp16 (bf16 rows) and the output's.
+    half = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+    rel = 2.0 ** -20 + (2.0 ** -11 if dtype == BF16 else 0.0)
+    top = torch.stack([vals[torch.as_tensor(np.asarray(x, np.int64))].abs().amax(0) for x in lists])
+    err = rel * mag + 2.0 ** -30 * top
+    within(o, want, err + half * (want.abs() + err) + 1e-300)
