@@ -163,20 +163,46 @@ struct Turn {
     }
 };
 
-__device__ __forceinline__ void walk_on(const Params& p, Walk& w) {       // to the next item, which exists
+// The last request from s on that ends at or before row `pos`, the last of all left out (s itself ends there): steps
+// twice as long each time, then halves.  Offsets that decrease give some request in that range.
+__device__ __forceinline__ int last_empty(const Params& p, int s, int pos) {
+    auto ends = [&](int64_t i) { return min(max(p.seg_ptr[i + 1], 0), p.n) <= pos; };
+    int64_t lo = s, hi = (int64_t)p.n_seg - 1;
+    for (int64_t step = 16; lo + step < hi; step *= 2) {
+        if (!ends(lo + step)) {
+            hi = lo + step;
+            break;
+        }
+        lo += step;
+    }
+    while (hi - lo > 1) {
+        const int64_t mid = (lo + hi) / 2;
+        (ends(mid) ? lo : hi) = mid;
+    }
+    return (int)lo;
+}
+
+// To the next item, which exists.  Runs of empty requests are searched through (one by one they cost 90 ns each, and the
+// other warps' waits run out over some ten million of them).
+__device__ __forceinline__ void walk_on(const Params& p, Walk& w) {
     w.lo += kTileM;
-    while (w.lo >= w.hi && w.seg + 1 < p.n_seg) {
+    for (int empty = 0; w.lo >= w.hi && w.seg + 1 < p.n_seg; ++empty) {
+        if (empty == 16) {
+            w.seg = last_empty(p, w.seg, w.hi);
+            empty = 0;
+        }
         ++w.seg;
         seg_rows(p, w.seg, w.lo, w.hi);
         w.adapter = seg_adapter(p, w.seg);
     }
+    w.lo = min(w.lo, w.hi);           // offsets that decrease: an item without rows, inside the tensor
 }
 
 // Cuts all items into one contiguous run per CTA: every thread counts the tiles of its share of the requests, the
 // CTA adds the counts up, and the thread in whose share this CTA's first item falls leaves it in shared memory.
 __device__ __forceinline__ void find_items(const Params& p, Bars* bars) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int share = (p.n_seg + kThreads - 1) / kThreads;
+    const int share = (int)(((int64_t)p.n_seg + kThreads - 1) / kThreads);
     // warp 0, which sets up the barriers and starts W on its way, takes the last share
     const int place = (warp == 0 ? kThreads : (int)threadIdx.x) - 32 + (warp == 0 ? lane : 0);
     const int64_t s0 = (int64_t)place * share;

@@ -49,6 +49,35 @@ def test_out_projection_over_thousands_of_short_requests(rank, residual):
     assert dg4.dg4_graph_poll_status(g) == 0
 
 
+@pytest.mark.parametrize("n_out", [128, 384])
+@pytest.mark.parametrize("before,between,behind", [(0, 20_000_000, 0), (0, 40, 17), (1000, 3_000_000, 5000), (15, 16, 1)])
+def test_long_runs_of_empty_requests(before, between, behind, n_out):
+    """Empty requests in front of the first row, inside one CTA's share of the items (some have rows next to them), and at
+    the end."""
+    n = 148 * 3 * 128
+    g = edgeless(n)
+    ptr = torch.cat([torch.full((k,), v, dtype=torch.int32) for k, v in
+                     ((before + 1, 0), (between + 1, 1), (30, 2), (2, 700), (behind + 1, n))]).cuda()
+    ids = torch.full((ptr.numel() - 1,), -1, dtype=torch.int32, device="cuda")
+    rows = torch.nonzero(ptr[1:] > ptr[:-1])[:, 0]               # the requests that have rows
+    ids[rows] = i32(k % 3 for k in range(len(rows)))
+    x, w, ad = normal(1, (n, 128)), normal(2, (n_out, 128), 0.1), make_adapters(3, 3, 16, n_out)
+    got, want = ([torch.full((n, 128), 7.0, dtype=BF16, device="cuda") for _ in range(n_out // 128)] for _ in range(2))
+    few = dg4.segments(torch.cat([ptr[rows], ptr[-1:]]), ids[rows].contiguous())
+
+    def call(seg, out):
+        if n_out == 128:
+            dg4.dg4_out_project_adapters(g, desc(), x, w, ad, seg, None, *out)
+        else:
+            dg4.dg4_qkv_project_adapters(g, desc(), x, w, ad, seg, *out)
+
+    call(dg4.segments(ptr, ids), got)
+    call(few, want)
+    torch.cuda.synchronize()
+    assert dg4.dg4_graph_poll_status(g) == 0
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and not any(bool((a == 7.0).all(1).any()) for a in got)
+
+
 # ---------------------------------------------------------------------------------------------------
 # attention over the table
 # ---------------------------------------------------------------------------------------------------
