@@ -81,7 +81,7 @@ class dg4_adapters(ctypes.Structure):
 
 
 _lib = None
-torch = None          # imported with the library; an import statement in every call would cost 0.4 us of some 7
+_torch_module = None
 
 
 def library_path() -> str:
@@ -90,10 +90,9 @@ def library_path() -> str:
 
 def load():
     """Loads libdg4.so (building it with nvcc if it is missing or stale).  Raises if that is impossible."""
-    global _lib, torch
+    global _lib
     if _lib is not None:
         return _lib
-    import torch
     path = _build.LIB
     if _build.needs_build():
         path = _build.build()
@@ -207,10 +206,23 @@ def _i32(a):
     return a, a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
 
 
+def _torch():
+    """torch, imported by the first call that needs it: handles are made, exported and destroyed without.  (An import
+    statement in every call would cost 0.4 us of some 7.)"""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 def _stream(stream):
     if stream is None:
-        # the raw handle, without a stream object around it: 0.4 instead of 3.6 us of a call that takes about 8
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        t = _torch_module or _torch()
+        try:               # the handle alone, not a public name: 0.4 instead of 3.6 us of a call that takes about 8
+            return t._C._cuda_getCurrentRawStream(t.cuda.current_device())
+        except AttributeError:
+            return t.cuda.current_stream().cuda_stream
     return int(getattr(stream, "cuda_stream", stream))                      # a raw handle or a torch stream
 
 
@@ -417,8 +429,9 @@ class Adapters:
 def segments(seg_ptr, seg_id) -> Segments:
     """seg_ptr [n_seg + 1] and seg_id [n_seg], CUDA int32: see dg4_segments in dg4.h."""
     load()
+    int32 = _torch().int32
     for t in (seg_ptr, seg_id):
-        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
+        if t.dtype != int32 or t.dim() != 1 or not t.is_contiguous() or not t.is_cuda:
             raise ValueError("segment arrays are contiguous one-dimensional CUDA int32 tensors")
     if seg_ptr.numel() != seg_id.numel() + 1:
         raise ValueError("seg_ptr has one entry more than seg_id")
@@ -428,6 +441,7 @@ def segments(seg_ptr, seg_id) -> Segments:
 def adapters(A, B, scale) -> Adapters:
     """A [n, rank, 128] and B [n, n_out, rank] bf16, scale [n] fp32, CUDA, contiguous: see dg4_adapters in dg4.h."""
     load()
+    torch = _torch()
     if A.dim() != 3 or B.dim() != 3 or scale.dim() != 1 or A.shape[2] != 128 or B.shape[1] not in (128, 384) \
             or B.shape[2] != A.shape[1] or not A.shape[0] == B.shape[0] == scale.shape[0]:
         raise ValueError("adapters are A [n, rank, 128], B [n, 128 or 384, rank] and scale [n]")
@@ -445,8 +459,7 @@ def _struct(x):
 def _nodes(nodes):
     if nodes is None:
         return None, 0
-    load()
-    if nodes.dtype != torch.int32 or nodes.dim() != 1 or not nodes.is_contiguous() or not nodes.is_cuda:
+    if nodes.dtype != _torch().int32 or nodes.dim() != 1 or not nodes.is_contiguous() or not nodes.is_cuda:
         raise ValueError("a node list is a contiguous one-dimensional CUDA int32 tensor")
     return _ptr(nodes), nodes.numel()
 
@@ -455,7 +468,7 @@ def _vec(t, rows=1):
     """Pointer of an fp32 vector of 128 (or of `rows` of them), or None."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
+    if t.dtype != _torch().float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
         raise ValueError("norm and gate vectors are contiguous CUDA fp32 tensors of 128 elements each")
     return _ptr(t)
 
@@ -582,7 +595,7 @@ def dg4_blocks_fwd_levelised(g: Graph, dsc: dg4_desc, H, blocks, eps, workspace,
 
 def dg4_graph_partition(g: Graph, delta: int):
     """Algorithm 1: returns (roots, group_ptr) as CUDA int32 tensors (roots trimmed to their number)."""
-    load()
+    import torch
     roots = torch.empty(g.n, dtype=torch.int32, device="cuda")
     group_ptr = torch.empty(int(g.info.n_levels) + 1, dtype=torch.int32, device="cuda")
     m = ctypes.c_int64(0)
