@@ -470,6 +470,8 @@ def _vec(t, rows=1):
         return None
     if t.dtype != _torch().float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
         raise ValueError("norm and gate vectors are contiguous CUDA fp32 tensors of 128 elements each")
+    if rows < 1:
+        raise ValueError("a gate tensor has at least one row (None: no gate)")
     return _ptr(t)
 
 

@@ -146,3 +146,18 @@ def test_large_scores_cost_the_values_no_precision(q_exp, hops, heads, dtype):
     top = torch.stack([vals[torch.as_tensor(np.asarray(x, np.int64))].abs().amax(0) for x in lists])
     err = rel * mag + 2.0 ** -30 * top
     within(o, want, err + half * (want.abs() + err) + 1e-300)
+
+
+# ---------------------------------------------------------------------------------------------------
+# what the binding refuses
+# ---------------------------------------------------------------------------------------------------
+def test_a_gate_without_rows_is_no_gate_of_ones():
+    n = 40
+    g = edgeless(n)
+    x, r2, y = normal(1, (n, 128)), torch.full((n, 128), 7.0, dtype=BF16, device="cuda"), torch.empty((n, 128), dtype=BF16, device="cuda")
+    one, seg = (torch.ones(128, device="cuda"), None), dg4.segments(i32([0, n]), i32([0]))
+    for gate in (torch.empty((0, 128), device="cuda"), torch.empty(0, device="cuda"), torch.ones((1, 120), device="cuda")):
+        with pytest.raises(ValueError):
+            dg4.dg4_norm_gate_fwd(g, desc(), x, x, 1.0, gate, seg, one, one, 1e-5, r2, y)
+    torch.cuda.synchronize()
+    assert bool((r2 == 7.0).all())
