@@ -464,6 +464,13 @@ def _nodes(nodes):
     return _ptr(nodes), nodes.numel()
 
 
+def _table(t):
+    """Pointer and row distance in bytes of an 8-bit table."""
+    if t.element_size() != 1:
+        raise ValueError("the 8-bit table is a tensor of bytes")
+    return _ptr(t), _ld(t)
+
+
 def _vec(t, rows=1):
     """Pointer of an fp32 vector of 128 (or of `rows` of them), or None."""
     if t is None:
@@ -498,7 +505,7 @@ def dg4_kv8_write(g: Graph, dsc: dg4_desc, K, V, T, nodes=None, stream=None):
     lst, count = _nodes(nodes)
     if nodes is not None and count == 0:
         return
-    _check(load().dg4_kv8_write(g.handle, ctypes.byref(dsc), _ptr(K), _ld(K), _ptr(V), _ld(V), _ptr(T), _ld(T), lst,
+    _check(load().dg4_kv8_write(g.handle, ctypes.byref(dsc), _ptr(K), _ld(K), _ptr(V), _ld(V), *_table(T), lst,
                                 count, _stream(stream)))
 
 
@@ -507,7 +514,7 @@ def dg4_kv8_read(g: Graph, dsc: dg4_desc, T, K, V, nodes=None, stream=None):
     lst, count = _nodes(nodes)
     if nodes is not None and count == 0:
         return
-    _check(load().dg4_kv8_read(g.handle, ctypes.byref(dsc), _ptr(T), _ld(T), _ptr(K), _ld(K), _ptr(V), _ld(V), lst,
+    _check(load().dg4_kv8_read(g.handle, ctypes.byref(dsc), *_table(T), _ptr(K), _ld(K), _ptr(V), _ld(V), lst,
                                count, _stream(stream)))
 
 
@@ -516,7 +523,7 @@ def dg4_sparse_attn_kv8_fwd(g: Graph, dsc: dg4_desc, Q, T, O, nodes=None, stream
     lst, count = _nodes(nodes)
     if nodes is not None and count == 0:
         return
-    _check(load().dg4_sparse_attn_kv8_fwd(g.handle, ctypes.byref(dsc), _ptr(Q), _ld(Q), _ptr(T), _ld(T), _ptr(O),
+    _check(load().dg4_sparse_attn_kv8_fwd(g.handle, ctypes.byref(dsc), _ptr(Q), _ld(Q), *_table(T), _ptr(O),
                                           _ld(O), lst, count, _stream(stream)))
 
 

@@ -161,3 +161,21 @@ def test_a_gate_without_rows_is_no_gate_of_ones():
             dg4.dg4_norm_gate_fwd(g, desc(), x, x, 1.0, gate, seg, one, one, 1e-5, r2, y)
     torch.cuda.synchronize()
     assert bool((r2 == 7.0).all())
+
+
+def test_a_table_of_wider_elements_is_refused():
+    n = 40
+    g = edgeless(n)
+    x, y = normal(1, (n, 128)), torch.empty((n, 128), dtype=BF16, device="cuda")
+    for dtype in (torch.float32, torch.int16):
+        t = torch.zeros((n, 288), dtype=dtype, device="cuda")
+        with pytest.raises(ValueError):
+            dg4.dg4_kv8_write(g, desc(), x, x, t)
+        with pytest.raises(ValueError):
+            dg4.dg4_kv8_read(g, desc(), t, y, y)
+        with pytest.raises(ValueError):
+            dg4.dg4_sparse_attn_kv8_fwd(g, desc(), x, t, y)
+    for dtype in (torch.uint8, torch.int8, torch.float8_e4m3fn):
+        t = torch.empty((n, 288), dtype=dtype, device="cuda")
+        dg4.dg4_kv8_write(g, desc(), x, x, t)
+        assert torch.equal(t.view(torch.uint8).cpu(), table_ref(x, x, 8)[0])
