@@ -5,8 +5,8 @@ import pytest
 import torch
 
 from paper_2502_01681_b200 import dg4
-from tests.test_gpu_serving import (BF16, attn_ref, circuit, desc, edgeless, i32, make_adapters, normal, project_ref,
-                                    table_ref, within)
+from tests.test_gpu_serving import (BF16, HALF, U32, attn_ref, circuit, desc, edgeless, f64, gated_ref, hard_rows, i32,
+                                    make_adapters, normal, project_ref, table_ref, vectors, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -146,6 +146,122 @@ def test_large_scores_cost_the_values_no_precision(q_exp, hops, heads, dtype):
     top = torch.stack([vals[torch.as_tensor(np.asarray(x, np.int64))].abs().amax(0) for x in lists])
     err = rel * mag + 2.0 ** -30 * top
     within(o, want, err + half * (want.abs() + err) + 1e-300)
+
+
+# ---------------------------------------------------------------------------------------------------
+# strides and alignments
+# ---------------------------------------------------------------------------------------------------
+def placed(x, ld, first, fill=7.0):
+    """A copy of x in rows `ld` apart whose first element stands at column `first` of a buffer, and the buffer."""
+    buf = torch.full((x.shape[0], ld), fill, dtype=x.dtype, device="cuda")
+    view = buf[:, first:first + 128]
+    view.copy_(x)
+    return view, buf
+
+
+@pytest.mark.parametrize("dtype,ld,first", [(torch.float32, 132, 0), (torch.float32, 136, 4), (torch.float32, 140, 8),
+                                            (torch.float32, 136, 8), (BF16, 136, 0), (BF16, 152, 8), (BF16, 384, 128)])
+@pytest.mark.parametrize("heads,n", [(8, 203), (1, 34), (16, 95)])
+def test_table_of_rows_at_any_16_byte_place(heads, n, dtype, ld, first):
+    """fp32 rows 32 bytes apart move 32 bytes at a time, others 16: the same codes and values either way."""
+    g, d = edgeless(n), desc(heads, dtype)
+    k, v = hard_rows(1, n, dtype), hard_rows(2, n, dtype).flip(0).contiguous()
+    want, vals = table_ref(k, v, heads)
+    (k2, _), (v2, _) = placed(k, ld, first), placed(v, 128, 0) if n % 2 else placed(v, ld, first)
+    t = torch.full((n, 288), 9, dtype=torch.uint8, device="cuda")
+    dg4.dg4_kv8_write(g, d, k2, v2, t)
+    assert torch.equal(t.cpu(), want)
+    (k3, kb), (v3, vb) = placed(k, ld, first), placed(v, ld, first)
+    k3.zero_(), v3.zero_()
+    dg4.dg4_kv8_read(g, d, t, k3, v3)
+    for got, val, buf in ((k3, vals[0], kb), (v3, vals[1], vb)):
+        fine = ~torch.isnan(val)
+        assert torch.equal(torch.isnan(got).cpu(), ~fine)
+        assert torch.equal(got.cpu()[fine], val.to(torch.float32).to(dtype)[fine])
+        assert bool((buf[:, :first] == 7.0).all()) and bool((buf[:, first + 128:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("hops,heads", [(1, 8), (2, 8), (2, 16), (3, 4), (4, 16)])
+def test_attention_with_strided_queries_outputs_and_table(hops, heads, dtype):
+    g, _ = circuit(16, 12, 180, hops)
+    n, d = g.n, desc(heads, dtype)
+    q, k, v = normal(1, (n, 128), 1.5, dtype), normal(2, (n, 128), 2.0, dtype), normal(3, (n, 128), 1.0, dtype)
+    t, o = torch.empty((n, 288), dtype=torch.uint8, device="cuda"), torch.empty_like(q)
+    dg4.dg4_kv8_write(g, d, k, v, t)
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q, t, o)
+    far = torch.full((n, 352), 5, dtype=torch.uint8, device="cuda")
+    far[:, 32:320] = t
+    for nodes in (None, i32([n - 1, 3, 3, 0, n // 2])):
+        (q2, _), (o2, buf) = placed(q, 160, 8), placed(torch.full_like(q, 7.0), 200, 64)
+        dg4.dg4_sparse_attn_kv8_fwd(g, d, q2, far[:, 32:320], o2, nodes)
+        on = torch.ones(n, dtype=torch.bool, device="cuda")
+        if nodes is not None:
+            on.zero_()
+            on[nodes.long()] = True
+        assert torch.equal(o2[on], o[on]) and bool((o2[~on] == 7.0).all())
+        assert bool((buf[:, :64] == 7.0).all()) and bool((buf[:, 192:] == 7.0).all())
+    q3, _ = placed(q, 160, 8)                                    # in place
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q3, t, q3)
+    assert torch.equal(q3, o)
+
+
+# ---------------------------------------------------------------------------------------------------
+# infinities and NaN through the gated norms
+# ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("rms", [False, True])
+def test_non_finite_values_follow_the_formula_and_stay_in_their_rows(rms, dtype):
+    n, rs = 300, 0.75
+    g, d = edgeless(n), desc(dtype=dtype, rms_norm=rms)
+    ptr, ids = [0, 40, 41, 44, 200, n - 20], [0, 2, 1, -1, 2]
+    s, r = normal(1, (n, 128), 3.0, dtype), normal(2, (n, 128), 2.0, dtype)
+    gate, post, pre = normal(3, (3, 128), 0.7, torch.float32), vectors(4), vectors(6)
+    seg = dg4.segments(i32(ptr), i32(ids))
+
+    def call(s, r, gate):
+        out = [torch.full((n, 128), 7.0, dtype=dtype, device="cuda") for _ in range(2)]
+        dg4.dg4_norm_gate_fwd(g, d, s, r, rs, gate, seg, post, pre, 1e-5, *out)
+        return out
+
+    clean = call(s, r, gate)
+    nan, inf = float("nan"), float("inf")
+    s2, r2, gate2 = s.clone(), r.clone(), gate.clone()
+    s2[10, 5], s2[50, 127], s2[60, 0], s2[n - 3, 4] = nan, inf, -inf, nan
+    r2[70, 64], r2[80, 1], r2[81], r2[n - 2, 3] = -inf, nan, inf, inf
+    gate2[1, 9], gate2[1, 10] = inf, nan                         # the request of rows 41 to 43
+    got = call(s2, r2, gate2)
+    hit = torch.zeros(n, dtype=torch.bool)
+    hit[[10, 50, 60, 70, 80, 81, 41, 42, 43]] = True
+    rest = ~hit.cuda()
+    for a, b in zip(got, clean):
+        assert torch.equal(a[rest], b[rest])                     # rows of no request (7.0) among them
+    gates = torch.ones((n, 128), dtype=torch.float64)
+    for lo, hi, i in zip(ptr[:-1], ptr[1:], ids):
+        gates[lo:hi] = f64(gate2)[i] if i >= 0 else 1.0
+
+    def norm(x, gamma, beta):
+        c = x if rms else x - x.mean(1, keepdim=True)
+        return c * torch.rsqrt((c * c).mean(1, keepdim=True) + 1e-5) * f64(gamma) + f64(beta)
+
+    p = norm(f64(s2), *post)
+    want_r = rs * f64(r2) + gates * p
+    want_y = norm(want_r, *pre)
+    # finite elements of these rows: some twenty roundings of terms of at most this size (the rows' values are of order
+    # one, sums over a row taken in 12 roundings), and the output's own
+    size = (rs * f64(r2)).abs() + gates.abs() * (p.abs() + f64(post[1]).abs())
+    for what, a, want, mag in (("R_out", got[0], want_r, size), ("Y", got[1], want_y, want_y.abs() + f64(pre[1]).abs())):
+        a, want, mag = f64(a)[hit], want[hit], mag[hit]
+        assert torch.equal(torch.isnan(a), torch.isnan(want)), what
+        assert torch.equal(torch.isinf(a), torch.isinf(want)) and bool((a[torch.isinf(a)] == want[torch.isinf(a)]).all()), what
+        fine = torch.isfinite(want)
+        tol = 40 * U32 * mag + HALF[dtype] * (want.abs() + 40 * U32 * mag)
+        assert bool(((a - want).abs()[fine] <= tol[fine]).all()), what
+    # the rows that were not hit are those of the formula
+    seen, (wr, tr), (wy, ty) = gated_ref(s, r, rs, gate, ptr, ids, post, pre, 1e-5, rms, dtype)
+    on = seen & ~hit
+    within(got[0][on.cuda()], wr[on], tr[on], "R_out")
+    within(got[1][on.cuda()], wy[on], ty[on], "Y")
 
 
 # ---------------------------------------------------------------------------------------------------
