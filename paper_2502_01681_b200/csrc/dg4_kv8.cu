@@ -199,11 +199,11 @@ template <bool BF16, int LANES> struct Query {
             for (int e = 0; e < kN; ++e) f[e] = q[e] * up;
         }
     }
-    // Score from a dot product with codes and the K scale.  Up to c = 2^96 the product with c goes first: it does not
+    // Score from a dot product with codes and the K scale.  Up to |c| = 2^96 the product with c goes first: it does not
     // overflow (queries of 2^113 and more have a larger c).  Beyond, the product with the scale goes first: it overflows
     // only where the score does, and what it loses to underflow is below 2^-149 c <= 2^-36 of a score.  FAR: some lane
     // of the warp is beyond; each lane goes by its own c.
-    __device__ __forceinline__ bool is_far() const { return c > 0x1p96f; }
+    __device__ __forceinline__ bool is_far() const { return fabsf(c) > 0x1p96f; }
     template <bool FAR> __device__ __forceinline__ float score(float dot, float k_scale) const {
         return FAR && is_far() ? dot * k_scale * c : dot * c * k_scale;
     }

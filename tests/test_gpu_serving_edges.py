@@ -98,6 +98,20 @@ def test_scores_of_ordinary_size_from_large_and_small_factors(hops, heads, dtype
 
 
 @pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("hops,heads", [(2, 8), (2, 16), (3, 4)])
+@pytest.mark.parametrize("q_exp,k_exp", [(122, -121), (2, -1)])
+def test_a_negative_scale_is_that_of_the_negated_queries(q_exp, k_exp, hops, heads, dtype):
+    g, _ = circuit(13, 12, 150, hops)
+    n = g.n
+    q, k, v = (normal(i, (n, 128), 2.0 ** e, dtype) for i, e in ((1, q_exp), (2, k_exp), (3, 0)))
+    t, o, o2, d = torch.empty((n, 288), dtype=torch.uint8, device="cuda"), torch.empty_like(q), torch.empty_like(q), desc(heads, dtype)
+    dg4.dg4_kv8_write(g, d, k, v, t)
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, -q, t, o)
+    dg4.dg4_sparse_attn_kv8_fwd(g, dg4.desc(heads, d.dtype, -d.scale), q, t, o2)
+    assert bool(torch.isfinite(o).all()) and torch.equal(o, o2)  # signs are exact
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
 @pytest.mark.parametrize("hops,heads", [(2, 8), (2, 1), (3, 8)])
 def test_the_largest_scores_choose_their_members(hops, heads, dtype):
     """Scores near the top of the range: the members with the largest share the weight, whatever the distance."""
