@@ -470,7 +470,8 @@ dg4_status dg4_out_project_adapters(const dg4_graph* g, const dg4_desc* desc, co
  * A slice that holds an infinity or a NaN is stored as NaN throughout (b = 255, codes 0x7f).  heads <= 16.
  *
  * dg4_kv8_write: rows of K and V into the table.  dg4_kv8_read: the values the table stands for into rows of K and V
- * (exact in fp32; in bf16 too unless they fall below its normal range).
+ * (exact in fp32; in bf16 too unless they fall below its normal range.  Magnitudes above 1.9375 * 2^127 round to 2^128,
+ * which reads back as infinity).
  *   T      device, [n, ldt] bytes, 32-byte aligned; ldt a multiple of 32, 288 .. 2^31 - 1.  Must not
  *          overlap K or V
  *   K, V   device, [n, d] of desc->dtype
@@ -484,8 +485,13 @@ dg4_status dg4_kv8_read(const dg4_graph* g, const dg4_desc* desc, const void* T,
                         void* V, int64_t ldv, const int32_t* nodes, int32_t count, void* stream);
 
 /*
- * dg4_sparse_attn_fwd over the 8-bit table: the same formula with K and V the values the table stands for, fp32
- * arithmetic, O rounded once.  For all nodes (nodes NULL) or for a list of them (a level, a single node); list,
+ * dg4_sparse_attn_fwd over the 8-bit table: the same formula with K and V the values the table stands for.  Scores,
+ * the softmax's maximum and sum, and the weighted sums are held in fp32; O is rounded once.  fp32 rows: query and weights
+ * are held in fp32 too.  bf16 rows: both go into the products in fp16.  A head's query is scaled by a power of two for that:
+ * it is exact down to 2^-25 of its largest magnitude and off by at most 2^-40 of that below.  A weight is rounded to
+ * nearest, off by at most 2^-11 of itself (where it is small, by 2^-39 of the head's largest product of weight and V
+ * scale), an eighth of O's own rounding; the softmax's sum is taken before that.  A score overflows only where it is itself
+ * out of fp32's range.  For all nodes (nodes NULL) or for a list of them (a level, a single node); list,
  * table and heads as above, cones of any depth.  O may be Q when there is no list (same leading dimension), and
  * must not overlap T.
  */
