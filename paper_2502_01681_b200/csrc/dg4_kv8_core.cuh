@@ -26,15 +26,6 @@ constexpr int kEl = 8;                        // elements of K (and of V) per la
 
 // 8 consecutive elements of a bf16 or fp32 row
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* row, int sub, float* f) {
-    if (BF16) {
-        attn::Elem<true>::unpack(attn::ld_piece_stream((const char*)row + sub * 16), f);
-    } else {
-        attn::Elem<false>::unpack(attn::ld_piece_stream((const char*)row + sub * 32), f);
-        attn::Elem<false>::unpack(attn::ld_piece_stream((const char*)row + sub * 32 + 16), f + 4);
-    }
-}
-template <bool BF16>
 __device__ __forceinline__ void store8(void* row, int sub, const float* f) {
     if (BF16) {
         attn::st_piece_stream((char*)row + sub * 16, attn::Elem<true>::pack(f));
