@@ -490,8 +490,8 @@ dg4_status dg4_kv8_read(const dg4_graph* g, const dg4_desc* desc, const void* T,
  * are held in fp32 too.  bf16 rows: both go into the products in fp16.  A head's query is scaled by a power of two for that:
  * it is exact down to 2^-25 of its largest magnitude and off by at most 2^-40 of that below.  A weight is rounded to
  * nearest, off by at most 2^-11 of itself (where it is small, by 2^-39 of the head's largest product of weight and V
- * scale), an eighth of O's own rounding; the softmax's sum is taken before that.  A score overflows only where it is itself
- * out of fp32's range.  For all nodes (nodes NULL) or for a list of them (a level, a single node); list,
+ * scale), an eighth of O's own rounding; the softmax's sum is taken before that.  For scales
+ * up to 2^14 a score overflows only where it is itself out of fp32's range.  For all nodes (nodes NULL) or for a list of them (a level, a single node); list,
  * table and heads as above, cones of any depth.  O may be Q when there is no list (same leading dimension), and
  * must not overlap T.
  */
@@ -507,7 +507,8 @@ dg4_status dg4_sparse_attn_kv8_fwd(const dg4_graph* g, const dg4_desc* desc, con
  * DG4_FLAG_RMS_NORM x / sqrt(mean(x^2) + eps) * gamma + beta.  fp32 arithmetic; Y is computed from R_out before that
  * is rounded; each output is rounded once.
  *   S, R, R_out, Y  device, [n, d] of desc->dtype.  Y may be NULL (R_out only; pre_gamma and pre_beta are then
- *                   ignored).  R_out and Y may each be S or R (same leading dimension), but not one another
+ *                   ignored).  R_out and Y may each be S or R (same leading dimension), but not one another.
+ *                   Rows of no request are read too (their outputs stay as they are)
  *   gate            device, [n_gates, d] fp32 or NULL (ones)
  *   segments        NULL: all rows use gate 0 (n_gates must be 1)
  *   gammas, betas   device, [d] fp32, 16-byte aligned; betas may be NULL (zeros)

@@ -23,12 +23,13 @@
 // SM, so that each fetches a third of W and has one block's epilogue.
 //
 // Bound by HBM, and under sustained load by power: a QKV row is 256 bytes in, 768 out, and 98 + r kflop.  1.01M rows,
-// rank 16, 200 requests: 189 us = 5.5 TB/s (85 % of the measured copy rate; the plain projection takes 185), sustained
-// 195 us, the SM clock falling from 1.97 to 1.5 GHz at 1 kW.  That is why the waits are suspended ones and the products
+// rank 16, 200 requests: 190 us = 5.5 TB/s (84 % of the measured copy rate; the plain projection takes 185) in short runs,
+// sustained 195 us, the SM clock falling from 1.97 to 1.5 GHz at 1 kW.  That is why the waits are suspended ones and the products
 // few and wide: a product of N columns reads the same 128 rows of X from shared memory whatever N is, so U apart and
-// three blocks apart (36 instructions of N <= 128 per item instead of 19) took 219 us.  Rank 64: 240 us, one X stage
+// three blocks apart (36 instructions of N <= 128 per item instead of 19) took 219 us.  Rank 64: 237 us (sustained 248), one X stage
 // beside W_qkv (rows stored from registers, without staging, made room for two and took 400).  Output projection with
-// residual, rank 64: 130 us = 6.0 TB/s, sustained 137.  64 requests of one row each: 7.4 us a call, 2 048 of them 36.
+// residual, rank 64: 129 us = 6.0 TB/s, sustained 131 to 137.  64 requests of one row each: 7.6 us on the device, 9.4 us a
+// call through the binding; 512 of them 14, 2 048 of them 37 on the device.
 //
 // Every mbarrier wait is bounded.  On expiry the kernel records DG4_ERR_TIMEOUT and raises an abort flag; every warp
 // leaves at its next item at the latest, without meeting others.  Then the producer waits for the copies it has started,

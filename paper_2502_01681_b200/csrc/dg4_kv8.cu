@@ -2,7 +2,8 @@
 //
 // Writing and reading are bound by HBM: 16 lanes per row (two rows per warp), 8 elements of K and of V per lane (see
 // dg4_kv8_core.cuh for the row); each row passes through registers once, 512 + 288 bytes in bf16.  1.01M rows written
-// and read back: 278 us, 5.8 TB/s (90 % of the measured copy rate); 250 007 fp32 rows: 111 us.
+// and read back: 276 us in short runs, 280 sustained, 5.8 TB/s (89 % of the measured copy rate); 250 007 fp32 rows: 111
+// and 114 us.
 // The attention gathers 288 bytes per member instead of 512 and is bound by instructions (see there).
 
 #include "dg4_internal.h"
@@ -297,8 +298,8 @@ __device__ __forceinline__ void store_row(void* row, int sub, const float* f) {
 // across the GPU are a contiguous range.  A member beyond a node's own list weighs zero (its filler is the node's own
 // row, so no value enters that the node does not read anyway).  The scores come in two runs without a branch inside, the
 // first three members and the others, so that their chains of dependent instructions overlap; the sums skip what lies
-// beyond the longest list of the warp (1.01M two-hop cones: 216 us, under sustained load 248; with a branch at every
-// member 244, with none 229 and 262).
+// beyond the longest list of the warp (1.01M two-hop cones: 216 us, under sustained load 243; with a branch at every
+// member 244, with none 229 and 262; fp32 rows 291 and 332).
 // The loads run ahead of the arithmetic: lists two nodes ahead, and a member's row of the next node goes into the
 // registers of this node's as soon as that has been added up.
 template <bool BF16, int LANES, int LPH, int MAXN>
@@ -495,8 +496,8 @@ __global__ void __launch_bounds__(256, 2) sparse_attn_kv8_wide_kernel(AttnArgs a
             }
         }
         // merge the groups: maxima first, then the sums, of which each step gives one half away and keeps the other, so
-        // that a lane ends with the four elements it stores (101 000 nodes, cones of five hops: 169 us; with all sums
-        // exchanged at both steps 181)
+        // that a lane ends with the four elements it stores (101 000 nodes, cones of five hops: 168 us, fp32
+        // rows 190; with all sums exchanged at both steps 181)
         float mm = m;
 #pragma unroll
         for (int o = LANES; o < 32; o <<= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, o));

@@ -2,7 +2,8 @@
 //     R' = res_scale * R + gate * Norm_post(S),      Y = Norm_pre(R'),
 // S the sub-layer's output, R the residual stream, the gate a vector per request.  Everything between the two loads
 // and the two stores of a row stays in registers in 32 bits (Y is computed from the unrounded R'), so a bf16 row
-// costs 512 bytes in and 512 out, which is the bound: 1.01M rows in 164 us, 6.3 TB/s (98 % of the measured copy rate).
+// costs 512 bytes in and 512 out, which is the bound: 1.01M rows in 164 us in short runs,
+// sustained 167 us, 6.2 TB/s (96 % of the measured copy rate); fp32 rows 334 us (96 %).
 //
 // 8 lanes per row, 16 elements per lane, four consecutive rows per warp: each sum over a row takes 3 shuffles for four
 // rows at once, and the arithmetic runs on pairs (packed fp32 instructions).  The norm vectors lie in shared memory in
