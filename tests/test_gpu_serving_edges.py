@@ -78,6 +78,34 @@ def test_long_runs_of_empty_requests(before, between, behind, n_out):
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and not any(bool((a == 7.0).all(1).any()) for a in got)
 
 
+@pytest.mark.parametrize("count", [40, 700, 5000])
+@pytest.mark.parametrize("seed", range(4))
+def test_many_unsorted_offsets_stay_inside_the_tensors(seed, count):
+    """Which rows are written is then unspecified, but nothing outside is, and no wait runs out."""
+    rng = np.random.default_rng(seed)
+    n = 900
+    spread = [(0, n), (-50, n + 50), (-2 ** 31, 2 ** 31 - 1), (n - 3, n + 3)][seed]
+    ptr = rng.integers(*spread, size=count + 1)
+    ptr[rng.random(count + 1) < 0.4] = ptr[0]                    # runs of equal ones among them
+    seg = dg4.segments(i32(ptr.tolist()), i32(rng.integers(-2, 5, size=count).tolist()))
+    g = edgeless(n)
+    x, res = normal(1, (n, 128)), normal(4, (n, 128))
+    for rank in (16, 64):
+        buf = torch.full((n + 512, 512), 3.0, dtype=BF16, device="cuda")
+        out = [buf[256:256 + n, 128 * j:128 * (j + 1)] for j in range(4)]
+        dg4.dg4_qkv_project_adapters(g, desc(), x, normal(2, (384, 128), 0.1), make_adapters(3, 3, rank, 384), seg, *out[:3])
+        dg4.dg4_out_project_adapters(g, desc(residual=True), x, normal(2, (128, 128), 0.1), make_adapters(3, 3, rank, 128), seg, res, out[3])
+        torch.cuda.synchronize()
+        assert bool((buf[:256] == 3.0).all()) and bool((buf[256 + n:] == 3.0).all())
+    buf = torch.full((n + 512, 256), 3.0, dtype=BF16, device="cuda")
+    one = (torch.ones(128, device="cuda"), None)
+    dg4.dg4_norm_gate_fwd(g, desc(), x, res, 1.0, normal(5, (3, 128), 0.7, torch.float32), seg, one, one, 1e-5,
+                          buf[256:256 + n, :128], buf[256:256 + n, 128:])
+    torch.cuda.synchronize()
+    assert bool((buf[:256] == 3.0).all()) and bool((buf[256 + n:] == 3.0).all())
+    assert dg4.dg4_graph_poll_status(g) == 0
+
+
 # ---------------------------------------------------------------------------------------------------
 # attention over the table
 # ---------------------------------------------------------------------------------------------------
@@ -160,6 +188,32 @@ def test_large_scores_cost_the_values_no_precision(q_exp, hops, heads, dtype):
     top = torch.stack([vals[torch.as_tensor(np.asarray(x, np.int64))].abs().amax(0) for x in lists])
     err = rel * mag + 2.0 ** -30 * top
     within(o, want, err + half * (want.abs() + err) + 1e-300)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("hops", [2, 4])
+def test_a_poisoned_query_reaches_its_own_head_only(hops, bad, dtype):
+    """Every score of that head is not a number or infinite, so the head is not a number; a node that is its own only
+    member takes its values whatever its query holds."""
+    g, lists = circuit(8, 10, 200, hops)
+    n, d = g.n, desc(8, dtype)
+    q, k, v = normal(1, (n, 128), 1.0, dtype), normal(2, (n, 128), 1.0, dtype), normal(3, (n, 128), 1.0, dtype)
+    t, o, o2 = torch.empty((n, 288), dtype=torch.uint8, device="cuda"), torch.empty_like(q), torch.empty_like(q)
+    dg4.dg4_kv8_write(g, d, k, v, t)
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q, t, o)
+    hit = {3: 0, 60: 20, 61: 127, n - 1: 64}                     # node 3 is an input
+    for node, at in hit.items():
+        q[node, at] = bad
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q, t, o2)
+    assert len(lists[3]) == 1
+    for node in range(n):
+        for h in range(8):
+            at = slice(16 * h, 16 * h + 16)
+            if node in hit and hit[node] // 16 == h and len(lists[node]) > 1:
+                assert bool(torch.isnan(o2[node, at]).all()), (node, h)
+            else:
+                assert torch.equal(o[node, at], o2[node, at]), (node, h)
 
 
 # ---------------------------------------------------------------------------------------------------
