@@ -126,6 +126,23 @@ def test_scores_of_ordinary_size_from_large_and_small_factors(hops, heads, dtype
 
 
 @pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("hops,heads", [(1, 8), (2, 8), (2, 1), (3, 4), (4, 16)])
+@pytest.mark.parametrize("v_exp,spread", [(115, 0), (-110, 0), (0, 40), (0, 110)])
+def test_values_of_any_size(v_exp, spread, hops, heads, dtype):
+    """Values near both ends of the range, and members' values that lie many binades apart."""
+    g, lists = circuit(17, 12, 150, hops)
+    n = g.n
+    q, k = normal(1, (n, 128), 1.0, dtype), normal(2, (n, 128), 1.0, dtype)
+    power = v_exp + (torch.arange(n, device="cuda") * 7 % (2 * spread + 1) - spread)
+    v = (normal(3, (n, 128), 1.0, torch.float32) * torch.exp2(power.float())[:, None]).to(dtype)
+    t, o, d = torch.empty((n, 288), dtype=torch.uint8, device="cuda"), torch.empty_like(q), desc(heads, dtype)
+    dg4.dg4_kv8_write(g, d, k, v, t)
+    dg4.dg4_sparse_attn_kv8_fwd(g, d, q, t, o)
+    want, tol = attn_ref(q, *table_ref(k, v, heads)[1], lists, heads, d.scale, range(n), dtype)
+    within(o, want, tol + 2.0 ** -132)                           # below 2^-126 a bf16 number's step is 2^-133, an fp32 one's finer
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
 @pytest.mark.parametrize("hops,heads", [(2, 8), (2, 16), (3, 4)])
 @pytest.mark.parametrize("q_exp,k_exp", [(122, -121), (2, -1)])
 def test_a_negative_scale_is_that_of_the_negated_queries(q_exp, k_exp, hops, heads, dtype):
