@@ -520,6 +520,75 @@ dg4_status dg4_norm_gate_fwd(const dg4_graph* g, const dg4_desc* desc, const voi
                              void* Y, int64_t ldy, void* stream);
 
 /*
+ * ---- Training the feed-forward half of a block --------------------------------------------------------------------
+ *
+ * The gated feed-forward sub-layer and the norm of a residual sum, each with its backward pass.  Pre-norm they are used as
+ *     N = Norm(H),  H' = H + GLU(N)            dN = GLU_bwd(dH'),  dH = dH' + Norm_bwd(dN)
+ * and post-norm as  Z = H + GLU(H),  H' = Norm(Z).  (Sec. 3.5 keeps the Transformer block around the restricted attention;
+ * a gated sub-layer in the place of its feed-forward one has no counterpart in the paper.)  The calls take all rows of the
+ * handle (an edgeless one will do), enqueue on `stream`, allocate nothing, keep nothing between calls and can be captured;
+ * calls on different streams are independent if their workspaces are different ones.  Gradients are overwritten, not added
+ * to; sums over rows are taken in a fixed order, so equal calls on one device give equal bits.
+ */
+typedef enum {
+    DG4_ACT_SILU = 0,          /* x / (1 + exp(-x))                                                           */
+    DG4_ACT_GELU = 1,          /* x / 2 * (1 + tanh(sqrt(2 / pi) * (x + 0.044715 x^3)))                        */
+    DG4_ACT_RELU = 2           /* max(0, x); derivative 0 at 0                                                 */
+} dg4_activation;
+
+/*
+ * Y = (act(X W_gate^T) * (X W_up^T)) W_down^T  (+ H_res if desc->flags has DG4_FLAG_RESIDUAL and H_res != NULL).
+ *   X               device, [n, d] bf16
+ *   W_gate, W_up    device, [d_ff, d] bf16 row-major, contiguous;   W_down   device, [d, d_ff] bf16, contiguous
+ *   d_ff            a multiple of 8, 8 .. 8192
+ *   Y               device, [n, d] bf16; may be X or H_res (same leading dimension)
+ * fp32 accumulation and activations; the d_ff hidden values of a row are rounded to bf16 between the two products and never
+ * written to global memory; Y is rounded once.  A row's values (infinities and NaNs too) reach its own row of Y only.
+ *
+ * dg4_glu_bwd: the gradients for dY = dL/dY (of the sum without H_res, whose own gradient is dY):
+ *   dX                        device, [n, d] bf16 or NULL; without the weights' gradients it may be X or dY (same leading
+ *                             dimension)
+ *   dW_gate, dW_up, dW_down   device, bf16, shaped as the weights, contiguous; all three NULL (frozen weights) or none
+ *   workspace                 device, dg4_glu_bwd_workspace_bytes() bytes (0 for few rows: NULL then), 16-byte aligned;
+ *                             only the weights' gradients need it
+ * The activations are computed again from X.  The hidden gradients are rounded to bf16 between the products; the weights'
+ * gradients are sums over all rows in fp32, rounded once.
+ * Errors: INVALID_ARG, UNSUPPORTED (dtype other than bf16; d_ff; activation), CUDA; a device-side wait that runs out
+ * records DG4_ERR_TIMEOUT in the handle's status word.
+ */
+dg4_status dg4_glu_fwd(const dg4_graph* g, const dg4_desc* desc, const void* X, int64_t ldx, const void* W_gate,
+                       const void* W_up, const void* W_down, int32_t d_ff, int32_t activation, const void* H_res,
+                       int64_t ldh, void* Y, int64_t ldy, void* stream);
+size_t dg4_glu_bwd_workspace_bytes(const dg4_graph* g, const dg4_desc* desc, int32_t d_ff);
+dg4_status dg4_glu_bwd(const dg4_graph* g, const dg4_desc* desc, const void* X, int64_t ldx, const void* W_gate,
+                       const void* W_up, const void* W_down, int32_t d_ff, int32_t activation, const void* dY, int64_t lddy,
+                       void* dX, int64_t lddx, void* dW_gate, void* dW_up, void* dW_down, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * Z = X + R,   Y = Norm(Z):  layer normalisation, or with DG4_FLAG_RMS_NORM division by the root mean square (as in
+ * dg4_norm_gate_fwd), with gamma and beta.  Y is computed from Z before that is rounded; each output is rounded once.
+ *   X, R    device, [n, d] of desc->dtype; R may be NULL (Z = X)
+ *   Z, Y    device, [n, d] of desc->dtype; Z may be NULL.  Each may be X or R (same leading dimension), but not one another
+ *   gamma   device, [d] fp32, 16-byte aligned; beta likewise or NULL (zeros)
+ *
+ * dg4_norm_bwd: the gradients of Y = Norm(Z) for dY = dL/dY, mean and variance taken from Z again:
+ *   dZ             device, [n, d] of desc->dtype or NULL: D_res + the norm's gradient (D_res the gradient that Z has by
+ *                  another way, the residual's; NULL: zeros).  dZ may be Z, dY or D_res (same leading dimension)
+ *   dgamma, dbeta  device, [d] fp32, 16-byte aligned, each may be NULL
+ *   workspace      device, dg4_norm_bwd_workspace_bytes() bytes (0 for few rows: NULL then), 16-byte aligned; only dgamma
+ *                  and dbeta need it
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+dg4_status dg4_add_norm_fwd(const dg4_graph* g, const dg4_desc* desc, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                            const float* gamma, const float* beta, float eps, void* Z, int64_t ldz, void* Y, int64_t ldy,
+                            void* stream);
+size_t dg4_norm_bwd_workspace_bytes(const dg4_graph* g, const dg4_desc* desc);
+dg4_status dg4_norm_bwd(const dg4_graph* g, const dg4_desc* desc, const void* Z, int64_t ldz, const float* gamma, float eps,
+                        const void* dY, int64_t lddy, const void* D_res, int64_t lddr, void* dZ, int64_t lddz, float* dgamma,
+                        float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Diagnostic (the paper has no counterpart): launches one small CTA that waits, with the same bounded wait the
  * pipelines of this library use, on a barrier nothing ever arrives on.  The wait gives up after its poll limit
  * (about a second) and the kernel writes DG4_ERR_TIMEOUT to *device_status (device int32) and returns normally:

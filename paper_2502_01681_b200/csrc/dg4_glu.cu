@@ -1,0 +1,948 @@
+// The gated feed-forward sub-layer  Y = (act(X Wg^T) * (X Wu^T)) Wd^T (+ R)  and its gradients.
+//
+// Hidden units are taken 64 at a time (a block).  G and U of a block are one product of 128 columns, for Wg's and Wu's
+// rows stand one behind the other in shared memory; the activations are formed in registers, rounded to bf16 and go back
+// into tensor memory as the A operand of the next product, so no hidden value reaches global memory in any direction.
+//
+// glu_fwd_kernel    per 128-row tile, per block:  G|U = X [Wg; Wu]^T,   Y += (act(G) * U) Wd^T
+// glu_dx_kernel     per 128-row tile, per block:  G|U again, dA = dY Wd,   dX += dG Wg + dU Wu
+//                   with  dU = dA act(G),  dG = dA U act'(G)
+// glu_dw_kernel     a CTA keeps one block and walks the row tiles:  G|U, dA again,   [dWg | dWu]^T += X^T [dG | dU],
+//                   dWd += dY^T (act(G) * U),   accumulated in tensor memory (192 columns of fp32)
+// glu_reduce_kernel sums the accumulators of the CTAs that share a block, in a fixed order
+//
+// Wg and Wu, 128 bytes of a row at a time, serve as K-major operands of the first products and, the same bytes read
+// MN-major, of dX; Wd likewise.  X and dY tiles likewise in glu_dw_kernel.  Nothing is transposed in memory.
+
+#include <cuda.h>
+
+#include <atomic>
+
+#include "dg4_internal.h"
+#include "dg4_sm100.cuh"
+
+using namespace sm100;
+
+namespace {
+
+constexpr int kTileM = 128;
+constexpr int kBlock = 64;                         // hidden units at a time
+constexpr int kHalfBytes = kTileM * 128;           // 64 columns of a 128-row tile
+constexpr int kTileBytes = 2 * kHalfBytes;
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr int kSmemLimit = 232448;                 // what one CTA may hold
+constexpr int kMaxDff = 8192;                      // at most as many blocks as SMs (glu_dw_kernel)
+
+// A place in a ring of n and the parity of its present round.
+struct Turn {
+    int at = 0;
+    uint32_t odd = 0;
+    __device__ __forceinline__ void next(int n) {
+        if (++at == n) { at = 0; odd ^= 1u; }
+    }
+};
+
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, const uint32_t* r) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ void ld_global_v4(const void* p, uint32_t* r) {
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p) : "memory");
+}
+__device__ __forceinline__ void st_global_v4(void* p, const uint32_t* r) {
+    asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t pk;
+    asm("cvt.rn.bf16x2.f32 %0, %2, %1;" : "=r"(pk) : "f"(lo), "f"(hi));
+    return pk;
+}
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// SiLU x * sigmoid(x), GELU by its tanh form x * sigmoid(2 sqrt(2/pi) (x + 0.044715 x^3)), ReLU max(0, x).
+constexpr float kLog2e = 1.4426950408889634f, kGelu1 = 1.5957691216057308f, kGelu3 = 0.07135481282052f;
+template <int ACT>
+__device__ __forceinline__ float sigmoid_of(float g) {
+    if (ACT == DG4_ACT_SILU) return rcp(1.f + ex2(-kLog2e * g));
+    return rcp(1.f + ex2(g * (-kLog2e * kGelu1 - kLog2e * kGelu3 * (g * g))));
+}
+template <int ACT>
+__device__ __forceinline__ float act_of(float g) {
+    if (ACT == DG4_ACT_RELU) return fmaxf(g, 0.f);
+    return g * sigmoid_of<ACT>(g);
+}
+// act(g), and act'(g) = s + g s (1 - s) p'(g) with s = sigmoid(p(g))
+template <int ACT>
+__device__ __forceinline__ void act_both(float g, float& a, float& da) {
+    if (ACT == DG4_ACT_RELU) {
+        a = fmaxf(g, 0.f);
+        da = g > 0.f ? 1.f : 0.f;
+        return;
+    }
+    const float s = sigmoid_of<ACT>(g);
+    a = g * s;
+    // beyond |g| = 1000 the factor 1 - s or s is zero: p' is kept finite there
+    const float dp = ACT == DG4_ACT_SILU ? 1.f : kGelu1 + 3.f * kGelu3 * fminf(g * g, 1e6f);
+    da = fmaf(a * (1.f - s), dp, s);
+}
+
+struct Params {
+    int32_t n, d_ff, n_tiles, n_blocks;
+    const __nv_bfloat16* R; int64_t ldr;     // forward: nullable residual
+    __nv_bfloat16* out; int64_t ldo;         // backward: dX
+    int32_t* status;
+    uint32_t poll_limit;
+};
+
+template <class Bars>
+__device__ __forceinline__ void raise_timeout(Bars* bars, int32_t* status) {
+    atomicExch(&bars->abort_flag, 1u);
+    if (status) atomicCAS(status, 0, (int)DG4_ERR_TIMEOUT);
+}
+
+// One block's Wg and Wu: two panels of 64 inputs, each 64 rows of Wg and 64 of Wu.
+__device__ __forceinline__ void load_gu(const CUtensorMap* wg, const CUtensorMap* wu, uint32_t dst, int block, uint32_t bar) {
+    for (int h = 0; h < 2; ++h) {
+        tma_load_2d(dst + h * kHalfBytes, wg, h * 64, block * kBlock, bar);
+        tma_load_2d(dst + h * kHalfBytes + kBlock * 128, wu, h * 64, block * kBlock, bar);
+    }
+}
+__device__ __forceinline__ void load_tile(const CUtensorMap* map, uint32_t dst, int row0, uint32_t bar) {
+    for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kHalfBytes, map, h * 64, row0, bar);
+}
+// d = A B^T over 128 inputs, both K-major in two panels of 64
+__device__ __forceinline__ void product_128(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+        const uint32_t off = (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32);
+        mma_bf16(d, smem_desc_sw128(a + off), smem_desc_sw128(b + off), idesc, ks > 0 ? 1u : 0u);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------------------------------
+// Tensor memory: Y in columns 0..127, three G|U buffers behind it, so that the products of two blocks run ahead of the
+// epilogue of a third.  The activations of a block overwrite its G: 16 columns from G's 0 and from G's 32 on.
+namespace fwd {
+constexpr int kStages = 3, kBufs = 3;
+constexpr int kOffGu = 2 * kTileBytes, kOffD = kOffGu + kStages * kTileBytes, kOffBars = kOffD + kStages * kHalfBytes;
+struct Bars {
+    uint64_t x_full[2], x_empty[2];
+    uint64_t gu_full[kStages], gu_empty[kStages], d_full[kStages], d_empty[kStages];
+    uint64_t acc_full[kBufs], a_ready[kBufs];
+    uint64_t y_full, y_empty, drain;
+    uint32_t tmem_base, abort_flag;
+};
+constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;        // 1024: the base is aligned by hand
+static_assert(kSmem <= kSmemLimit, "shared memory");
+}  // namespace fwd
+
+template <int ACT>
+__global__ void __launch_bounds__(kThreads, 1)
+glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_wg,
+               const __grid_constant__ CUtensorMap map_wu, const __grid_constant__ CUtensorMap map_wd,
+               const __grid_constant__ CUtensorMap map_y, Params p) {
+    using namespace fwd;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nb = p.n_blocks;
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    auto bar = [](const uint64_t& b) { return smem_u32(&b); };
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), kEpiWarps); }
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(bar(bars->gu_full[i]), 1); mbar_init(bar(bars->gu_empty[i]), 1);
+            mbar_init(bar(bars->d_full[i]), 1); mbar_init(bar(bars->d_empty[i]), 1);
+        }
+        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kEpiWarps); }
+        mbar_init(bar(bars->y_full), 1); mbar_init(bar(bars->y_empty), kEpiWarps); mbar_init(bar(bars->drain), 1);
+        bars->abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_wg); tma_prefetch_desc(&map_wu);
+        tma_prefetch_desc(&map_wd); tma_prefetch_desc(&map_y);
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;
+    const int tiles = (p.n_tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    const uint32_t limit = p.poll_limit;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ producer
+        if (lane == 0) {
+            Turn x, w;
+            int armed_x = 0, armed_gu = 0, armed_d = 0;
+            bool ok = true;
+            for (int t = 0; t < tiles && ok; ++t, x.next(2)) {
+                ok = t < 2 || mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit);
+                if (!ok) break;
+                mbar_expect_tx(bar(bars->x_full[x.at]), kTileBytes);
+                load_tile(&map_x, base + x.at * kTileBytes, ((int)blockIdx.x + t * (int)gridDim.x) * kTileM, bar(bars->x_full[x.at]));
+                ++armed_x;
+                for (int b = 0; b < nb && ok; ++b, w.next(kStages)) {
+                    ok = !*abort_flag && (armed_gu < kStages || mbar_wait_relaxed(bar(bars->gu_empty[w.at]), w.odd ^ 1u, limit));
+                    if (!ok) break;
+                    mbar_expect_tx(bar(bars->gu_full[w.at]), kTileBytes);
+                    load_gu(&map_wg, &map_wu, base + kOffGu + w.at * kTileBytes, b, bar(bars->gu_full[w.at]));
+                    ++armed_gu;
+                    ok = armed_d < kStages || mbar_wait_relaxed(bar(bars->d_empty[w.at]), w.odd ^ 1u, limit);
+                    if (!ok) break;
+                    mbar_expect_tx(bar(bars->d_full[w.at]), kHalfBytes);
+                    tma_load_2d(base + kOffD + w.at * kHalfBytes, &map_wd, b * kBlock, 0, bar(bars->d_full[w.at]));
+                    ++armed_d;
+                }
+            }
+            if (!ok) raise_timeout(bars, p.status);
+            // leave with no copy still landing in shared memory (these waits keep the default limit)
+            for (int i = max(0, armed_x - 2); i < armed_x; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
+            for (int i = max(0, armed_gu - kStages); i < armed_gu; ++i) mbar_wait(bar(bars->gu_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+            for (int i = max(0, armed_d - kStages); i < armed_d; ++i) mbar_wait(bar(bars->d_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            const uint32_t idesc = idesc_bf16_f32(128, 128);
+            const int total = tiles * nb;
+            Turn x, gu, d, buf1, buf2;
+            int b1 = 0, b2 = 0;                          // blocks within their tiles
+            uint32_t y_odd = 1;
+            bool ok = true;
+            // First products run two blocks ahead of second ones.  (One where a tile is one block: the tile two further on
+            // takes the place of X that this tile's epilogue leaves, which comes after this tile's second product.)
+            const int ahead = nb == 1 ? 1 : 2;
+            for (int c = 0; c < total + ahead && ok; ++c) {
+                if (c < total) {
+                    if (b1 == 0) ok = mbar_wait_relaxed(bar(bars->x_full[x.at]), x.odd, limit);
+                    ok = ok && !*abort_flag && mbar_wait_relaxed(bar(bars->gu_full[gu.at]), gu.odd, limit);
+                    if (!ok) break;
+                    tc_fence_after();
+                    product_128(tmem + 128 + buf1.at * 128, base + x.at * kTileBytes, base + kOffGu + gu.at * kTileBytes, idesc);
+                    mma_commit(bar(bars->acc_full[buf1.at]));
+                    mma_commit(bar(bars->gu_empty[gu.at]));
+                    gu.next(kStages); buf1.next(kBufs);
+                    if (++b1 == nb) { b1 = 0; x.next(2); }
+                }
+                if (c >= ahead) {
+                    ok = mbar_wait_relaxed(bar(bars->d_full[d.at]), d.odd, limit) && mbar_wait_relaxed(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                    if (ok && b2 == 0) { ok = mbar_wait_relaxed(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int steps = min(4, (p.d_ff - b2 * kBlock + 15) / 16);
+                    for (int ks = 0; ks < steps; ++ks)
+                        mma_bf16_ta(tmem, tmem + 128 + buf2.at * 128 + (ks >> 1) * 32 + (ks & 1) * 8,
+                                    smem_desc_sw128(base + kOffD + d.at * kHalfBytes + ks * 32), idesc, (b2 | ks) ? 1u : 0u);
+                    mma_commit(bar(bars->d_empty[d.at]));
+                    d.next(kStages); buf2.next(kBufs);
+                    if (++b2 == nb) { b2 = 0; mma_commit(bar(bars->y_full)); }
+                }
+            }
+            if (!ok) raise_timeout(bars, p.status);
+            mma_commit(bar(bars->drain));                // tensor memory is freed below: every product must be done
+            mbar_wait(bar(bars->drain), 0);
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue
+        const int quad = warp & 3, half = (warp - 2) >> 2;           // 32 rows, and which half of a block's (or Y's) columns
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        Turn x, buf;
+        uint32_t y_odd = 0;
+        bool ok = true, stored = false;
+        for (int t = 0; t < tiles && ok; ++t, x.next(2)) {
+            const int row0 = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM + quad * 32;
+            for (int b = 0; b < nb; ++b, buf.next(kBufs)) {
+                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * 128 + half * 32);
+                uint32_t g[32], u[32], a[16];
+                tmem_ld_32x32(at, g);
+                tmem_ld_32x32(at + 64, u);
+                tmem_ld_wait();
+                const int valid = p.d_ff - b * kBlock - half * 32;   // hidden units past the last: zero
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float lo = act_of<ACT>(__uint_as_float(g[2 * i])) * __uint_as_float(u[2 * i]);
+                    const float hi = act_of<ACT>(__uint_as_float(g[2 * i + 1])) * __uint_as_float(u[2 * i + 1]);
+                    a[i] = pack_bf16(lo, hi);
+                }
+                if (valid < 32) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) if (2 * i >= valid) a[i] = 0u;
+                }
+                tmem_st_32x8(at, a);
+                tmem_st_32x8(at + 8, a + 8);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(bars->a_ready[buf.at]));
+                    if (stored && b == 0) {                          // the tile before has left its staging rows
+                        bulk_wait_read0();
+                        mbar_arrive(bar(bars->x_empty[x.at ^ 1]));
+                    }
+                }
+            }
+            if (!ok) break;
+            uint32_t r[32];
+            const bool res = p.R != nullptr && row0 + lane < p.n;
+            if (res) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + half * 64 + i * 8, r + 4 * i);
+            }
+            ok = mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit);
+            if (!ok) break;
+            y_odd ^= 1u;
+            tc_fence_after();
+            uint32_t y[64];
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64), y);
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64 + 32), y + 32);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(bars->y_empty));
+            // Y's products are done, so X's are: its place stages the rows
+            const uint32_t stage = base + x.at * kTileBytes + half * kHalfBytes + quad * 4096;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float lo = __uint_as_float(y[8 * i + 2 * e]), hi = __uint_as_float(y[8 * i + 2 * e + 1]);
+                    if (res) {
+                        lo += __uint_as_float(r[4 * i + e] << 16);
+                        hi += __uint_as_float(r[4 * i + e] & 0xffff0000u);
+                    }
+                    o[e] = pack_bf16(lo, hi);
+                }
+                st_shared_v4(stage + sw128_offset(lane, i), o);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && row0 < p.n) {
+                tma_store_2d(&map_y, half * 64, row0, stage);
+                bulk_commit();
+            }
+            stored = true;
+        }
+        if (!ok) raise_timeout(bars, p.status);
+        if (lane == 0) bulk_wait_all();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// backward: dX
+// ---------------------------------------------------------------------------------------------------
+// Tensor memory: dX in columns 0..127, two buffers of G | U | dA behind it.  dG overwrites G, dU overwrites U (16 columns
+// from 0 and from 32 on of each).
+namespace dx {
+constexpr int kStages = 3, kBufs = 2, kBufCols = 192;
+constexpr int kStageBytes = kTileBytes + kHalfBytes;              // Wg and Wu, then Wd
+constexpr int kOffW = 2 * kTileBytes, kOffBars = kOffW + kStages * kStageBytes;
+struct Bars {
+    uint64_t x_full, x_empty;
+    uint64_t w_full[kStages], w_empty[kStages];
+    uint64_t acc_full[kBufs], a_ready[kBufs];
+    uint64_t y_full, y_empty, drain;
+    uint32_t tmem_base, abort_flag;
+};
+constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;
+static_assert(kSmem <= kSmemLimit, "shared memory");
+}  // namespace dx
+
+template <int ACT>
+__global__ void __launch_bounds__(kThreads, 1)
+glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_dy,
+              const __grid_constant__ CUtensorMap map_wg, const __grid_constant__ CUtensorMap map_wu,
+              const __grid_constant__ CUtensorMap map_wd, Params p) {
+    using namespace dx;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int nb = p.n_blocks;
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    auto bar = [](const uint64_t& b) { return smem_u32(&b); };
+
+    if (threadIdx.x == 0) {
+        mbar_init(bar(bars->x_full), 1); mbar_init(bar(bars->x_empty), 1);
+        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); }
+        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kEpiWarps); }
+        mbar_init(bar(bars->y_full), 1); mbar_init(bar(bars->y_empty), kEpiWarps); mbar_init(bar(bars->drain), 1);
+        bars->abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy); tma_prefetch_desc(&map_wg); tma_prefetch_desc(&map_wu);
+        tma_prefetch_desc(&map_wd);
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;
+    const int tiles = (p.n_tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    const uint32_t limit = p.poll_limit;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ producer
+        if (lane == 0) {
+            Turn w;
+            uint32_t x_odd = 1;
+            int armed_x = 0, armed_w = 0;
+            bool ok = true;
+            for (int t = 0; t < tiles && ok; ++t, x_odd ^= 1u) {
+                ok = mbar_wait_relaxed(bar(bars->x_empty), x_odd, limit);
+                if (!ok) break;
+                const int row0 = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM;
+                mbar_expect_tx(bar(bars->x_full), 2 * kTileBytes);
+                load_tile(&map_x, base, row0, bar(bars->x_full));
+                load_tile(&map_dy, base + kTileBytes, row0, bar(bars->x_full));
+                ++armed_x;
+                for (int b = 0; b < nb && ok; ++b, w.next(kStages)) {
+                    ok = !*abort_flag && (armed_w < kStages || mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit));
+                    if (!ok) break;
+                    const uint32_t dst = base + kOffW + w.at * kStageBytes;
+                    mbar_expect_tx(bar(bars->w_full[w.at]), kStageBytes);
+                    load_gu(&map_wg, &map_wu, dst, b, bar(bars->w_full[w.at]));
+                    tma_load_2d(dst + kTileBytes, &map_wd, b * kBlock, 0, bar(bars->w_full[w.at]));
+                    ++armed_w;
+                }
+            }
+            if (!ok) raise_timeout(bars, p.status);
+            if (armed_x > 0) mbar_wait(bar(bars->x_full), (uint32_t)(armed_x - 1) & 1u);
+            for (int i = max(0, armed_w - kStages); i < armed_w; ++i) mbar_wait(bar(bars->w_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
+                           id_dx = idesc_bf16_f32(128, 128) | kIdescBMn;
+            const int total = tiles * nb;
+            Turn w1, w2, buf1, buf2;
+            int b1 = 0, b2 = 0;
+            uint32_t x_odd = 0, y_odd = 1;
+            bool ok = true;
+            for (int c = 0; c < total + 1 && ok; ++c) {
+                if (c < total) {
+                    if (b1 == 0) { ok = mbar_wait_relaxed(bar(bars->x_full), x_odd, limit); x_odd ^= 1u; }
+                    ok = ok && !*abort_flag && mbar_wait_relaxed(bar(bars->w_full[w1.at]), w1.odd, limit);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t w = base + kOffW + w1.at * kStageBytes, d = tmem + 128 + buf1.at * kBufCols;
+                    product_128(d, base, w, id_gu);
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)                   // dA = dY Wd: Wd's rows run along K
+                        mma_bf16(d + 128, smem_desc_sw128(base + kTileBytes + (ks >> 2) * kHalfBytes + (ks & 3) * 32),
+                                 smem_desc_sw128_mn(w + kTileBytes + ks * 2048, kHalfBytes), id_da, ks > 0 ? 1u : 0u);
+                    mma_commit(bar(bars->acc_full[buf1.at]));
+                    w1.next(kStages); buf1.next(kBufs);
+                    if (++b1 == nb) { b1 = 0; mma_commit(bar(bars->x_empty)); }
+                }
+                if (c >= 1) {
+                    ok = mbar_wait_relaxed(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                    if (ok && b2 == 0) { ok = mbar_wait_relaxed(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t w = base + kOffW + w2.at * kStageBytes, a = tmem + 128 + buf2.at * kBufCols;
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)                   // dX += [dG | dU] [Wg; Wu]: their rows run along K
+                        mma_bf16_ta(tmem, a + (ks >> 1) * 32 + (ks & 1) * 8, smem_desc_sw128_mn(w + ks * 2048, kHalfBytes), id_dx, (b2 | ks) ? 1u : 0u);
+                    mma_commit(bar(bars->w_empty[w2.at]));
+                    w2.next(kStages); buf2.next(kBufs);
+                    if (++b2 == nb) { b2 = 0; mma_commit(bar(bars->y_full)); }
+                }
+            }
+            if (!ok) raise_timeout(bars, p.status);
+            mma_commit(bar(bars->drain));
+            mbar_wait(bar(bars->drain), 0);
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        Turn buf;
+        uint32_t y_odd = 0;
+        bool ok = true;
+        for (int t = 0; t < tiles && ok; ++t) {
+            const int row = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM + quad * 32 + lane;
+            for (int b = 0; b < nb; ++b, buf.next(kBufs)) {
+                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * kBufCols + half * 32);
+                uint32_t g[32], u[32], h[32];
+                tmem_ld_32x32(at, g);
+                tmem_ld_32x32(at + 64, u);
+                tmem_ld_32x32(at + 128, h);
+                tmem_ld_wait();
+                const int valid = p.d_ff - b * kBlock - half * 32;
+                uint32_t dg[16], du[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float vg[2], vu[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float dh = __uint_as_float(h[2 * i + e]);
+                        float a, da;
+                        act_both<ACT>(__uint_as_float(g[2 * i + e]), a, da);
+                        vu[e] = dh * a;
+                        vg[e] = dh * __uint_as_float(u[2 * i + e]) * da;
+                    }
+                    dg[i] = pack_bf16(vg[0], vg[1]);
+                    du[i] = pack_bf16(vu[0], vu[1]);
+                }
+                if (valid < 32) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) if (2 * i >= valid) dg[i] = du[i] = 0u;
+                }
+                tmem_st_32x8(at, dg);
+                tmem_st_32x8(at + 8, dg + 8);
+                tmem_st_32x8(at + 64, du);
+                tmem_st_32x8(at + 72, du + 8);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(bars->a_ready[buf.at]));
+            }
+            if (!ok) break;
+            ok = mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit);
+            if (!ok) break;
+            y_odd ^= 1u;
+            tc_fence_after();
+            uint32_t y[64];
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64), y);
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64 + 32), y + 32);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(bars->y_empty));
+            if (row < p.n) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
+                    st_global_v4(p.out + (int64_t)row * p.ldo + half * 64 + i * 8, o);
+                }
+            }
+            __syncwarp();
+        }
+        if (!ok) raise_timeout(bars, p.status);
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// backward: the weights
+// ---------------------------------------------------------------------------------------------------
+// Tensor memory: [dWg | dWu]^T in columns 0..127 (lane = input, column = hidden unit of the block), dWd in 128..191 (lane =
+// output, column = hidden unit), G | U | dA in 192..383.  The epilogue takes its 96 values into registers at once, and the
+// next tile's first products run while it computes.
+// Shared memory: the block's weights, two stages of X and dY, and the bf16 values dG | dU | act(G) U as MN-major operands.
+namespace dw {
+constexpr int kStages = 2;
+constexpr int kOffX = kTileBytes + kHalfBytes, kOffA = kOffX + kStages * 2 * kTileBytes, kOffBars = kOffA + 3 * kHalfBytes;
+constexpr int kPart = 3 * kBlock * 128;            // fp32 values of a CTA's accumulators: dWg, dWu, dWd^T, [unit][128] each
+struct Bars {
+    uint64_t w_full, x_full[kStages], x_empty[kStages];
+    uint64_t acc_full, acc_empty, a_full, a_empty, w_done;
+    uint64_t drain;
+    uint32_t tmem_base, abort_flag;
+};
+constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;
+static_assert(kSmem <= kSmemLimit, "shared memory");
+}  // namespace dw
+
+struct DwOut {
+    float* part;                                   // [groups][blocks][kPart], or null: one group, straight to bf16
+    __nv_bfloat16 *wg, *wu, *wd;
+};
+
+template <int ACT>
+__global__ void __launch_bounds__(kThreads, 1)
+glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_dy,
+              const __grid_constant__ CUtensorMap map_wg, const __grid_constant__ CUtensorMap map_wu,
+              const __grid_constant__ CUtensorMap map_wd, Params p, DwOut out) {
+    using namespace dw;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int block = blockIdx.x, group = blockIdx.y, groups = gridDim.y;
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    auto bar = [](const uint64_t& b) { return smem_u32(&b); };
+
+    if (threadIdx.x == 0) {
+        mbar_init(bar(bars->w_full), 1);
+        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), 1); }
+        mbar_init(bar(bars->acc_full), 1); mbar_init(bar(bars->acc_empty), kEpiWarps);
+        mbar_init(bar(bars->a_full), kEpiWarps); mbar_init(bar(bars->a_empty), 1);
+        mbar_init(bar(bars->w_done), 1); mbar_init(bar(bars->drain), 1);
+        bars->abort_flag = 0;
+        mbar_fence_init();
+        tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy);
+    }
+    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;
+    const int tiles = (p.n_tiles - group + groups - 1) / groups;     // at least one: groups <= n_tiles
+    const uint32_t limit = p.poll_limit;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ producer
+        if (lane == 0) {
+            mbar_expect_tx(bar(bars->w_full), kTileBytes + kHalfBytes);
+            load_gu(&map_wg, &map_wu, base, block, bar(bars->w_full));
+            tma_load_2d(base + kTileBytes, &map_wd, block * kBlock, 0, bar(bars->w_full));
+            Turn x;
+            int armed = 0;
+            bool ok = true;
+            for (int t = 0; t < tiles && ok; ++t, x.next(kStages)) {
+                ok = !*abort_flag && (t < kStages || mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit));
+                if (!ok) break;
+                const uint32_t dst = base + kOffX + x.at * 2 * kTileBytes;
+                const int row0 = (group + t * groups) * kTileM;
+                mbar_expect_tx(bar(bars->x_full[x.at]), 2 * kTileBytes);
+                load_tile(&map_x, dst, row0, bar(bars->x_full[x.at]));
+                load_tile(&map_dy, dst + kTileBytes, row0, bar(bars->x_full[x.at]));
+                ++armed;
+            }
+            if (!ok) raise_timeout(bars, p.status);
+            mbar_wait(bar(bars->w_full), 0);
+            for (int i = max(0, armed - kStages); i < armed; ++i) mbar_wait(bar(bars->x_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0) {
+            const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
+                           id_w = idesc_bf16_f32(128, 128) | kIdescAMn | kIdescBMn, id_wd = idesc_bf16_f32(128, 64) | kIdescAMn | kIdescBMn;
+            Turn x1, x2;
+            uint32_t acc_odd = 1, a_odd = 0, polls = 0;
+            bool ok = mbar_wait_relaxed(bar(bars->w_full), 0, limit);
+            // Whichever can go first: the next tile's first products (its rows have come, the epilogue has taken its
+            // values) or this tile's second ones.  With a fixed order the tensor cores would wait for rows that can only
+            // come when second products have left a stage.
+            for (int t1 = 0, t2 = 0; t2 < tiles && ok;) {
+                if (t1 < tiles && mbar_test(bar(bars->x_full[x1.at]), x1.odd) && mbar_test(bar(bars->acc_empty), acc_odd)) {
+                    acc_odd ^= 1u;
+                    tc_fence_after();
+                    const uint32_t x = base + kOffX + x1.at * 2 * kTileBytes, d = tmem + 192;
+                    product_128(d, x, base, id_gu);
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)
+                        mma_bf16(d + 128, smem_desc_sw128(x + kTileBytes + (ks >> 2) * kHalfBytes + (ks & 3) * 32),
+                                 smem_desc_sw128_mn(base + kTileBytes + ks * 2048, kHalfBytes), id_da, ks > 0 ? 1u : 0u);
+                    mma_commit(bar(bars->acc_full));
+                    x1.next(kStages);
+                    ++t1;
+                    polls = 0;
+                } else if (t2 < t1 && mbar_test(bar(bars->a_full), a_odd)) {
+                    a_odd ^= 1u;
+                    tc_fence_after();
+                    const uint32_t x = base + kOffX + x2.at * 2 * kTileBytes, a = base + kOffA;
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks) {                 // sixteen rows at a time
+                        mma_bf16(tmem, smem_desc_sw128_mn(x + ks * 2048, kHalfBytes), smem_desc_sw128_mn(a + ks * 2048, kHalfBytes), id_w, t2 > 0 || ks > 0 ? 1u : 0u);
+                        mma_bf16(tmem + 128, smem_desc_sw128_mn(x + kTileBytes + ks * 2048, kHalfBytes),
+                                 smem_desc_sw128_mn(a + 2 * kHalfBytes + ks * 2048, kHalfBytes), id_wd, t2 > 0 || ks > 0 ? 1u : 0u);
+                    }
+                    mma_commit(bar(bars->a_empty));
+                    mma_commit(bar(bars->x_empty[x2.at]));
+                    x2.next(kStages);
+                    ++t2;
+                    polls = 0;
+                } else {
+                    ok = !*abort_flag && ++polls <= limit;
+                    if (polls > 64) __nanosleep(40);
+                }
+            }
+            if (ok) mma_commit(bar(bars->w_done));
+            else raise_timeout(bars, p.status);
+            mma_commit(bar(bars->drain));
+            mbar_wait(bar(bars->drain), 0);
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue
+        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const int valid = p.d_ff - block * kBlock - half * 32;       // hidden units of this warp's 32 that exist
+        uint32_t odd = 0;
+        bool ok = true;
+        for (int t = 0; t < tiles && ok; ++t, odd ^= 1u) {
+            const bool in = (group + t * groups) * kTileM + quad * 32 + lane < p.n;
+            ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full), odd, limit);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t at = tmem + lanes + (uint32_t)(192 + half * 32);
+            uint32_t g[32], u[32], h[32];
+            tmem_ld_32x32(at, g);
+            tmem_ld_32x32(at + 64, u);
+            tmem_ld_32x32(at + 128, h);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(bars->acc_empty));
+            ok = mbar_wait_relaxed_warp(bar(bars->a_empty), odd ^ 1u, limit);
+            if (!ok) break;
+            // a row past the last (its X and dY read as zero) and a unit past the last add nothing, whatever the weights
+            // hold: 0 * infinity would
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t v[3][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float vg[2], vu[2], va[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int k = 8 * c + 2 * i + e;
+                        const float dh = __uint_as_float(h[k]), uu = __uint_as_float(u[k]);
+                        float a, da;
+                        act_both<ACT>(__uint_as_float(g[k]), a, da);
+                        vu[e] = dh * a;
+                        vg[e] = dh * uu * da;
+                        va[e] = a * uu;
+                    }
+                    const bool keep = in && 8 * c + 2 * i < valid;
+                    v[0][i] = keep ? pack_bf16(vg[0], vg[1]) : 0u;
+                    v[1][i] = keep ? pack_bf16(vu[0], vu[1]) : 0u;
+                    v[2][i] = keep ? pack_bf16(va[0], va[1]) : 0u;
+                }
+                const uint32_t off = base + kOffA + sw128_offset(quad * 32 + lane, half * 4 + c);
+#pragma unroll
+                for (int m = 0; m < 3; ++m) st_shared_v4(off + m * kHalfBytes, v[m]);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(bars->a_full));
+        }
+        ok = ok && mbar_wait_relaxed_warp(bar(bars->w_done), 0, limit);
+        if (ok) {
+            tc_fence_after();
+            const int col = quad * 32 + lane;                        // an input (dWg, dWu) or an output (dWd)
+            float* part = out.part ? out.part + ((int64_t)group * gridDim.x + block) * kPart : nullptr;
+#pragma unroll 1
+            for (int m = 0; m < 3; ++m) {
+                uint32_t w[32];
+                tmem_ld_32x32(tmem + lanes + (uint32_t)(m * 64 + half * 32), w);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    const float f = __uint_as_float(w[i]);
+                    const int unit = block * kBlock + half * 32 + i;
+                    if (part) part[(m * kBlock + half * 32 + i) * 128 + col] = f;
+                    else if (i < valid) {
+                        if (m == 2) out.wd[(int64_t)col * p.d_ff + unit] = __float2bfloat16(f);
+                        else (m == 0 ? out.wg : out.wu)[(int64_t)unit * 128 + col] = __float2bfloat16(f);
+                    }
+                }
+            }
+            tc_fence_before();
+        } else {
+            raise_timeout(bars, p.status);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// One CTA per hidden unit and matrix, one thread per input or output: the groups' sums in the order of the groups.
+__global__ void glu_reduce_kernel(DwOut out, int d_ff, int n_blocks, int groups) {
+    const int unit = blockIdx.x, m = blockIdx.y, col = threadIdx.x;
+    const float* src = out.part + (int64_t)(unit / kBlock) * dw::kPart + (m * kBlock + unit % kBlock) * 128 + col;
+    float f = 0.f;
+    for (int g = 0; g < groups; ++g) f += src[(int64_t)g * n_blocks * dw::kPart];
+    if (m == 2) out.wd[(int64_t)col * d_ff + unit] = __float2bfloat16(f);
+    else (m == 0 ? out.wg : out.wu)[(int64_t)unit * 128 + col] = __float2bfloat16(f);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------------------
+#define CHECK(expr) do { dg4_status _s = (expr); if (_s != DG4_OK) return _s; } while (0)
+
+dg4_status sm_count(int dev, int* out) {
+    static std::atomic<int> known[64];
+    if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
+    int sms = known[dev].load(std::memory_order_relaxed);
+    if (sms == 0) {
+        DG4_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        known[dev].store(sms, std::memory_order_relaxed);
+    }
+    *out = sms;
+    return DG4_OK;
+}
+
+// the opt-in to more than 48 KB of shared memory, once per kernel and device
+template <auto kKernel>
+dg4_status allow_smem(int dev, int bytes) {
+    static std::atomic<bool> done[64];
+    if (dev < 0 || dev >= 64) DG4_FAIL(DG4_ERR_UNSUPPORTED, "device ordinal %d is out of range", dev);
+    if (!done[dev].load(std::memory_order_relaxed)) {
+        DG4_CUDA_TRY(cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        done[dev].store(true, std::memory_order_relaxed);
+    }
+    return DG4_OK;
+}
+
+struct Maps { CUtensorMap x, dy, wg, wu, wd, y; };
+
+int blocks_of(int d_ff) { return (d_ff + kBlock - 1) / kBlock; }
+// Row groups of glu_dw_kernel: as many as the device has SMs for, and no more than there are tiles.
+int groups_of(const dg4_graph* g, int d_ff, int sms) {
+    const int tiles = (int)(((int64_t)g->n + kTileM - 1) / kTileM), most = sms / blocks_of(d_ff);
+    return tiles < most ? tiles : (most > 0 ? most : 1);
+}
+
+dg4_status check_weights(const void* wg, const void* wu, const void* wd, int32_t d_ff, int32_t act) {
+    if (act != DG4_ACT_SILU && act != DG4_ACT_GELU && act != DG4_ACT_RELU) DG4_FAIL(DG4_ERR_UNSUPPORTED, "unknown activation %d", act);
+    if (d_ff < 8 || d_ff > kMaxDff || d_ff % 8 != 0) DG4_FAIL(DG4_ERR_UNSUPPORTED, "d_ff = %d: must be a multiple of 8 up to %d", d_ff, kMaxDff);
+    CHECK(dg4i_check_tensor("W_gate", wg, 128, 2, 128));
+    CHECK(dg4i_check_tensor("W_up", wu, 128, 2, 128));
+    CHECK(dg4i_check_tensor("W_down", wd, d_ff, 2, d_ff));
+    return DG4_OK;
+}
+
+dg4_status weight_maps(Maps* m, const void* wg, const void* wu, const void* wd, int d_ff) {
+    CHECK(dg4i_make_row_map(&m->wg, wg, d_ff, 128, kBlock));
+    CHECK(dg4i_make_row_map(&m->wu, wu, d_ff, 128, kBlock));
+    CHECK(dg4i_make_map(&m->wd, wd, d_ff, 128, d_ff, 128, 64));
+    return DG4_OK;
+}
+
+template <int ACT>
+dg4_status launch_fwd(const Maps& m, const Params& p, int dev, int sms, cudaStream_t st) {
+    CHECK(allow_smem<glu_fwd_kernel<ACT>>(dev, fwd::kSmem));
+    glu_fwd_kernel<ACT><<<p.n_tiles < sms ? p.n_tiles : sms, kThreads, fwd::kSmem, st>>>(m.x, m.wg, m.wu, m.wd, m.y, p);
+    dg4i_count_launch();
+    DG4_CUDA_TRY(cudaGetLastError());
+    return DG4_OK;
+}
+
+template <int ACT>
+dg4_status launch_bwd(const Maps& m, const Params& p, const DwOut& out, int groups, int dev, int sms, cudaStream_t st) {
+    if (p.out) {
+        CHECK(allow_smem<glu_dx_kernel<ACT>>(dev, dx::kSmem));
+        glu_dx_kernel<ACT><<<p.n_tiles < sms ? p.n_tiles : sms, kThreads, dx::kSmem, st>>>(m.x, m.dy, m.wg, m.wu, m.wd, p);
+        dg4i_count_launch();
+        DG4_CUDA_TRY(cudaGetLastError());
+    }
+    if (out.wg) {
+        CHECK(allow_smem<glu_dw_kernel<ACT>>(dev, dw::kSmem));
+        glu_dw_kernel<ACT><<<dim3(p.n_blocks, groups), kThreads, dw::kSmem, st>>>(m.x, m.dy, m.wg, m.wu, m.wd, p, out);
+        dg4i_count_launch();
+        DG4_CUDA_TRY(cudaGetLastError());
+        if (out.part) {
+            glu_reduce_kernel<<<dim3(p.d_ff, 3), 128, 0, st>>>(out, p.d_ff, p.n_blocks, groups);
+            dg4i_count_launch();
+            DG4_CUDA_TRY(cudaGetLastError());
+        }
+    }
+    return DG4_OK;
+}
+
+Params make_params(const dg4_graph* g, int d_ff) {
+    Params p = {};
+    p.n = g->n; p.d_ff = d_ff; p.n_blocks = blocks_of(d_ff);
+    p.n_tiles = (int)(((int64_t)g->n + kTileM - 1) / kTileM);
+    p.status = g->dev_status; p.poll_limit = dg4i_poll_limit();
+    return p;
+}
+
+}  // namespace
+
+extern "C" dg4_status dg4_glu_fwd(const dg4_graph* g, const dg4_desc* desc, const void* X, int64_t ldx, const void* W_gate,
+                                  const void* W_up, const void* W_down, int32_t d_ff, int32_t activation, const void* H_res,
+                                  int64_t ldh, void* Y, int64_t ldy, void* stream) {
+    CHECK(dg4i_check_device(g));
+    CHECK(dg4i_check_desc(desc, true));
+    CHECK(dg4i_check_tensor("X", X, ldx, 2, 128));
+    CHECK(check_weights(W_gate, W_up, W_down, d_ff, activation));
+    const bool res = (desc->flags & DG4_FLAG_RESIDUAL) && H_res;
+    if (res) CHECK(dg4i_check_tensor("H_res", H_res, ldh, 2, 128));
+    CHECK(dg4i_check_tensor("Y", Y, ldy, 2, 128));
+    int sms;
+    CHECK(sm_count(g->device, &sms));
+    Maps m;
+    CHECK(weight_maps(&m, W_gate, W_up, W_down, d_ff));
+    CHECK(dg4i_make_row_map(&m.x, X, g->n, ldx, kTileM));
+    CHECK(dg4i_make_row_map(&m.y, Y, g->n, ldy, 32));
+    Params p = make_params(g, d_ff);
+    p.R = res ? (const __nv_bfloat16*)H_res : nullptr; p.ldr = ldh;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (activation == DG4_ACT_SILU) return launch_fwd<DG4_ACT_SILU>(m, p, g->device, sms, st);
+    if (activation == DG4_ACT_GELU) return launch_fwd<DG4_ACT_GELU>(m, p, g->device, sms, st);
+    return launch_fwd<DG4_ACT_RELU>(m, p, g->device, sms, st);
+}
+
+extern "C" size_t dg4_glu_bwd_workspace_bytes(const dg4_graph* g, const dg4_desc* desc, int32_t d_ff) {
+    int sms;
+    if (!g || dg4i_check_desc(desc, true) != DG4_OK || d_ff < 8 || d_ff > kMaxDff || sm_count(g->device, &sms) != DG4_OK) return 0;
+    const int groups = groups_of(g, d_ff, sms);
+    return groups > 1 ? (size_t)groups * blocks_of(d_ff) * dw::kPart * sizeof(float) : 0;
+}
+
+extern "C" dg4_status dg4_glu_bwd(const dg4_graph* g, const dg4_desc* desc, const void* X, int64_t ldx, const void* W_gate,
+                                  const void* W_up, const void* W_down, int32_t d_ff, int32_t activation, const void* dY,
+                                  int64_t lddy, void* dX, int64_t lddx, void* dW_gate, void* dW_up, void* dW_down,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+    CHECK(dg4i_check_device(g));
+    CHECK(dg4i_check_desc(desc, true));
+    CHECK(dg4i_check_tensor("X", X, ldx, 2, 128));
+    CHECK(check_weights(W_gate, W_up, W_down, d_ff, activation));
+    CHECK(dg4i_check_tensor("dY", dY, lddy, 2, 128));
+    if (dX) CHECK(dg4i_check_tensor("dX", dX, lddx, 2, 128));
+    const bool weights = dW_gate || dW_up || dW_down;
+    if (!dX && !weights) DG4_FAIL(DG4_ERR_INVALID_ARG, "neither dX nor the weights' gradients are asked for");
+    int sms;
+    CHECK(sm_count(g->device, &sms));
+    DwOut out = {};
+    const int groups = groups_of(g, d_ff, sms);
+    if (weights) {
+        CHECK(dg4i_check_tensor("dW_gate", dW_gate, 128, 2, 128));
+        CHECK(dg4i_check_tensor("dW_up", dW_up, 128, 2, 128));
+        CHECK(dg4i_check_tensor("dW_down", dW_down, d_ff, 2, d_ff));
+        // dX's kernel is done with X and dY before the weights' kernel reads them again
+        if (dX && (dX == X || dX == dY)) DG4_FAIL(DG4_ERR_INVALID_ARG, "dX must not be X or dY when the weights' gradients are asked for");
+        const size_t need = dg4_glu_bwd_workspace_bytes(g, desc, d_ff);
+        if (need && (!workspace || workspace_bytes < need))
+            DG4_FAIL(DG4_ERR_INVALID_ARG, "workspace too small: %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+        if (need && ((uintptr_t)workspace & 15u)) DG4_FAIL(DG4_ERR_INVALID_ARG, "the workspace is not 16-byte aligned");
+        out.part = need ? (float*)workspace : nullptr;
+        out.wg = (__nv_bfloat16*)dW_gate; out.wu = (__nv_bfloat16*)dW_up; out.wd = (__nv_bfloat16*)dW_down;
+    }
+    Maps m;
+    CHECK(weight_maps(&m, W_gate, W_up, W_down, d_ff));
+    CHECK(dg4i_make_row_map(&m.x, X, g->n, ldx, kTileM));
+    CHECK(dg4i_make_row_map(&m.dy, dY, g->n, lddy, kTileM));
+    Params p = make_params(g, d_ff);
+    p.out = (__nv_bfloat16*)dX; p.ldo = lddx;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (activation == DG4_ACT_SILU) return launch_bwd<DG4_ACT_SILU>(m, p, out, groups, g->device, sms, st);
+    if (activation == DG4_ACT_GELU) return launch_bwd<DG4_ACT_GELU>(m, p, out, groups, g->device, sms, st);
+    return launch_bwd<DG4_ACT_RELU>(m, p, out, groups, g->device, sms, st);
+}

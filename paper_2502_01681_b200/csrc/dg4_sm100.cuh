@@ -157,6 +157,18 @@ __device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t smem_addr) {
     d |= (uint64_t)4 << 61;                          // layout: 64-byte swizzle
     return d;
 }
+// The same bytes read as an MN-major operand (the 64 elements of a 128-byte row run along M or N, the rows along K):
+// groups of 8 rows are 1024 bytes apart, further groups of 64 elements of M or N `panel` bytes.  Sixteen K are 2048 bytes.
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t smem_addr, uint32_t panel) {
+    uint64_t d = 0;
+    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(panel >> 4) << 16;               // leading byte offset: the next 64 of M or N
+    d |= (uint64_t)(1024u >> 4) << 32;               // stride byte offset: the next 8 of K
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+constexpr uint32_t kIdescAMn = 1u << 15, kIdescBMn = 1u << 16;   // A, B given MN-major
 __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"

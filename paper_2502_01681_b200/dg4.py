@@ -32,6 +32,7 @@ DG4_FLAG_RESIDUAL = 1
 DG4_FLAG_LEVEL_LAUNCHES = 2
 DG4_FLAG_FUSED_LAYER = 4
 DG4_FLAG_RMS_NORM = 8
+DG4_ACT_SILU, DG4_ACT_GELU, DG4_ACT_RELU = 0, 1, 2
 
 DG4_KV8_ROW_BYTES = 288
 
@@ -50,6 +51,8 @@ EXPORTS = [
     "dg4_blocks_workspace_bytes", "dg4_blocks_fwd_levelised",
     "dg4_qkv_project_adapters", "dg4_out_project_adapters", "dg4_kv8_write", "dg4_kv8_read",
     "dg4_sparse_attn_kv8_fwd", "dg4_norm_gate_fwd",
+    "dg4_glu_fwd", "dg4_glu_bwd_workspace_bytes", "dg4_glu_bwd", "dg4_add_norm_fwd", "dg4_norm_bwd_workspace_bytes",
+    "dg4_norm_bwd",
 ]
 
 
@@ -192,6 +195,19 @@ def load():
     lib.dg4_debug_set_poll_limit.argtypes = [ctypes.c_uint32]
     lib.dg4_debug_override_current_device.restype = None
     lib.dg4_debug_override_current_device.argtypes = [ctypes.c_int32]
+    i32, f32, sz = ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+    lib.dg4_glu_fwd.restype = ctypes.c_int
+    lib.dg4_glu_fwd.argtypes = [vp, dp, vp, i64, vp, vp, vp, i32, i32, vp, i64, vp, i64, vp]
+    lib.dg4_glu_bwd_workspace_bytes.restype = sz
+    lib.dg4_glu_bwd_workspace_bytes.argtypes = [vp, dp, i32]
+    lib.dg4_glu_bwd.restype = ctypes.c_int
+    lib.dg4_glu_bwd.argtypes = [vp, dp, vp, i64, vp, vp, vp, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.dg4_add_norm_fwd.restype = ctypes.c_int
+    lib.dg4_add_norm_fwd.argtypes = [vp, dp, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp, i64, vp]
+    lib.dg4_norm_bwd_workspace_bytes.restype = sz
+    lib.dg4_norm_bwd_workspace_bytes.argtypes = [vp, dp]
+    lib.dg4_norm_bwd.restype = ctypes.c_int
+    lib.dg4_norm_bwd.argtypes = [vp, dp, vp, i64, vp, f32, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -537,6 +553,67 @@ def dg4_norm_gate_fwd(g: Graph, dsc: dg4_desc, S, R, res_scale, gate, seg, post,
                                     _vec(gate, n_gates), n_gates, _struct(seg), _vec(post[0]), _vec(post[1]),
                                     _vec(pre[0]), _vec(pre[1]), float(eps), _ptr(R_out), _ld(R_out), _ptr(Y),
                                     _ld(Y) if Y is not None else 0, _stream(stream)))
+
+
+def _opt(t):
+    """Pointer and row distance of a tensor that may be None."""
+    return (_ptr(t), _ld(t)) if t is not None else (None, 0)
+
+
+def _glu_weights(W_gate, W_up, W_down):
+    """Pointers of a gated sub-layer's weights (or of their gradients), and d_ff."""
+    d_ff = W_gate.shape[0]
+    if tuple(W_gate.shape) != (d_ff, 128) or tuple(W_up.shape) != (d_ff, 128) or tuple(W_down.shape) != (128, d_ff):
+        raise ValueError("a gated sub-layer's weights are [d_ff, 128], [d_ff, 128] and [128, d_ff]")
+    bf16 = _torch().bfloat16
+    for t in (W_gate, W_up, W_down):
+        if t.dtype != bf16 or not t.is_contiguous() or not t.is_cuda:
+            raise ValueError("a gated sub-layer's weights and their gradients are contiguous CUDA bf16 tensors")
+    return W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), d_ff
+
+
+def _workspace(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def dg4_glu_fwd(g: Graph, dsc: dg4_desc, X, W_gate, W_up, W_down, activation: int, H_res, Y, stream=None):
+    """Y = (act(X W_gate^T) * (X W_up^T)) W_down^T, plus H_res if dsc has the residual flag (H_res may be None)."""
+    _check(load().dg4_glu_fwd(g.handle, ctypes.byref(dsc), _ptr(X), _ld(X), *_glu_weights(W_gate, W_up, W_down), activation,
+                              *_opt(H_res), _ptr(Y), _ld(Y), _stream(stream)))
+
+
+def dg4_glu_bwd_workspace_bytes(g: Graph, dsc: dg4_desc, d_ff: int) -> int:
+    return int(load().dg4_glu_bwd_workspace_bytes(g.handle, ctypes.byref(dsc), d_ff))
+
+
+def dg4_glu_bwd(g: Graph, dsc: dg4_desc, X, W_gate, W_up, W_down, activation: int, dY, dX, dW_gate, dW_up, dW_down,
+                workspace=None, stream=None):
+    """The gradients of dg4_glu_fwd's gated sub-layer for dY; dX, or all three weights' gradients, may be None."""
+    weights = _glu_weights(W_gate, W_up, W_down)
+    grads = (None, None, None)
+    if dW_gate is not None or dW_up is not None or dW_down is not None:
+        if dW_gate is None or dW_up is None or dW_down is None or dW_gate.shape != W_gate.shape:
+            raise ValueError("the weights' gradients are given all three, shaped as the weights, or none")
+        grads = _glu_weights(dW_gate, dW_up, dW_down)[:3]
+    _check(load().dg4_glu_bwd(g.handle, ctypes.byref(dsc), _ptr(X), _ld(X), *weights, activation, _ptr(dY), _ld(dY),
+                              *_opt(dX), *grads, *_workspace(workspace), _stream(stream)))
+
+
+def dg4_add_norm_fwd(g: Graph, dsc: dg4_desc, X, R, gamma, beta, eps, Z, Y, stream=None):
+    """Z = X + R, Y = Norm(Z); R, beta and Z may be None."""
+    _check(load().dg4_add_norm_fwd(g.handle, ctypes.byref(dsc), _ptr(X), _ld(X), *_opt(R), _vec(gamma), _vec(beta), eps,
+                                   *_opt(Z), _ptr(Y), _ld(Y), _stream(stream)))
+
+
+def dg4_norm_bwd_workspace_bytes(g: Graph, dsc: dg4_desc) -> int:
+    return int(load().dg4_norm_bwd_workspace_bytes(g.handle, ctypes.byref(dsc)))
+
+
+def dg4_norm_bwd(g: Graph, dsc: dg4_desc, Z, gamma, eps, dY, D_res, dZ, dgamma, dbeta, workspace=None, stream=None):
+    """dZ = D_res + the gradient of Norm at Z for dY, and gamma's and beta's gradients; D_res and each output may be None."""
+    _check(load().dg4_norm_bwd(g.handle, ctypes.byref(dsc), _ptr(Z), _ld(Z), _vec(gamma), eps, _ptr(dY), _ld(dY),
+                               *_opt(D_res), *_opt(dZ), _vec(dgamma), _vec(dbeta), *_workspace(workspace),
+                               _stream(stream)))
 
 
 def dg4_debug_set_poll_limit(polls: int):
