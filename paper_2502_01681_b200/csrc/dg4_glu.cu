@@ -19,6 +19,7 @@
 #include <atomic>
 
 #include "dg4_internal.h"
+#include "dg4_pairs.cuh"
 #include "dg4_sm100.cuh"
 
 using namespace sm100;
@@ -29,7 +30,8 @@ constexpr int kTileM = 128;
 constexpr int kBlock = 64;                         // hidden units at a time
 constexpr int kHalfBytes = kTileM * 128;           // 64 columns of a 128-row tile
 constexpr int kTileBytes = 2 * kHalfBytes;
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 16;                      // four per scheduler: some compute while others wait for tensor memory
+constexpr int kEl = 16;                            // a block's values of a row that an epilogue thread takes, by its warp
 constexpr int kThreads = (2 + kEpiWarps) * 32;
 constexpr int kSmemLimit = 232448;                 // what one CTA may hold
 constexpr int kMaxDff = 8192;                      // at most as many blocks as SMs (glu_dw_kernel)
@@ -62,29 +64,93 @@ __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32
 
 // SiLU x * sigmoid(x), GELU by its tanh form x * sigmoid(2 sqrt(2/pi) (x + 0.044715 x^3)), ReLU max(0, x).
 constexpr float kLog2e = 1.4426950408889634f, kGelu1 = 1.5957691216057308f, kGelu3 = 0.07135481282052f;
+// sigmoid(p(g)) of eight values.  The special-function unit is what bounds the epilogues (an exponential and a reciprocal
+// per value: 1024 clocks per block and SM, the products 768), so two values share a reciprocal: 1/x = y / (xy).  Where the
+// exponentials are too large for that (2^63: g below -43 or so), and for NaN, which would reach the other value, each has
+// its own.
 template <int ACT>
-__device__ __forceinline__ float sigmoid_of(float g) {
-    if (ACT == DG4_ACT_SILU) return rcp(1.f + ex2(-kLog2e * g));
-    return rcp(1.f + ex2(g * (-kLog2e * kGelu1 - kLog2e * kGelu3 * (g * g))));
-}
-template <int ACT>
-__device__ __forceinline__ float act_of(float g) {
-    if (ACT == DG4_ACT_RELU) return fmaxf(g, 0.f);
-    return g * sigmoid_of<ACT>(g);
-}
-// act(g), and act'(g) = s + g s (1 - s) p'(g) with s = sigmoid(p(g))
-template <int ACT>
-__device__ __forceinline__ void act_both(float g, float& a, float& da) {
-    if (ACT == DG4_ACT_RELU) {
-        a = fmaxf(g, 0.f);
-        da = g > 0.f ? 1.f : 0.f;
-        return;
+__device__ __forceinline__ void sigmoid8(const float* g, float* s) {
+    float e[8], d[8];
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const Pair x = pair(g[i], g[i + 1]);
+        Pair p;
+        if (ACT == DG4_ACT_SILU) p = mul2(x, pair(-kLog2e, -kLog2e));
+        else p = mul2(x, fma2(mul2(x, x), pair(-kLog2e * kGelu3, -kLog2e * kGelu3), pair(-kLog2e * kGelu1, -kLog2e * kGelu1)));
+        split(p, e[i], e[i + 1]);
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(e[i]));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(e[i + 1]));
+        split(add2(pair(ex2(e[i]), ex2(e[i + 1])), pair(1.f, 1.f)), d[i], d[i + 1]);
+        const float r = rcp(d[i] * d[i + 1]);
+        s[i] = r * d[i + 1];
+        s[i + 1] = r * d[i];
     }
-    const float s = sigmoid_of<ACT>(g);
-    a = g * s;
-    // beyond |g| = 1000 the factor 1 - s or s is zero: p' is kept finite there
-    const float dp = ACT == DG4_ACT_SILU ? 1.f : kGelu1 + 3.f * kGelu3 * fminf(g * g, 1e6f);
-    da = fmaf(a * (1.f - s), dp, s);
+    if (!(top <= 63.f)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = rcp(1.f + ex2(e[i]));
+    }
+}
+// Sixteen values act(g) * u as eight pairs of bf16.
+template <int ACT>
+__device__ __forceinline__ void gated(const uint32_t* g_bits, const uint32_t* u_bits, uint32_t* out) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const float *g = reinterpret_cast<const float*>(g_bits) + 8 * c, *u = reinterpret_cast<const float*>(u_bits) + 8 * c;
+        float s[8];
+        if (ACT != DG4_ACT_RELU) sigmoid8<ACT>(g, s);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            Pair x = pair(g[i], g[i + 1]);
+            if (ACT == DG4_ACT_RELU) x = pair(fmaxf(g[i], 0.f), fmaxf(g[i + 1], 0.f));
+            else x = mul2(x, pair(s[i], s[i + 1]));
+            float lo, hi;
+            split(mul2(x, pair(u[i], u[i + 1])), lo, hi);
+            out[4 * c + i / 2] = pack_bf16(lo, hi);
+        }
+    }
+}
+// The same backward, for h = dL/d(act(g) u):  dg = h u act'(g),  du = h act(g),  a = act(g) u (not asked for: null), with
+// act'(g) = s + g s (1 - s) p'(g), s = sigmoid(p(g)).
+template <int ACT, bool VALUES>
+__device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t* u_bits, const uint32_t* h_bits, uint32_t* dg,
+                                          uint32_t* du, uint32_t* a) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const float *g = reinterpret_cast<const float*>(g_bits) + 8 * c, *u = reinterpret_cast<const float*>(u_bits) + 8 * c,
+                    *h = reinterpret_cast<const float*>(h_bits) + 8 * c;
+        float s[8];
+        if (ACT != DG4_ACT_RELU) sigmoid8<ACT>(g, s);
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const Pair uu = pair(u[i], u[i + 1]), hh = pair(h[i], h[i + 1]);
+            Pair act, slope;
+            if (ACT == DG4_ACT_RELU) {
+                act = pair(fmaxf(g[i], 0.f), fmaxf(g[i + 1], 0.f));
+                slope = pair(g[i] > 0.f ? 1.f : 0.f, g[i + 1] > 0.f ? 1.f : 0.f);
+            } else {
+                const Pair x = pair(g[i], g[i + 1]), ss = pair(s[i], s[i + 1]);
+                act = mul2(x, ss);
+                Pair t = mul2(act, fma2(ss, pair(-1.f, -1.f), pair(1.f, 1.f)));
+                if (ACT == DG4_ACT_GELU) {
+                    // beyond |g| = 1000 s or 1 - s is zero: p' is kept finite there
+                    float x0, x1;
+                    split(mul2(x, x), x0, x1);
+                    t = mul2(t, fma2(pair(fminf(x0, 1e6f), fminf(x1, 1e6f)), pair(3.f * kGelu3, 3.f * kGelu3), pair(kGelu1, kGelu1)));
+                }
+                slope = add2(t, ss);
+            }
+            float lo, hi;
+            split(mul2(hh, act), lo, hi);
+            du[4 * c + i / 2] = pack_bf16(lo, hi);
+            split(mul2(mul2(hh, uu), slope), lo, hi);
+            dg[4 * c + i / 2] = pack_bf16(lo, hi);
+            if (VALUES) {
+                split(mul2(act, uu), lo, hi);
+                a[4 * c + i / 2] = pack_bf16(lo, hi);
+            }
+        }
+    }
 }
 
 struct Params {
@@ -124,7 +190,7 @@ __device__ __forceinline__ void product_128(uint32_t d, uint32_t a, uint32_t b, 
 // forward
 // ---------------------------------------------------------------------------------------------------
 // Tensor memory: Y in columns 0..127, three G|U buffers behind it, so that the products of two blocks run ahead of the
-// epilogue of a third.  The activations of a block overwrite its G: 16 columns from G's 0 and from G's 32 on.
+// epilogue of a third.  The activations of a block overwrite its G, each warp's 16 values in 8 of the columns it has read.
 namespace fwd {
 constexpr int kStages = 3, kBufs = 3;
 constexpr int kOffGu = 2 * kTileBytes, kOffD = kOffGu + kStages * kTileBytes, kOffBars = kOffD + kStages * kHalfBytes;
@@ -236,7 +302,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     tc_fence_after();
                     const int steps = min(4, (p.d_ff - b2 * kBlock + 15) / 16);
                     for (int ks = 0; ks < steps; ++ks)
-                        mma_bf16_ta(tmem, tmem + 128 + buf2.at * 128 + (ks >> 1) * 32 + (ks & 1) * 8,
+                        mma_bf16_ta(tmem, tmem + 128 + buf2.at * 128 + ks * 16,
                                     smem_desc_sw128(base + kOffD + d.at * kHalfBytes + ks * 32), idesc, (b2 | ks) ? 1u : 0u);
                     mma_commit(bar(bars->d_empty[d.at]));
                     d.next(kStages); buf2.next(kBufs);
@@ -249,7 +315,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         }
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int quad = warp & 3, half = (warp - 2) >> 2;           // 32 rows, and which half of a block's (or Y's) columns
+        // 32 rows, and which 16 columns of a block (of Y: which 32)
+        const int quad = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         Turn x, buf;
         uint32_t y_odd = 0;
@@ -260,24 +327,18 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * 128 + half * 32);
-                uint32_t g[32], u[32], a[16];
-                tmem_ld_32x32(at, g);
-                tmem_ld_32x32(at + 64, u);
+                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * 128 + part * kEl);
+                uint32_t g[kEl], u[kEl], a[kEl / 2];
+                tmem_ld_32x16(at, g);
+                tmem_ld_32x16(at + 64, u);
                 tmem_ld_wait();
-                const int valid = p.d_ff - b * kBlock - half * 32;   // hidden units past the last: zero
+                gated<ACT>(g, u, a);
+                const int valid = p.d_ff - b * kBlock - part * kEl;  // hidden units past the last: zero
+                if (valid < kEl) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float lo = act_of<ACT>(__uint_as_float(g[2 * i])) * __uint_as_float(u[2 * i]);
-                    const float hi = act_of<ACT>(__uint_as_float(g[2 * i + 1])) * __uint_as_float(u[2 * i + 1]);
-                    a[i] = pack_bf16(lo, hi);
-                }
-                if (valid < 32) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) if (2 * i >= valid) a[i] = 0u;
+                    for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) a[i] = 0u;
                 }
                 tmem_st_32x8(at, a);
-                tmem_st_32x8(at + 8, a + 8);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -290,27 +351,26 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 }
             }
             if (!ok) break;
-            uint32_t r[32];
+            uint32_t r[16];
             const bool res = p.R != nullptr && row0 + lane < p.n;
             if (res) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + half * 64 + i * 8, r + 4 * i);
+                for (int i = 0; i < 4; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + part * 32 + i * 8, r + 4 * i);
             }
             ok = mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit);
             if (!ok) break;
             y_odd ^= 1u;
             tc_fence_after();
-            uint32_t y[64];
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64), y);
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64 + 32), y + 32);
+            uint32_t y[32];
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 32), y);
             tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(bars->y_empty));
             // Y's products are done, so X's are: its place stages the rows
-            const uint32_t stage = base + x.at * kTileBytes + half * kHalfBytes + quad * 4096;
+            const uint32_t stage = base + x.at * kTileBytes + (warp - 2) * 2048;       // rows of 64 bytes, 64-byte swizzle
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 4; ++i) {
                 uint32_t o[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -321,12 +381,12 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     }
                     o[e] = pack_bf16(lo, hi);
                 }
-                st_shared_v4(stage + sw128_offset(lane, i), o);
+                st_shared_v4(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4), o);
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0 && row0 < p.n) {
-                tma_store_2d(&map_y, half * 64, row0, stage);
+                tma_store_2d(&map_y, part * 32, row0, stage);
                 bulk_commit();
             }
             stored = true;
@@ -346,8 +406,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 // ---------------------------------------------------------------------------------------------------
 // backward: dX
 // ---------------------------------------------------------------------------------------------------
-// Tensor memory: dX in columns 0..127, two buffers of G | U | dA behind it.  dG overwrites G, dU overwrites U (16 columns
-// from 0 and from 32 on of each).
+// Tensor memory: dX in columns 0..127, two buffers of G | U | dA behind it.  dG overwrites G, dU overwrites U, each warp's
+// 16 values in 8 of the columns it has read.
 namespace dx {
 constexpr int kStages = 3, kBufs = 2, kBufCols = 192;
 constexpr int kStageBytes = kTileBytes + kHalfBytes;              // Wg and Wu, then Wd
@@ -458,7 +518,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     const uint32_t w = base + kOffW + w2.at * kStageBytes, a = tmem + 128 + buf2.at * kBufCols;
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)                   // dX += [dG | dU] [Wg; Wu]: their rows run along K
-                        mma_bf16_ta(tmem, a + (ks >> 1) * 32 + (ks & 1) * 8, smem_desc_sw128_mn(w + ks * 2048, kHalfBytes), id_dx, (b2 | ks) ? 1u : 0u);
+                        mma_bf16_ta(tmem, a + ks * 16, smem_desc_sw128_mn(w + ks * 2048, kHalfBytes), id_dx, (b2 | ks) ? 1u : 0u);
                     mma_commit(bar(bars->w_empty[w2.at]));
                     w2.next(kStages); buf2.next(kBufs);
                     if (++b2 == nb) { b2 = 0; mma_commit(bar(bars->y_full)); }
@@ -470,7 +530,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         }
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const int quad = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         Turn buf;
         uint32_t y_odd = 0;
@@ -481,36 +541,20 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * kBufCols + half * 32);
-                uint32_t g[32], u[32], h[32];
-                tmem_ld_32x32(at, g);
-                tmem_ld_32x32(at + 64, u);
-                tmem_ld_32x32(at + 128, h);
+                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * kBufCols + part * kEl);
+                uint32_t g[kEl], u[kEl], h[kEl], dg[kEl / 2], du[kEl / 2];
+                tmem_ld_32x16(at, g);
+                tmem_ld_32x16(at + 64, u);
+                tmem_ld_32x16(at + 128, h);
                 tmem_ld_wait();
-                const int valid = p.d_ff - b * kBlock - half * 32;
-                uint32_t dg[16], du[16];
+                gated_bwd<ACT, false>(g, u, h, dg, du, nullptr);
+                const int valid = p.d_ff - b * kBlock - part * kEl;
+                if (valid < kEl) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float vg[2], vu[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float dh = __uint_as_float(h[2 * i + e]);
-                        float a, da;
-                        act_both<ACT>(__uint_as_float(g[2 * i + e]), a, da);
-                        vu[e] = dh * a;
-                        vg[e] = dh * __uint_as_float(u[2 * i + e]) * da;
-                    }
-                    dg[i] = pack_bf16(vg[0], vg[1]);
-                    du[i] = pack_bf16(vu[0], vu[1]);
-                }
-                if (valid < 32) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) if (2 * i >= valid) dg[i] = du[i] = 0u;
+                    for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) dg[i] = du[i] = 0u;
                 }
                 tmem_st_32x8(at, dg);
-                tmem_st_32x8(at + 8, dg + 8);
                 tmem_st_32x8(at + 64, du);
-                tmem_st_32x8(at + 72, du + 8);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
@@ -521,20 +565,19 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             if (!ok) break;
             y_odd ^= 1u;
             tc_fence_after();
-            uint32_t y[64];
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64), y);
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(half * 64 + 32), y + 32);
+            uint32_t y[32];
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 32), y);
             tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(bars->y_empty));
             if (row < p.n) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 4; ++i) {
                     uint32_t o[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
-                    st_global_v4(p.out + (int64_t)row * p.ldo + half * 64 + i * 8, o);
+                    st_global_v4(p.out + (int64_t)row * p.ldo + part * 32 + i * 8, o);
                 }
             }
             __syncwarp();
@@ -683,9 +726,9 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         }
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int quad = warp & 3, half = (warp - 2) >> 2;
+        const int quad = warp & 3, part = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const int valid = p.d_ff - block * kBlock - half * 32;       // hidden units of this warp's 32 that exist
+        const int valid = p.d_ff - block * kBlock - part * kEl;      // hidden units of this warp's 16 that exist
         uint32_t odd = 0;
         bool ok = true;
         for (int t = 0; t < tiles && ok; ++t, odd ^= 1u) {
@@ -693,43 +736,29 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full), odd, limit);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t at = tmem + lanes + (uint32_t)(192 + half * 32);
-            uint32_t g[32], u[32], h[32];
-            tmem_ld_32x32(at, g);
-            tmem_ld_32x32(at + 64, u);
-            tmem_ld_32x32(at + 128, h);
+            const uint32_t at = tmem + lanes + (uint32_t)(192 + part * kEl);
+            uint32_t g[kEl], u[kEl], h[kEl], v[3][kEl / 2];
+            tmem_ld_32x16(at, g);
+            tmem_ld_32x16(at + 64, u);
+            tmem_ld_32x16(at + 128, h);
             tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(bars->acc_empty));
-            ok = mbar_wait_relaxed_warp(bar(bars->a_empty), odd ^ 1u, limit);
-            if (!ok) break;
+            gated_bwd<ACT, true>(g, u, h, v[0], v[1], v[2]);
             // a row past the last (its X and dY read as zero) and a unit past the last add nothing, whatever the weights
             // hold: 0 * infinity would
+            if (!in || valid < kEl) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[3][4];
+                for (int i = 0; i < kEl / 2; ++i) if (!in || 2 * i >= valid) v[0][i] = v[1][i] = v[2][i] = 0u;
+            }
+            ok = mbar_wait_relaxed_warp(bar(bars->a_empty), odd ^ 1u, limit);
+            if (!ok) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float vg[2], vu[2], va[2];
+            for (int c = 0; c < 2; ++c) {
+                const uint32_t off = base + kOffA + sw128_offset(quad * 32 + lane, part * 2 + c);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int k = 8 * c + 2 * i + e;
-                        const float dh = __uint_as_float(h[k]), uu = __uint_as_float(u[k]);
-                        float a, da;
-                        act_both<ACT>(__uint_as_float(g[k]), a, da);
-                        vu[e] = dh * a;
-                        vg[e] = dh * uu * da;
-                        va[e] = a * uu;
-                    }
-                    const bool keep = in && 8 * c + 2 * i < valid;
-                    v[0][i] = keep ? pack_bf16(vg[0], vg[1]) : 0u;
-                    v[1][i] = keep ? pack_bf16(vu[0], vu[1]) : 0u;
-                    v[2][i] = keep ? pack_bf16(va[0], va[1]) : 0u;
-                }
-                const uint32_t off = base + kOffA + sw128_offset(quad * 32 + lane, half * 4 + c);
-#pragma unroll
-                for (int m = 0; m < 3; ++m) st_shared_v4(off + m * kHalfBytes, v[m]);
+                for (int m = 0; m < 3; ++m) st_shared_v4(off + m * kHalfBytes, v[m] + 4 * c);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -739,17 +768,17 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         if (ok) {
             tc_fence_after();
             const int col = quad * 32 + lane;                        // an input (dWg, dWu) or an output (dWd)
-            float* part = out.part ? out.part + ((int64_t)group * gridDim.x + block) * kPart : nullptr;
+            float* sums = out.part ? out.part + ((int64_t)group * gridDim.x + block) * kPart : nullptr;
 #pragma unroll 1
             for (int m = 0; m < 3; ++m) {
-                uint32_t w[32];
-                tmem_ld_32x32(tmem + lanes + (uint32_t)(m * 64 + half * 32), w);
+                uint32_t w[kEl];
+                tmem_ld_32x16(tmem + lanes + (uint32_t)(m * 64 + part * kEl), w);
                 tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
+                for (int i = 0; i < kEl; ++i) {
                     const float f = __uint_as_float(w[i]);
-                    const int unit = block * kBlock + half * 32 + i;
-                    if (part) part[(m * kBlock + half * 32 + i) * 128 + col] = f;
+                    const int unit = block * kBlock + part * kEl + i;
+                    if (sums) sums[(m * kBlock + part * kEl + i) * 128 + col] = f;
                     else if (i < valid) {
                         if (m == 2) out.wd[(int64_t)col * p.d_ff + unit] = __float2bfloat16(f);
                         else (m == 0 ? out.wg : out.wu)[(int64_t)unit * 128 + col] = __float2bfloat16(f);
@@ -890,7 +919,7 @@ extern "C" dg4_status dg4_glu_fwd(const dg4_graph* g, const dg4_desc* desc, cons
     Maps m;
     CHECK(weight_maps(&m, W_gate, W_up, W_down, d_ff));
     CHECK(dg4i_make_row_map(&m.x, X, g->n, ldx, kTileM));
-    CHECK(dg4i_make_row_map(&m.y, Y, g->n, ldy, 32));
+    CHECK(dg4i_make_map(&m.y, Y, 128, g->n, ldy, 32, 32));
     Params p = make_params(g, d_ff);
     p.R = res ? (const __nv_bfloat16*)H_res : nullptr; p.ldr = ldh;
     const cudaStream_t st = (cudaStream_t)stream;

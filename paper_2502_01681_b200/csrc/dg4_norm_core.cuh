@@ -3,6 +3,7 @@
 
 #include "dg4_attn_core.cuh"
 #include "dg4_internal.h"
+#include "dg4_pairs.cuh"
 
 namespace normcore {
 
@@ -10,18 +11,6 @@ constexpr int kRows = 4;                    // rows of a warp at a time
 constexpr int kLanes = 8;                   // lanes per row
 constexpr int kEl = 128 / kLanes;           // elements per lane
 constexpr int kPairs = kEl / 2;
-
-// pairs of fp32 numbers in one 64-bit register, and the packed instructions on them
-typedef unsigned long long Pair;
-__device__ __forceinline__ Pair pair(float lo, float hi) {
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
-    return p;
-}
-__device__ __forceinline__ void split(Pair p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
-__device__ __forceinline__ Pair add2(Pair a, Pair b) { Pair c; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(a), "l"(b)); return c; }
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) { Pair c; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(a), "l"(b)); return c; }
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
 
 // Which four elements of a row the i-th quadruple of a lane is (counted in quadruples): a lane's loads are 16 bytes, 8
 // lanes side by side, so bf16 rows give it two neighbouring quadruples at a time and fp32 rows one.
