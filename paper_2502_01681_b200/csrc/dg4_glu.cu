@@ -178,13 +178,14 @@ __device__ __forceinline__ void load_tile(const CUtensorMap* map, uint32_t dst, 
     for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kHalfBytes, map, h * 64, row0, bar);
 }
 // d = A B^T over 128 inputs, both K-major in two panels of 64
-__device__ __forceinline__ void product_128(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+__device__ __forceinline__ void product_128(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
-        const uint32_t off = (uint32_t)((ks >> 2) * kHalfBytes + (ks & 3) * 32);
-        mma_bf16(d, smem_desc_sw128(a + off), smem_desc_sw128(b + off), idesc, ks > 0 ? 1u : 0u);
+        const uint64_t off = (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4);
+        mma_bf16_by(elected, d, a + off, b + off, idesc, ks > 0 ? 1u : 0u);
     }
 }
+constexpr uint64_t kStepMn = 2048 >> 4;            // sixteen K of an MN-major operand, in descriptor units
 
 // ---------------------------------------------------------------------------------------------------
 // forward
@@ -214,7 +215,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int nb = p.n_blocks;
     volatile uint32_t* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
@@ -236,7 +237,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;
+    const uint32_t tmem = uniform(bars->tmem_base);
     const int tiles = (p.n_tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
     const uint32_t limit = p.poll_limit;
 
@@ -273,46 +274,45 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        if (lane == 0) {
-            const uint32_t idesc = idesc_bf16_f32(128, 128);
-            const int total = tiles * nb;
-            Turn x, gu, d, buf1, buf2;
-            int b1 = 0, b2 = 0;                          // blocks within their tiles
-            uint32_t y_odd = 1;
-            bool ok = true;
-            // First products run two blocks ahead of second ones.  (One where a tile is one block: the tile two further on
-            // takes the place of X that this tile's epilogue leaves, which comes after this tile's second product.)
-            const int ahead = nb == 1 ? 1 : 2;
-            for (int c = 0; c < total + ahead && ok; ++c) {
-                if (c < total) {
-                    if (b1 == 0) ok = mbar_wait_relaxed(bar(bars->x_full[x.at]), x.odd, limit);
-                    ok = ok && !*abort_flag && mbar_wait_relaxed(bar(bars->gu_full[gu.at]), gu.odd, limit);
-                    if (!ok) break;
-                    tc_fence_after();
-                    product_128(tmem + 128 + buf1.at * 128, base + x.at * kTileBytes, base + kOffGu + gu.at * kTileBytes, idesc);
-                    mma_commit(bar(bars->acc_full[buf1.at]));
-                    mma_commit(bar(bars->gu_empty[gu.at]));
-                    gu.next(kStages); buf1.next(kBufs);
-                    if (++b1 == nb) { b1 = 0; x.next(2); }
-                }
-                if (c >= ahead) {
-                    ok = mbar_wait_relaxed(bar(bars->d_full[d.at]), d.odd, limit) && mbar_wait_relaxed(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
-                    if (ok && b2 == 0) { ok = mbar_wait_relaxed(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
-                    if (!ok) break;
-                    tc_fence_after();
-                    const int steps = min(4, (p.d_ff - b2 * kBlock + 15) / 16);
-                    for (int ks = 0; ks < steps; ++ks)
-                        mma_bf16_ta(tmem, tmem + 128 + buf2.at * 128 + ks * 16,
-                                    smem_desc_sw128(base + kOffD + d.at * kHalfBytes + ks * 32), idesc, (b2 | ks) ? 1u : 0u);
-                    mma_commit(bar(bars->d_empty[d.at]));
-                    d.next(kStages); buf2.next(kBufs);
-                    if (++b2 == nb) { b2 = 0; mma_commit(bar(bars->y_full)); }
-                }
+        const uint32_t idesc = idesc_bf16_f32(128, 128), elected = elect_one();
+        const int total = tiles * nb;
+        Turn x, gu, d, buf1, buf2;
+        int b1 = 0, b2 = 0;                              // blocks within their tiles
+        uint32_t y_odd = 1;
+        bool ok = true;
+        // First products run two blocks ahead of second ones.  (One where a tile is one block: the tile two further on
+        // takes the place of X that this tile's epilogue leaves, which comes after this tile's second product.)
+        const int ahead = nb == 1 ? 1 : 2;
+        for (int c = 0; c < total + ahead && ok; ++c) {
+            if (c < total) {
+                if (b1 == 0) ok = mbar_wait_relaxed_warp(bar(bars->x_full[x.at]), x.odd, limit);
+                ok = ok && mbar_wait_relaxed_warp(bar(bars->gu_full[gu.at]), gu.odd, limit);
+                if (!ok) break;
+                tc_fence_after();
+                product_128(elected, tmem + 128 + buf1.at * 128, smem_desc_sw128(base + x.at * kTileBytes), smem_desc_sw128(base + kOffGu + gu.at * kTileBytes), idesc);
+                mma_commit_by(elected, bar(bars->acc_full[buf1.at]));
+                mma_commit_by(elected, bar(bars->gu_empty[gu.at]));
+                gu.next(kStages); buf1.next(kBufs);
+                if (++b1 == nb) { b1 = 0; x.next(2); }
             }
-            if (!ok) raise_timeout(bars, p.status);
-            mma_commit(bar(bars->drain));                // tensor memory is freed below: every product must be done
-            mbar_wait(bar(bars->drain), 0);
+            if (c >= ahead) {
+                ok = mbar_wait_relaxed_warp(bar(bars->d_full[d.at]), d.odd, limit) && mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
+                if (!ok) break;
+                tc_fence_after();
+                const int steps = min(4, (p.d_ff - b2 * kBlock + 15) / 16);
+                const uint64_t wd = smem_desc_sw128(base + kOffD + d.at * kHalfBytes);
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                    if (ks < steps) mma_bf16_ta_by(elected, tmem, tmem + 128 + buf2.at * 128 + ks * 16, wd + ks * 2, idesc, (b2 | ks) ? 1u : 0u);
+                mma_commit_by(elected, bar(bars->d_empty[d.at]));
+                d.next(kStages); buf2.next(kBufs);
+                if (++b2 == nb) { b2 = 0; mma_commit_by(elected, bar(bars->y_full)); }
+            }
         }
+        if (!ok) raise_timeout(bars, p.status);
+        mma_commit_by(elected, bar(bars->drain));        // tensor memory is freed below: every product must be done
+        mbar_wait_warp(bar(bars->drain), 0);
     } else {
         // ------------------------------------------------------------------ epilogue
         // 32 rows, and which 16 columns of a block (of Y: which 32)
@@ -432,7 +432,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int nb = p.n_blocks;
     volatile uint32_t* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
@@ -451,7 +451,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;
+    const uint32_t tmem = uniform(bars->tmem_base);
     const int tiles = (p.n_tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
     const uint32_t limit = p.poll_limit;
 
@@ -486,48 +486,48 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        if (lane == 0) {
-            const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
-                           id_dx = idesc_bf16_f32(128, 128) | kIdescBMn;
-            const int total = tiles * nb;
-            Turn w1, w2, buf1, buf2;
-            int b1 = 0, b2 = 0;
-            uint32_t x_odd = 0, y_odd = 1;
-            bool ok = true;
-            for (int c = 0; c < total + 1 && ok; ++c) {
-                if (c < total) {
-                    if (b1 == 0) { ok = mbar_wait_relaxed(bar(bars->x_full), x_odd, limit); x_odd ^= 1u; }
-                    ok = ok && !*abort_flag && mbar_wait_relaxed(bar(bars->w_full[w1.at]), w1.odd, limit);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t w = base + kOffW + w1.at * kStageBytes, d = tmem + 128 + buf1.at * kBufCols;
-                    product_128(d, base, w, id_gu);
+        const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
+                       id_dx = idesc_bf16_f32(128, 128) | kIdescBMn, elected = elect_one();
+        const int total = tiles * nb;
+        Turn w1, w2, buf1, buf2;
+        int b1 = 0, b2 = 0;
+        uint32_t x_odd = 0, y_odd = 1;
+        bool ok = true;
+        const uint64_t desc_x = smem_desc_sw128(base), desc_dy = smem_desc_sw128(base + kTileBytes);
+        for (int c = 0; c < total + 1 && ok; ++c) {
+            if (c < total) {
+                if (b1 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->x_full), x_odd, limit); x_odd ^= 1u; }
+                ok = ok && mbar_wait_relaxed_warp(bar(bars->w_full[w1.at]), w1.odd, limit);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t w = base + kOffW + w1.at * kStageBytes, d = tmem + 128 + buf1.at * kBufCols;
+                product_128(elected, d, desc_x, smem_desc_sw128(w), id_gu);
+                const uint64_t wd = smem_desc_sw128_mn(w + kTileBytes, kHalfBytes);
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)                   // dA = dY Wd: Wd's rows run along K
-                        mma_bf16(d + 128, smem_desc_sw128(base + kTileBytes + (ks >> 2) * kHalfBytes + (ks & 3) * 32),
-                                 smem_desc_sw128_mn(w + kTileBytes + ks * 2048, kHalfBytes), id_da, ks > 0 ? 1u : 0u);
-                    mma_commit(bar(bars->acc_full[buf1.at]));
-                    w1.next(kStages); buf1.next(kBufs);
-                    if (++b1 == nb) { b1 = 0; mma_commit(bar(bars->x_empty)); }
-                }
-                if (c >= 1) {
-                    ok = mbar_wait_relaxed(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
-                    if (ok && b2 == 0) { ok = mbar_wait_relaxed(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t w = base + kOffW + w2.at * kStageBytes, a = tmem + 128 + buf2.at * kBufCols;
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)                   // dX += [dG | dU] [Wg; Wu]: their rows run along K
-                        mma_bf16_ta(tmem, a + ks * 16, smem_desc_sw128_mn(w + ks * 2048, kHalfBytes), id_dx, (b2 | ks) ? 1u : 0u);
-                    mma_commit(bar(bars->w_empty[w2.at]));
-                    w2.next(kStages); buf2.next(kBufs);
-                    if (++b2 == nb) { b2 = 0; mma_commit(bar(bars->y_full)); }
-                }
+                for (int ks = 0; ks < 8; ++ks)                       // dA = dY Wd: Wd's rows run along K
+                    mma_bf16_by(elected, d + 128, desc_dy + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), wd + ks * kStepMn, id_da, ks > 0 ? 1u : 0u);
+                mma_commit_by(elected, bar(bars->acc_full[buf1.at]));
+                w1.next(kStages); buf1.next(kBufs);
+                if (++b1 == nb) { b1 = 0; mma_commit_by(elected, bar(bars->x_empty)); }
             }
-            if (!ok) raise_timeout(bars, p.status);
-            mma_commit(bar(bars->drain));
-            mbar_wait(bar(bars->drain), 0);
+            if (c >= 1) {
+                ok = mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t w = smem_desc_sw128_mn(base + kOffW + w2.at * kStageBytes, kHalfBytes);
+                const uint32_t a = tmem + 128 + buf2.at * kBufCols;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)                       // dX += [dG | dU] [Wg; Wu]: their rows run along K
+                    mma_bf16_ta_by(elected, tmem, a + ks * 16, w + ks * kStepMn, id_dx, (b2 | ks) ? 1u : 0u);
+                mma_commit_by(elected, bar(bars->w_empty[w2.at]));
+                w2.next(kStages); buf2.next(kBufs);
+                if (++b2 == nb) { b2 = 0; mma_commit_by(elected, bar(bars->y_full)); }
+            }
         }
+        if (!ok) raise_timeout(bars, p.status);
+        mma_commit_by(elected, bar(bars->drain));
+        mbar_wait_warp(bar(bars->drain), 0);
     } else {
         // ------------------------------------------------------------------ epilogue
         const int quad = warp & 3, part = (warp - 2) >> 2;
@@ -628,7 +628,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int block = blockIdx.x, group = blockIdx.y, groups = gridDim.y;
     volatile uint32_t* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
@@ -647,7 +647,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;
+    const uint32_t tmem = uniform(bars->tmem_base);
     const int tiles = (p.n_tiles - group + groups - 1) / groups;     // at least one: groups <= n_tiles
     const uint32_t limit = p.poll_limit;
 
@@ -676,54 +676,55 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        if (lane == 0) {
-            const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
-                           id_w = idesc_bf16_f32(128, 128) | kIdescAMn | kIdescBMn, id_wd = idesc_bf16_f32(128, 64) | kIdescAMn | kIdescBMn;
-            Turn x1, x2;
-            uint32_t acc_odd = 1, a_odd = 0, polls = 0;
-            bool ok = mbar_wait_relaxed(bar(bars->w_full), 0, limit);
-            // Whichever can go first: the next tile's first products (its rows have come, the epilogue has taken its
-            // values) or this tile's second ones.  With a fixed order the tensor cores would wait for rows that can only
-            // come when second products have left a stage.
-            for (int t1 = 0, t2 = 0; t2 < tiles && ok;) {
-                if (t1 < tiles && mbar_test(bar(bars->x_full[x1.at]), x1.odd) && mbar_test(bar(bars->acc_empty), acc_odd)) {
-                    acc_odd ^= 1u;
-                    tc_fence_after();
-                    const uint32_t x = base + kOffX + x1.at * 2 * kTileBytes, d = tmem + 192;
-                    product_128(d, x, base, id_gu);
+        const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
+                       id_w = idesc_bf16_f32(128, 128) | kIdescAMn | kIdescBMn, id_wd = idesc_bf16_f32(128, 64) | kIdescAMn | kIdescBMn,
+                       elected = elect_one();
+        Turn x1, x2;
+        uint32_t acc_odd = 1, a_odd = 0, polls = 0;
+        bool ok = mbar_wait_relaxed_warp(bar(bars->w_full), 0, limit);
+        const uint64_t desc_gu = smem_desc_sw128(base), desc_wd = smem_desc_sw128_mn(base + kTileBytes, kHalfBytes),
+                       desc_a = smem_desc_sw128_mn(base + kOffA, kHalfBytes);
+        auto here = [](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity) ? 1 : 0) != 0; };
+        // Whichever can go first: the next tile's first products (its rows have come, the epilogue has taken its values) or
+        // this tile's second ones.  With a fixed order the tensor cores would wait for rows that can only come when second
+        // products have left a stage.
+        for (int t1 = 0, t2 = 0; t2 < tiles && ok;) {
+            if (t1 < tiles && here(bar(bars->x_full[x1.at]), x1.odd) && here(bar(bars->acc_empty), acc_odd)) {
+                acc_odd ^= 1u;
+                tc_fence_after();
+                const uint32_t x = base + kOffX + x1.at * 2 * kTileBytes, d = tmem + 192;
+                product_128(elected, d, smem_desc_sw128(x), desc_gu, id_gu);
+                const uint64_t dy = smem_desc_sw128(x + kTileBytes);
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)
-                        mma_bf16(d + 128, smem_desc_sw128(x + kTileBytes + (ks >> 2) * kHalfBytes + (ks & 3) * 32),
-                                 smem_desc_sw128_mn(base + kTileBytes + ks * 2048, kHalfBytes), id_da, ks > 0 ? 1u : 0u);
-                    mma_commit(bar(bars->acc_full));
-                    x1.next(kStages);
-                    ++t1;
-                    polls = 0;
-                } else if (t2 < t1 && mbar_test(bar(bars->a_full), a_odd)) {
-                    a_odd ^= 1u;
-                    tc_fence_after();
-                    const uint32_t x = base + kOffX + x2.at * 2 * kTileBytes, a = base + kOffA;
+                for (int ks = 0; ks < 8; ++ks)
+                    mma_bf16_by(elected, d + 128, dy + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), desc_wd + ks * kStepMn, id_da, ks > 0 ? 1u : 0u);
+                mma_commit_by(elected, bar(bars->acc_full));
+                x1.next(kStages);
+                ++t1;
+                polls = 0;
+            } else if (t2 < t1 && here(bar(bars->a_full), a_odd)) {
+                a_odd ^= 1u;
+                tc_fence_after();
+                const uint64_t x = smem_desc_sw128_mn(base + kOffX + x2.at * 2 * kTileBytes, kHalfBytes), dy = x + (kTileBytes >> 4);
 #pragma unroll
-                    for (int ks = 0; ks < 8; ++ks) {                 // sixteen rows at a time
-                        mma_bf16(tmem, smem_desc_sw128_mn(x + ks * 2048, kHalfBytes), smem_desc_sw128_mn(a + ks * 2048, kHalfBytes), id_w, t2 > 0 || ks > 0 ? 1u : 0u);
-                        mma_bf16(tmem + 128, smem_desc_sw128_mn(x + kTileBytes + ks * 2048, kHalfBytes),
-                                 smem_desc_sw128_mn(a + 2 * kHalfBytes + ks * 2048, kHalfBytes), id_wd, t2 > 0 || ks > 0 ? 1u : 0u);
-                    }
-                    mma_commit(bar(bars->a_empty));
-                    mma_commit(bar(bars->x_empty[x2.at]));
-                    x2.next(kStages);
-                    ++t2;
-                    polls = 0;
-                } else {
-                    ok = !*abort_flag && ++polls <= limit;
-                    if (polls > 64) __nanosleep(40);
+                for (int ks = 0; ks < 8; ++ks) {                     // sixteen rows at a time
+                    mma_bf16_by(elected, tmem, x + ks * kStepMn, desc_a + ks * kStepMn, id_w, t2 > 0 || ks > 0 ? 1u : 0u);
+                    mma_bf16_by(elected, tmem + 128, dy + ks * kStepMn, desc_a + (2 * kHalfBytes >> 4) + ks * kStepMn, id_wd, t2 > 0 || ks > 0 ? 1u : 0u);
                 }
+                mma_commit_by(elected, bar(bars->a_empty));
+                mma_commit_by(elected, bar(bars->x_empty[x2.at]));
+                x2.next(kStages);
+                ++t2;
+                polls = 0;
+            } else {
+                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && ++polls <= limit;
+                if (polls > 64) __nanosleep(40);
             }
-            if (ok) mma_commit(bar(bars->w_done));
-            else raise_timeout(bars, p.status);
-            mma_commit(bar(bars->drain));
-            mbar_wait(bar(bars->drain), 0);
         }
+        if (ok) mma_commit_by(elected, bar(bars->w_done));
+        else raise_timeout(bars, p.status);
+        mma_commit_by(elected, bar(bars->drain));
+        mbar_wait_warp(bar(bars->drain), 0);
     } else {
         // ------------------------------------------------------------------ epilogue
         const int quad = warp & 3, part = (warp - 2) >> 2;
