@@ -32,7 +32,9 @@ constexpr int kHalfBytes = kTileM * 128;           // 64 columns of a 128-row ti
 constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kEpiWarps = 16;                      // four per scheduler: some compute while others wait for tensor memory
 constexpr int kEl = 16;                            // a block's values of a row that an epilogue thread takes, by its warp
-constexpr int kThreads = (2 + kEpiWarps) * 32;
+constexpr int kCtrlWarps = 4;                      // warp 0, 2, 3: loads, warp 1: products
+constexpr int kThreads = (kCtrlWarps + kEpiWarps) * 32;
+constexpr int kSetWarps = kEpiWarps / 2;           // forward and dX: half of the epilogue warps take every other block
 constexpr int kSmemLimit = 232448;                 // what one CTA may hold
 constexpr int kMaxDff = 8192;                      // at most as many blocks as SMs (glu_dw_kernel)
 
@@ -65,8 +67,8 @@ __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32
 // SiLU x * sigmoid(x), GELU by its tanh form x * sigmoid(2 sqrt(2/pi) (x + 0.044715 x^3)), ReLU max(0, x).
 constexpr float kLog2e = 1.4426950408889634f, kGelu1 = 1.5957691216057308f, kGelu3 = 0.07135481282052f;
 // sigmoid(p(g)) of eight values.  The special-function unit is what bounds the epilogues (an exponential and a reciprocal
-// per value: 1024 clocks per block and SM, the products 768), so two values share a reciprocal: 1/x = y / (xy).  Where the
-// exponentials are too large for that (2^63: g below -43 or so), and for NaN, which would reach the other value, each has
+// per value: 1024 clocks per block and SM, the products 768), so four values share a reciprocal: 1/x = y / (xy).  Where the
+// exponentials are too large for that (2^31: g below -21 or so), and for NaN, which would reach the other values, each has
 // its own.
 template <int ACT>
 __device__ __forceinline__ void sigmoid8(const float* g, float* s) {
@@ -82,11 +84,15 @@ __device__ __forceinline__ void sigmoid8(const float* g, float* s) {
         asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(e[i]));
         asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(e[i + 1]));
         split(add2(pair(ex2(e[i]), ex2(e[i + 1])), pair(1.f, 1.f)), d[i], d[i + 1]);
-        const float r = rcp(d[i] * d[i + 1]);
-        s[i] = r * d[i + 1];
-        s[i + 1] = r * d[i];
     }
-    if (!(top <= 63.f)) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        const float d01 = d[i] * d[i + 1], d23 = d[i + 2] * d[i + 3], r = rcp(d01 * d23);
+        const Pair r01 = mul2(pair(r, r), pair(d23, d23)), r23 = mul2(pair(r, r), pair(d01, d01));
+        split(mul2(r01, pair(d[i + 1], d[i])), s[i], s[i + 1]);
+        split(mul2(r23, pair(d[i + 3], d[i + 2])), s[i + 2], s[i + 3]);
+    }
+    if (!(top <= 31.f)) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] = rcp(1.f + ex2(e[i]));
     }
@@ -177,6 +183,10 @@ __device__ __forceinline__ void load_gu(const CUtensorMap* wg, const CUtensorMap
 __device__ __forceinline__ void load_tile(const CUtensorMap* map, uint32_t dst, int row0, uint32_t bar) {
     for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kHalfBytes, map, h * 64, row0, bar);
 }
+__device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int row0) {
+    for (int h = 0; h < 2; ++h)
+        asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(h * 64), "r"(row0) : "memory");
+}
 // d = A B^T over 128 inputs, both K-major in two panels of 64
 __device__ __forceinline__ void product_128(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
 #pragma unroll
@@ -191,7 +201,7 @@ constexpr uint64_t kStepMn = 2048 >> 4;            // sixteen K of an MN-major o
 // forward
 // ---------------------------------------------------------------------------------------------------
 // Tensor memory: Y in columns 0..127, three G|U buffers behind it, so that the products of two blocks run ahead of the
-// epilogue of a third.  The activations of a block overwrite its G, each warp's 16 values in 8 of the columns it has read.
+// epilogue of a third.  The activations of a block overwrite its G, 16 values in 8 of the columns they were computed from.
 namespace fwd {
 constexpr int kStages = 3, kBufs = 3;
 constexpr int kOffGu = 2 * kTileBytes, kOffD = kOffGu + kStages * kTileBytes, kOffBars = kOffD + kStages * kHalfBytes;
@@ -226,7 +236,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             mbar_init(bar(bars->gu_full[i]), 1); mbar_init(bar(bars->gu_empty[i]), 1);
             mbar_init(bar(bars->d_full[i]), 1); mbar_init(bar(bars->d_empty[i]), 1);
         }
-        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kEpiWarps); }
+        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kSetWarps); }
         mbar_init(bar(bars->y_full), 1); mbar_init(bar(bars->y_empty), kEpiWarps); mbar_init(bar(bars->drain), 1);
         bars->abort_flag = 0;
         mbar_fence_init();
@@ -242,35 +252,45 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     const uint32_t limit = p.poll_limit;
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ producer
+        // ------------------------------------------------------------------ Wg and Wu
         if (lane == 0) {
-            Turn x, w;
-            int armed_x = 0, armed_gu = 0, armed_d = 0;
-            bool ok = true;
-            for (int t = 0; t < tiles && ok; ++t, x.next(2)) {
-                ok = t < 2 || mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit);
-                if (!ok) break;
+            Turn w;
+            const int total = tiles * nb;
+            int c = 0, b = 0;
+            for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->gu_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
+                mbar_expect_tx(bar(bars->gu_full[w.at]), kTileBytes);
+                load_gu(&map_wg, &map_wu, base + kOffGu + w.at * kTileBytes, b, bar(bars->gu_full[w.at]));
+                if (++b == nb) b = 0;
+            }
+            // leave with no copy still landing in shared memory (these waits keep the default limit)
+            for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->gu_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+        }
+    } else if (warp == 2) {
+        // ------------------------------------------------------------------ Wd
+        if (lane == 0) {
+            Turn w;
+            const int total = tiles * nb;
+            int c = 0, b = 0;
+            for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->d_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
+                mbar_expect_tx(bar(bars->d_full[w.at]), kHalfBytes);
+                tma_load_2d(base + kOffD + w.at * kHalfBytes, &map_wd, b * kBlock, 0, bar(bars->d_full[w.at]));
+                if (++b == nb) b = 0;
+            }
+            for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->d_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+        }
+    } else if (warp == 3) {
+        // ------------------------------------------------------------------ X
+        if (lane == 0) {
+            Turn x;
+            int t = 0;
+            for (; t < tiles && !*abort_flag; ++t, x.next(2)) {
+                if (t >= 2 && !mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
                 mbar_expect_tx(bar(bars->x_full[x.at]), kTileBytes);
                 load_tile(&map_x, base + x.at * kTileBytes, ((int)blockIdx.x + t * (int)gridDim.x) * kTileM, bar(bars->x_full[x.at]));
-                ++armed_x;
-                for (int b = 0; b < nb && ok; ++b, w.next(kStages)) {
-                    ok = !*abort_flag && (armed_gu < kStages || mbar_wait_relaxed(bar(bars->gu_empty[w.at]), w.odd ^ 1u, limit));
-                    if (!ok) break;
-                    mbar_expect_tx(bar(bars->gu_full[w.at]), kTileBytes);
-                    load_gu(&map_wg, &map_wu, base + kOffGu + w.at * kTileBytes, b, bar(bars->gu_full[w.at]));
-                    ++armed_gu;
-                    ok = armed_d < kStages || mbar_wait_relaxed(bar(bars->d_empty[w.at]), w.odd ^ 1u, limit);
-                    if (!ok) break;
-                    mbar_expect_tx(bar(bars->d_full[w.at]), kHalfBytes);
-                    tma_load_2d(base + kOffD + w.at * kHalfBytes, &map_wd, b * kBlock, 0, bar(bars->d_full[w.at]));
-                    ++armed_d;
-                }
             }
-            if (!ok) raise_timeout(bars, p.status);
-            // leave with no copy still landing in shared memory (these waits keep the default limit)
-            for (int i = max(0, armed_x - 2); i < armed_x; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
-            for (int i = max(0, armed_gu - kStages); i < armed_gu; ++i) mbar_wait(bar(bars->gu_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
-            for (int i = max(0, armed_d - kStages); i < armed_d; ++i) mbar_wait(bar(bars->d_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+            for (int i = max(0, t - 2); i < t; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
@@ -315,60 +335,35 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         mbar_wait_warp(bar(bars->drain), 0);
     } else {
         // ------------------------------------------------------------------ epilogue
-        // 32 rows, and which 16 columns of a block (of Y: which 32)
-        const int quad = warp & 3, part = (warp - 2) >> 2;
+        // Two sets of warps take the blocks in turn, so that one computes while the other waits.  A warp has 32 rows and 32 of
+        // a block's 64 columns (and 32 of Y's 128).  A tile's Y is taken after the next tile's first block: its last
+        // product has long been done then.
+        const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1, y_part = ew >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        Turn x, buf;
+        const uint32_t stage_at = base + ew * 2048;                  // in X's place: rows of 64 bytes, 64-byte swizzle
+        Turn buf;
         uint32_t y_odd = 0;
-        bool ok = true, stored = false;
-        for (int t = 0; t < tiles && ok; ++t, x.next(2)) {
+        bool ok = true;
+        int turn = set;                                              // 0: the next block is this set's
+        // Y of tile t: X's products are done, so its place stages the rows
+        auto finish = [&](int t) {
             const int row0 = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM + quad * 32;
-            for (int b = 0; b < nb; ++b, buf.next(kBufs)) {
-                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * 128 + part * kEl);
-                uint32_t g[kEl], u[kEl], a[kEl / 2];
-                tmem_ld_32x16(at, g);
-                tmem_ld_32x16(at + 64, u);
-                tmem_ld_wait();
-                gated<ACT>(g, u, a);
-                const int valid = p.d_ff - b * kBlock - part * kEl;  // hidden units past the last: zero
-                if (valid < kEl) {
-#pragma unroll
-                    for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) a[i] = 0u;
-                }
-                tmem_st_32x8(at, a);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(bar(bars->a_ready[buf.at]));
-                    if (stored && b == 0) {                          // the tile before has left its staging rows
-                        bulk_wait_read0();
-                        mbar_arrive(bar(bars->x_empty[x.at ^ 1]));
-                    }
-                }
-            }
-            if (!ok) break;
             uint32_t r[16];
             const bool res = p.R != nullptr && row0 + lane < p.n;
             if (res) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + part * 32 + i * 8, r + 4 * i);
+                for (int i = 0; i < 4; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + y_part * 32 + i * 8, r + 4 * i);
             }
-            ok = mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit);
-            if (!ok) break;
+            if (!mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit)) return false;
             y_odd ^= 1u;
             tc_fence_after();
             uint32_t y[32];
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 32), y);
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(y_part * 32), y);
             tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(bars->y_empty));
-            // Y's products are done, so X's are: its place stages the rows
-            const uint32_t stage = base + x.at * kTileBytes + (warp - 2) * 2048;       // rows of 64 bytes, 64-byte swizzle
+            const uint32_t stage = stage_at + (t & 1) * kTileBytes;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t o[4];
@@ -386,11 +381,60 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0 && row0 < p.n) {
-                tma_store_2d(&map_y, part * 32, row0, stage);
+                tma_store_2d(&map_y, y_part * 32, row0, stage);
                 bulk_commit();
             }
-            stored = true;
+            return true;
+        };
+        int owed = -1;                                               // the tile whose rows have not yet left their place
+        auto leave = [&]() {
+            if (owed >= 0 && lane == 0) {
+                bulk_wait_read0();
+                mbar_arrive(bar(bars->x_empty[owed & 1]));
+            }
+            owed = -1;
+        };
+        for (int t = 0; t < tiles && ok; ++t) {
+            leave();
+            bool open = t > 0;                                       // the tile before is to be finished
+            for (int b = 0; b < nb; ++b, buf.next(kBufs), turn ^= 1) {
+                if (turn) continue;
+                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * 128 + part * 32 + c * kEl);
+                    uint32_t g[kEl], u[kEl], a[kEl / 2];
+                    tmem_ld_32x16(at, g);
+                    tmem_ld_32x16(at + 64, u);
+                    tmem_ld_wait();
+                    gated<ACT>(g, u, a);
+                    const int valid = p.d_ff - b * kBlock - part * 32 - c * kEl;   // hidden units past the last: zero
+                    if (valid < kEl) {
+#pragma unroll
+                        for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) a[i] = 0u;
+                    }
+                    tmem_st_32x8(at, a);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(bars->a_ready[buf.at]));
+                leave();
+                if (open) {
+                    open = false;
+                    ok = finish(t - 1);
+                    if (!ok) break;
+                    owed = t - 1;
+                }
+            }
+            if (ok && open) {
+                ok = finish(t - 1);
+                owed = t - 1;
+            }
         }
+        ok = ok && finish(tiles - 1);
         if (!ok) raise_timeout(bars, p.status);
         if (lane == 0) bulk_wait_all();
     }
@@ -440,7 +484,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     if (threadIdx.x == 0) {
         mbar_init(bar(bars->x_full), 1); mbar_init(bar(bars->x_empty), 1);
         for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); }
-        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kEpiWarps); }
+        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kSetWarps); }
         mbar_init(bar(bars->y_full), 1); mbar_init(bar(bars->y_empty), kEpiWarps); mbar_init(bar(bars->drain), 1);
         bars->abort_flag = 0;
         mbar_fence_init();
@@ -456,34 +500,41 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const uint32_t limit = p.poll_limit;
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ producer
+        // ------------------------------------------------------------------ weights
         if (lane == 0) {
             Turn w;
-            uint32_t x_odd = 1;
-            int armed_x = 0, armed_w = 0;
-            bool ok = true;
-            for (int t = 0; t < tiles && ok; ++t, x_odd ^= 1u) {
-                ok = mbar_wait_relaxed(bar(bars->x_empty), x_odd, limit);
-                if (!ok) break;
+            const int total = tiles * nb;
+            int c = 0, b = 0;
+            for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
+                const uint32_t dst = base + kOffW + w.at * kStageBytes;
+                mbar_expect_tx(bar(bars->w_full[w.at]), kStageBytes);
+                load_gu(&map_wg, &map_wu, dst, b, bar(bars->w_full[w.at]));
+                tma_load_2d(dst + kTileBytes, &map_wd, b * kBlock, 0, bar(bars->w_full[w.at]));
+                if (++b == nb) b = 0;
+            }
+            for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->w_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+        }
+    } else if (warp == 3) {
+        // ------------------------------------------------------------------ X and dY
+        if (lane == 0) {
+            int t = 0;
+            for (; t < tiles && !*abort_flag; ++t) {
+                if (t > 0 && !mbar_wait_relaxed(bar(bars->x_empty), (uint32_t)(t - 1) & 1u, limit)) { raise_timeout(bars, p.status); break; }
                 const int row0 = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM;
                 mbar_expect_tx(bar(bars->x_full), 2 * kTileBytes);
                 load_tile(&map_x, base, row0, bar(bars->x_full));
                 load_tile(&map_dy, base + kTileBytes, row0, bar(bars->x_full));
-                ++armed_x;
-                for (int b = 0; b < nb && ok; ++b, w.next(kStages)) {
-                    ok = !*abort_flag && (armed_w < kStages || mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit));
-                    if (!ok) break;
-                    const uint32_t dst = base + kOffW + w.at * kStageBytes;
-                    mbar_expect_tx(bar(bars->w_full[w.at]), kStageBytes);
-                    load_gu(&map_wg, &map_wu, dst, b, bar(bars->w_full[w.at]));
-                    tma_load_2d(dst + kTileBytes, &map_wd, b * kBlock, 0, bar(bars->w_full[w.at]));
-                    ++armed_w;
+                if (t + 1 < tiles) {                                 // the next tile's rows into L2 meanwhile
+                    const int next = row0 + (int)gridDim.x * kTileM;
+                    prefetch_tile(&map_x, next);
+                    prefetch_tile(&map_dy, next);
                 }
             }
-            if (!ok) raise_timeout(bars, p.status);
-            if (armed_x > 0) mbar_wait(bar(bars->x_full), (uint32_t)(armed_x - 1) & 1u);
-            for (int i = max(0, armed_w - kStages); i < armed_w; ++i) mbar_wait(bar(bars->w_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+            if (t > 0) mbar_wait(bar(bars->x_full), (uint32_t)(t - 1) & 1u);
         }
+    } else if (warp == 2) {
+        // (no part in this kernel)
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
@@ -530,43 +581,20 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         mbar_wait_warp(bar(bars->drain), 0);
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int quad = warp & 3, part = (warp - 2) >> 2;
+        // as in the forward kernel: two sets of warps, dX of a tile after the next one's first block
+        const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1, y_part = ew >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         Turn buf;
         uint32_t y_odd = 0;
         bool ok = true;
-        for (int t = 0; t < tiles && ok; ++t) {
+        int turn = set;
+        auto finish = [&](int t) {
             const int row = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM + quad * 32 + lane;
-            for (int b = 0; b < nb; ++b, buf.next(kBufs)) {
-                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * kBufCols + part * kEl);
-                uint32_t g[kEl], u[kEl], h[kEl], dg[kEl / 2], du[kEl / 2];
-                tmem_ld_32x16(at, g);
-                tmem_ld_32x16(at + 64, u);
-                tmem_ld_32x16(at + 128, h);
-                tmem_ld_wait();
-                gated_bwd<ACT, false>(g, u, h, dg, du, nullptr);
-                const int valid = p.d_ff - b * kBlock - part * kEl;
-                if (valid < kEl) {
-#pragma unroll
-                    for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) dg[i] = du[i] = 0u;
-                }
-                tmem_st_32x8(at, dg);
-                tmem_st_32x8(at + 64, du);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(bars->a_ready[buf.at]));
-            }
-            if (!ok) break;
-            ok = mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit);
-            if (!ok) break;
+            if (!mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit)) return false;
             y_odd ^= 1u;
             tc_fence_after();
             uint32_t y[32];
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 32), y);
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(y_part * 32), y);
             tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
@@ -577,11 +605,49 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     uint32_t o[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
-                    st_global_v4(p.out + (int64_t)row * p.ldo + part * 32 + i * 8, o);
+                    st_global_v4(p.out + (int64_t)row * p.ldo + y_part * 32 + i * 8, o);
                 }
             }
             __syncwarp();
+            return true;
+        };
+        for (int t = 0; t < tiles && ok; ++t) {
+            bool open = t > 0;
+            for (int b = 0; b < nb; ++b, buf.next(kBufs), turn ^= 1) {
+                if (turn) continue;
+                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * kBufCols + part * 32 + c * kEl);
+                    uint32_t g[kEl], u[kEl], h[kEl], dg[kEl / 2], du[kEl / 2];
+                    tmem_ld_32x16(at, g);
+                    tmem_ld_32x16(at + 64, u);
+                    tmem_ld_32x16(at + 128, h);
+                    tmem_ld_wait();
+                    gated_bwd<ACT, false>(g, u, h, dg, du, nullptr);
+                    const int valid = p.d_ff - b * kBlock - part * 32 - c * kEl;
+                    if (valid < kEl) {
+#pragma unroll
+                        for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) dg[i] = du[i] = 0u;
+                    }
+                    tmem_st_32x8(at, dg);
+                    tmem_st_32x8(at + 64, du);
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(bars->a_ready[buf.at]));
+                if (open) {
+                    open = false;
+                    ok = finish(t - 1);
+                    if (!ok) break;
+                }
+            }
+            if (ok && open) ok = finish(t - 1);
         }
+        ok = ok && finish(tiles - 1);
         if (!ok) raise_timeout(bars, p.status);
     }
 
@@ -669,6 +735,12 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 load_tile(&map_x, dst, row0, bar(bars->x_full[x.at]));
                 load_tile(&map_dy, dst + kTileBytes, row0, bar(bars->x_full[x.at]));
                 ++armed;
+                // the rows of two tiles on into L2: every block's CTA of the group wants them, one asks
+                const int next = row0 + 2 * groups * kTileM;
+                if (next < p.n && t % (int)gridDim.x == block) {
+                    prefetch_tile(&map_x, next);
+                    prefetch_tile(&map_dy, next);
+                }
             }
             if (!ok) raise_timeout(bars, p.status);
             mbar_wait(bar(bars->w_full), 0);
@@ -725,9 +797,9 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         else raise_timeout(bars, p.status);
         mma_commit_by(elected, bar(bars->drain));
         mbar_wait_warp(bar(bars->drain), 0);
-    } else {
+    } else if (warp >= kCtrlWarps) {
         // ------------------------------------------------------------------ epilogue
-        const int quad = warp & 3, part = (warp - 2) >> 2;
+        const int quad = warp & 3, part = (warp - kCtrlWarps) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const int valid = p.d_ff - block * kBlock - part * kEl;      // hidden units of this warp's 16 that exist
         uint32_t odd = 0;
