@@ -173,6 +173,13 @@ __device__ __forceinline__ void raise_timeout(Bars* bars, int32_t* status) {
     if (status) atomicCAS(status, 0, (int)DG4_ERR_TIMEOUT);
 }
 
+// The pair's form: the other CTA's roles are told too.
+template <class Bars>
+__device__ __forceinline__ void raise_timeout_pair(Bars* bars, int32_t* status, uint32_t rank) {
+    raise_timeout(bars, status);
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(&bars->abort_flag), rank ^ 1u)), "r"(1u) : "memory");
+}
+
 // One block's Wg and Wu: two panels of 64 inputs, each 64 rows of Wg and 64 of Wu.
 __device__ __forceinline__ void load_gu(const CUtensorMap* wg, const CUtensorMap* wu, uint32_t dst, int block, uint32_t bar) {
     for (int h = 0; h < 2; ++h) {
@@ -200,16 +207,23 @@ constexpr uint64_t kStepMn = 2048 >> 4;            // sixteen K of an MN-major o
 // ---------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------
-// Tensor memory: Y in columns 0..127, three G|U buffers behind it, so that the products of two blocks run ahead of the
-// epilogue of a third.  The activations of a block overwrite its G, 16 values in 8 of the columns they were computed from.
+// A pair of CTAs takes 256 rows.  Each fetches half of every block's weights (one Wg, the other Wu, and each half of Wd's
+// outputs), and the products read both halves: half the traffic from L2 and half the reads of shared memory per product,
+// which bound a CTA alone (48 KB of weights in, 80 KB of operands read per block: 1000 clocks, where the products take 768).
+// The CTA of rank 0 issues the products for both; rank 1's warp 1 passes on which of its loads have come.
+//
+// Tensor memory (each CTA its rows): Y in columns 0..127, three G|U buffers behind it, so that the products of two blocks
+// run ahead of the epilogue of a third.  The activations of a block overwrite its G, 16 values in 8 of the columns they were
+// computed from.
 namespace fwd {
-constexpr int kStages = 3, kBufs = 3;
-constexpr int kOffGu = 2 * kTileBytes, kOffD = kOffGu + kStages * kTileBytes, kOffBars = kOffD + kStages * kHalfBytes;
+constexpr int kStages = 6, kBufs = 3;
+constexpr int kGuBytes = kBlock * 256, kWdBytes = 64 * 128;       // this CTA's half of [Wg; Wu], and of Wd
+constexpr int kOffGu = 2 * kTileBytes, kOffD = kOffGu + kStages * kGuBytes, kOffBars = kOffD + kStages * kWdBytes;
 struct Bars {
-    uint64_t x_full[2], x_empty[2];
-    uint64_t gu_full[kStages], gu_empty[kStages], d_full[kStages], d_empty[kStages];
-    uint64_t acc_full[kBufs], a_ready[kBufs];
-    uint64_t y_full, y_empty, drain;
+    uint64_t x_full[2], x_peer[2], x_empty[2];                    // *_peer: rank 0's, rank 1's loads have come
+    uint64_t gu_full[kStages], gu_peer[kStages], gu_empty[kStages], d_full[kStages], d_peer[kStages], d_empty[kStages];
+    uint64_t acc_full[kBufs], a_ready[kBufs];                     // a_ready and y_empty: rank 0's, both CTAs arrive
+    uint64_t y_full[2], y_empty, drain;                           // y_full in turn: a set of warps may see every other tile
     uint32_t tmem_base, abort_flag;
 };
 constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;        // 1024: the base is aligned by hand
@@ -217,7 +231,7 @@ static_assert(kSmem <= kSmemLimit, "shared memory");
 }  // namespace fwd
 
 template <int ACT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_wg,
                const __grid_constant__ CUtensorMap map_wu, const __grid_constant__ CUtensorMap map_wd,
                const __grid_constant__ CUtensorMap map_y, Params p) {
@@ -227,40 +241,45 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
     const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int nb = p.n_blocks;
+    const uint32_t rank = cluster_rank();
     volatile uint32_t* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), kEpiWarps); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_peer[i]), 1); mbar_init(bar(bars->x_empty[i]), kSetWarps); }
         for (int i = 0; i < kStages; ++i) {
-            mbar_init(bar(bars->gu_full[i]), 1); mbar_init(bar(bars->gu_empty[i]), 1);
-            mbar_init(bar(bars->d_full[i]), 1); mbar_init(bar(bars->d_empty[i]), 1);
+            mbar_init(bar(bars->gu_full[i]), 1); mbar_init(bar(bars->gu_peer[i]), 1); mbar_init(bar(bars->gu_empty[i]), 1);
+            mbar_init(bar(bars->d_full[i]), 1); mbar_init(bar(bars->d_peer[i]), 1); mbar_init(bar(bars->d_empty[i]), 1);
         }
-        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kSetWarps); }
-        mbar_init(bar(bars->y_full), 1); mbar_init(bar(bars->y_empty), kEpiWarps); mbar_init(bar(bars->drain), 1);
+        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
+        mbar_init(bar(bars->y_full[0]), 1); mbar_init(bar(bars->y_full[1]), 1); mbar_init(bar(bars->y_empty), 2 * kSetWarps); mbar_init(bar(bars->drain), 1);
         bars->abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_wg); tma_prefetch_desc(&map_wu);
         tma_prefetch_desc(&map_wd); tma_prefetch_desc(&map_y);
     }
-    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    if (warp == 1) tmem_alloc_pair(smem_u32(&bars->tmem_base), 512);
     tc_fence_before();
     __syncthreads();
+    cluster_sync();                                  // the other CTA's barriers are there too
     tc_fence_after();
     const uint32_t tmem = uniform(bars->tmem_base);
-    const int tiles = (p.n_tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    const int pairs = (int)gridDim.x / 2, pair0 = (int)blockIdx.x / 2;
+    const int tiles = (p.n_tiles - pair0 + pairs - 1) / pairs, total = tiles * nb;
+    auto row_of = [&](int t) { return (pair0 + t * pairs) * 2 * kTileM + (int)rank * kTileM; };
     const uint32_t limit = p.poll_limit;
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ Wg and Wu
+        // ------------------------------------------------------------------ Wg or Wu
         if (lane == 0) {
+            const CUtensorMap* map = rank == 0 ? &map_wg : &map_wu;
             Turn w;
-            const int total = tiles * nb;
             int c = 0, b = 0;
             for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
-                if (c >= kStages && !mbar_wait_relaxed(bar(bars->gu_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
-                mbar_expect_tx(bar(bars->gu_full[w.at]), kTileBytes);
-                load_gu(&map_wg, &map_wu, base + kOffGu + w.at * kTileBytes, b, bar(bars->gu_full[w.at]));
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->gu_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
+                mbar_expect_tx(bar(bars->gu_full[w.at]), kGuBytes);
+                for (int h = 0; h < 2; ++h)
+                    tma_load_2d(base + kOffGu + w.at * kGuBytes + h * kBlock * 128, map, h * 64, b * kBlock, bar(bars->gu_full[w.at]));
                 if (++b == nb) b = 0;
             }
             // leave with no copy still landing in shared memory (these waits keep the default limit)
@@ -270,12 +289,11 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         // ------------------------------------------------------------------ Wd
         if (lane == 0) {
             Turn w;
-            const int total = tiles * nb;
             int c = 0, b = 0;
             for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
-                if (c >= kStages && !mbar_wait_relaxed(bar(bars->d_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
-                mbar_expect_tx(bar(bars->d_full[w.at]), kHalfBytes);
-                tma_load_2d(base + kOffD + w.at * kHalfBytes, &map_wd, b * kBlock, 0, bar(bars->d_full[w.at]));
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->d_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
+                mbar_expect_tx(bar(bars->d_full[w.at]), kWdBytes);
+                tma_load_2d(base + kOffD + w.at * kWdBytes, &map_wd, b * kBlock, (int)rank * 64, bar(bars->d_full[w.at]));
                 if (++b == nb) b = 0;
             }
             for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->d_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
@@ -286,102 +304,136 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             Turn x;
             int t = 0;
             for (; t < tiles && !*abort_flag; ++t, x.next(2)) {
-                if (t >= 2 && !mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
+                if (t >= 2 && !mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
                 mbar_expect_tx(bar(bars->x_full[x.at]), kTileBytes);
-                load_tile(&map_x, base + x.at * kTileBytes, ((int)blockIdx.x + t * (int)gridDim.x) * kTileM, bar(bars->x_full[x.at]));
+                load_tile(&map_x, base + x.at * kTileBytes, row_of(t), bar(bars->x_full[x.at]));
             }
             for (int i = max(0, t - 2); i < t; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
         }
+    } else if (warp == 1 && rank == 1) {
+        // ------------------------------------------------------------------ rank 1: tells rank 0 what has come
+        if (lane == 0) {
+            Turn x, w;
+            bool ok = true;
+            for (int c = 0, b = 0; c < total && ok && !*abort_flag; ++c, w.next(kStages)) {
+                if (b == 0) {
+                    ok = mbar_wait_relaxed(bar(bars->x_full[x.at]), x.odd, limit);
+                    if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->x_peer[x.at]), 0));
+                    x.next(2);
+                }
+                ok = ok && mbar_wait_relaxed(bar(bars->gu_full[w.at]), w.odd, limit);
+                if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->gu_peer[w.at]), 0));
+                ok = ok && mbar_wait_relaxed(bar(bars->d_full[w.at]), w.odd, limit);
+                if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->d_peer[w.at]), 0));
+                if (++b == nb) b = 0;
+            }
+            if (!ok) raise_timeout_pair(bars, p.status, rank);
+        }
+        __syncwarp();
+        mbar_wait_warp(bar(bars->drain), 0);             // the last arrival that rank 0's products send here
     } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer
-        const uint32_t idesc = idesc_bf16_f32(128, 128), elected = elect_one();
-        const int total = tiles * nb;
+        // ------------------------------------------------------------------ rank 0: issues the products
+        const uint32_t idesc = idesc_bf16_f32(256, 128), elected = elect_one();
         Turn x, gu, d, buf1, buf2;
         int b1 = 0, b2 = 0;                              // blocks within their tiles
         uint32_t y_odd = 1;
         bool ok = true;
+        auto both = [&](const uint64_t& mine, const uint64_t& peer, uint32_t parity) {
+            return mbar_wait_relaxed_warp(smem_u32(&mine), parity, limit) && mbar_wait_relaxed_warp(smem_u32(&peer), parity, limit);
+        };
         // First products run two blocks ahead of second ones.  (One where a tile is one block: the tile two further on
         // takes the place of X that this tile's epilogue leaves, which comes after this tile's second product.)
         const int ahead = nb == 1 ? 1 : 2;
         for (int c = 0; c < total + ahead && ok; ++c) {
             if (c < total) {
-                if (b1 == 0) ok = mbar_wait_relaxed_warp(bar(bars->x_full[x.at]), x.odd, limit);
-                ok = ok && mbar_wait_relaxed_warp(bar(bars->gu_full[gu.at]), gu.odd, limit);
+                if (b1 == 0) ok = both(bars->x_full[x.at], bars->x_peer[x.at], x.odd);
+                ok = ok && both(bars->gu_full[gu.at], bars->gu_peer[gu.at], gu.odd);
                 if (!ok) break;
                 tc_fence_after();
-                product_128(elected, tmem + 128 + buf1.at * 128, smem_desc_sw128(base + x.at * kTileBytes), smem_desc_sw128(base + kOffGu + gu.at * kTileBytes), idesc);
-                mma_commit_by(elected, bar(bars->acc_full[buf1.at]));
-                mma_commit_by(elected, bar(bars->gu_empty[gu.at]));
+                const uint64_t dx = smem_desc_sw128(base + x.at * kTileBytes), dw = smem_desc_sw128(base + kOffGu + gu.at * kGuBytes);
+                const uint32_t to = tmem + 128 + buf1.at * 128;
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    mma_pair_by(elected, to, dx + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4),
+                                dw + (uint64_t)(((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), idesc, ks > 0 ? 1u : 0u);
+                mma_commit_pair_by(elected, bar(bars->acc_full[buf1.at]));
+                mma_commit_pair_by(elected, bar(bars->gu_empty[gu.at]));
                 gu.next(kStages); buf1.next(kBufs);
                 if (++b1 == nb) { b1 = 0; x.next(2); }
             }
             if (c >= ahead) {
-                ok = mbar_wait_relaxed_warp(bar(bars->d_full[d.at]), d.odd, limit) && mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                ok = both(bars->d_full[d.at], bars->d_peer[d.at], d.odd) && mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
                 if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
                 if (!ok) break;
                 tc_fence_after();
                 const int steps = min(4, (p.d_ff - b2 * kBlock + 15) / 16);
-                const uint64_t wd = smem_desc_sw128(base + kOffD + d.at * kHalfBytes);
+                const uint64_t wd = smem_desc_sw128(base + kOffD + d.at * kWdBytes);
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks)
-                    if (ks < steps) mma_bf16_ta_by(elected, tmem, tmem + 128 + buf2.at * 128 + ks * 16, wd + ks * 2, idesc, (b2 | ks) ? 1u : 0u);
-                mma_commit_by(elected, bar(bars->d_empty[d.at]));
+                    if (ks < steps) mma_pair_ta_by(elected, tmem, tmem + 128 + buf2.at * 128 + ks * 16, wd + ks * 2, idesc, (b2 | ks) ? 1u : 0u);
+                mma_commit_pair_by(elected, bar(bars->d_empty[d.at]));
                 d.next(kStages); buf2.next(kBufs);
-                if (++b2 == nb) { b2 = 0; mma_commit_by(elected, bar(bars->y_full)); }
+                if (++b2 == nb) { b2 = 0; mma_commit_pair_by(elected, bar(bars->y_full[y_odd])); }
             }
         }
-        if (!ok) raise_timeout(bars, p.status);
-        mma_commit_by(elected, bar(bars->drain));        // tensor memory is freed below: every product must be done
+        if (!ok) raise_timeout_pair(bars, p.status, rank);
+        mma_commit_pair_by(elected, bar(bars->drain));   // tensor memory is freed below: every product must be done
         mbar_wait_warp(bar(bars->drain), 0);
     } else {
         // ------------------------------------------------------------------ epilogue
         // Two sets of warps take the blocks in turn, so that one computes while the other waits.  A warp has 32 rows and 32 of
-        // a block's 64 columns (and 32 of Y's 128).  A tile's Y is taken after the next tile's first block: its last
-        // product has long been done then.
-        const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1, y_part = ew >> 2;
+        // a block's 64 columns.  A tile's Y is taken by the set that has the next tile's first block, after that block: its
+        // last product has long been done then.
+        const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const uint32_t stage_at = base + ew * 2048;                  // in X's place: rows of 64 bytes, 64-byte swizzle
+        const uint32_t stage_at = base + part * kHalfBytes + quad * 4096;          // in X's place
+        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), 0), y_empty0 = cluster_addr(bar(bars->y_empty), 0);
         Turn buf;
-        uint32_t y_odd = 0;
         bool ok = true;
         int turn = set;                                              // 0: the next block is this set's
         // Y of tile t: X's products are done, so its place stages the rows
         auto finish = [&](int t) {
-            const int row0 = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM + quad * 32;
-            uint32_t r[16];
+            const int row0 = row_of(t) + quad * 32;
             const bool res = p.R != nullptr && row0 + lane < p.n;
-            if (res) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + y_part * 32 + i * 8, r + 4 * i);
-            }
-            if (!mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit)) return false;
-            y_odd ^= 1u;
-            tc_fence_after();
-            uint32_t y[32];
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(y_part * 32), y);
-            tmem_ld_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(bars->y_empty));
             const uint32_t stage = stage_at + (t & 1) * kTileBytes;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t o[4];
+            for (int c = 0; c < 2; ++c) {
+                uint32_t r[16];
+                if (res) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float lo = __uint_as_float(y[8 * i + 2 * e]), hi = __uint_as_float(y[8 * i + 2 * e + 1]);
-                    if (res) {
-                        lo += __uint_as_float(r[4 * i + e] << 16);
-                        hi += __uint_as_float(r[4 * i + e] & 0xffff0000u);
-                    }
-                    o[e] = pack_bf16(lo, hi);
+                    for (int i = 0; i < 4; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + part * 64 + c * 32 + i * 8, r + 4 * i);
                 }
-                st_shared_v4(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4), o);
+                if (c == 0) {
+                    if (!mbar_wait_relaxed_warp(bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
+                    tc_fence_after();
+                }
+                uint32_t y[32];
+                tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64 + c * 32), y);
+                tmem_ld_wait();
+                if (c == 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(y_empty0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float lo = __uint_as_float(y[8 * i + 2 * e]), hi = __uint_as_float(y[8 * i + 2 * e + 1]);
+                        if (res) {
+                            lo += __uint_as_float(r[4 * i + e] << 16);
+                            hi += __uint_as_float(r[4 * i + e] & 0xffff0000u);
+                        }
+                        o[e] = pack_bf16(lo, hi);
+                    }
+                    st_shared_v4(stage + sw128_offset(lane, c * 4 + i), o);
+                }
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0 && row0 < p.n) {
-                tma_store_2d(&map_y, y_part * 32, row0, stage);
+                tma_store_2d(&map_y, part * 64, row0, stage);
                 bulk_commit();
             }
             return true;
@@ -396,7 +448,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         };
         for (int t = 0; t < tiles && ok; ++t) {
             leave();
-            bool open = t > 0;                                       // the tile before is to be finished
+            bool open = t > 0 && turn == 0;                          // the tile before is this set's to finish
             for (int b = 0; b < nb; ++b, buf.next(kBufs), turn ^= 1) {
                 if (turn) continue;
                 ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
@@ -420,7 +472,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(bars->a_ready[buf.at]));
+                if (lane == 0) mbar_arrive_cluster(a_ready0 + buf.at * 8);
                 leave();
                 if (open) {
                     open = false;
@@ -429,38 +481,38 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     owed = t - 1;
                 }
             }
-            if (ok && open) {
-                ok = finish(t - 1);
-                owed = t - 1;
-            }
         }
-        ok = ok && finish(tiles - 1);
-        if (!ok) raise_timeout(bars, p.status);
+        if (ok && turn == 0) ok = finish(tiles - 1);
+        if (!ok) raise_timeout_pair(bars, p.status, rank);
         if (lane == 0) bulk_wait_all();
     }
 
     tc_fence_before();
     __syncthreads();
+    cluster_sync();                                  // no product reads this CTA's memory any more, no arrival is on its way
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc_pair(tmem, 512);
     }
 }
 
 // ---------------------------------------------------------------------------------------------------
 // backward: dX
 // ---------------------------------------------------------------------------------------------------
-// Tensor memory: dX in columns 0..127, two buffers of G | U | dA behind it.  dG overwrites G, dU overwrites U, each warp's
-// 16 values in 8 of the columns it has read.
+// Pairs of CTAs as in the forward kernel.  Of a block each fetches Wg or Wu (for G|U), its half of the inputs of both (for
+// dX) and its half of the hidden units of Wd (for dA).
+// Tensor memory: dX in columns 0..127, two buffers of G | U | dA behind it.  dG overwrites G, dU overwrites U, 16 values in 8
+// of the columns they were computed from.
 namespace dx {
-constexpr int kStages = 3, kBufs = 2, kBufCols = 192;
-constexpr int kStageBytes = kTileBytes + kHalfBytes;              // Wg and Wu, then Wd
+constexpr int kStages = 4, kBufs = 2, kBufCols = 192;
+constexpr int kGuBytes = kBlock * 256, kInBytes = 2 * kBlock * 128, kWdBytes = kTileM * 64;
+constexpr int kStageBytes = kGuBytes + kInBytes + kWdBytes;
 constexpr int kOffW = 2 * kTileBytes, kOffBars = kOffW + kStages * kStageBytes;
 struct Bars {
-    uint64_t x_full, x_empty;
-    uint64_t w_full[kStages], w_empty[kStages];
+    uint64_t x_full, x_peer, x_empty;
+    uint64_t w_full[kStages], w_peer[kStages], w_empty[kStages];
     uint64_t acc_full[kBufs], a_ready[kBufs];
-    uint64_t y_full, y_empty, drain;
+    uint64_t y_full[2], y_empty, drain;                           // y_full in turn: a set of warps may see every other tile
     uint32_t tmem_base, abort_flag;
 };
 constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;
@@ -468,7 +520,7 @@ static_assert(kSmem <= kSmemLimit, "shared memory");
 }  // namespace dx
 
 template <int ACT>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_dy,
               const __grid_constant__ CUtensorMap map_wg, const __grid_constant__ CUtensorMap map_wu,
               const __grid_constant__ CUtensorMap map_wd, Params p) {
@@ -478,39 +530,45 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
     const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int nb = p.n_blocks;
+    const uint32_t rank = cluster_rank();
     volatile uint32_t* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
 
     if (threadIdx.x == 0) {
-        mbar_init(bar(bars->x_full), 1); mbar_init(bar(bars->x_empty), 1);
-        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); }
-        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), kSetWarps); }
-        mbar_init(bar(bars->y_full), 1); mbar_init(bar(bars->y_empty), kEpiWarps); mbar_init(bar(bars->drain), 1);
+        mbar_init(bar(bars->x_full), 1); mbar_init(bar(bars->x_peer), 1); mbar_init(bar(bars->x_empty), 1);
+        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_peer[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); }
+        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
+        mbar_init(bar(bars->y_full[0]), 1); mbar_init(bar(bars->y_full[1]), 1); mbar_init(bar(bars->y_empty), 2 * kSetWarps); mbar_init(bar(bars->drain), 1);
         bars->abort_flag = 0;
         mbar_fence_init();
         tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy); tma_prefetch_desc(&map_wg); tma_prefetch_desc(&map_wu);
         tma_prefetch_desc(&map_wd);
     }
-    if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    if (warp == 1) tmem_alloc_pair(smem_u32(&bars->tmem_base), 512);
     tc_fence_before();
     __syncthreads();
+    cluster_sync();
     tc_fence_after();
     const uint32_t tmem = uniform(bars->tmem_base);
-    const int tiles = (p.n_tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    const int pairs = (int)gridDim.x / 2, pair0 = (int)blockIdx.x / 2;
+    const int tiles = (p.n_tiles - pair0 + pairs - 1) / pairs, total = tiles * nb;
+    auto row_of = [&](int t) { return (pair0 + t * pairs) * 2 * kTileM + (int)rank * kTileM; };
     const uint32_t limit = p.poll_limit;
 
     if (warp == 0) {
         // ------------------------------------------------------------------ weights
         if (lane == 0) {
+            const CUtensorMap* map = rank == 0 ? &map_wg : &map_wu;
             Turn w;
-            const int total = tiles * nb;
             int c = 0, b = 0;
             for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
-                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
-                const uint32_t dst = base + kOffW + w.at * kStageBytes;
-                mbar_expect_tx(bar(bars->w_full[w.at]), kStageBytes);
-                load_gu(&map_wg, &map_wu, dst, b, bar(bars->w_full[w.at]));
-                tma_load_2d(dst + kTileBytes, &map_wd, b * kBlock, 0, bar(bars->w_full[w.at]));
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
+                const uint32_t dst = base + kOffW + w.at * kStageBytes, full = bar(bars->w_full[w.at]);
+                mbar_expect_tx(full, kStageBytes);
+                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kBlock * 128, map, h * 64, b * kBlock, full);
+                tma_load_2d(dst + kGuBytes, &map_wg, (int)rank * 64, b * kBlock, full);
+                tma_load_2d(dst + kGuBytes + kBlock * 128, &map_wu, (int)rank * 64, b * kBlock, full);
+                tma_load_2d(dst + kGuBytes + kInBytes, &map_wd, b * kBlock + (int)rank * 32, 0, full);
                 if (++b == nb) b = 0;
             }
             for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->w_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
@@ -520,99 +578,126 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         if (lane == 0) {
             int t = 0;
             for (; t < tiles && !*abort_flag; ++t) {
-                if (t > 0 && !mbar_wait_relaxed(bar(bars->x_empty), (uint32_t)(t - 1) & 1u, limit)) { raise_timeout(bars, p.status); break; }
-                const int row0 = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM;
+                if (t > 0 && !mbar_wait_relaxed(bar(bars->x_empty), (uint32_t)(t - 1) & 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
                 mbar_expect_tx(bar(bars->x_full), 2 * kTileBytes);
-                load_tile(&map_x, base, row0, bar(bars->x_full));
-                load_tile(&map_dy, base + kTileBytes, row0, bar(bars->x_full));
+                load_tile(&map_x, base, row_of(t), bar(bars->x_full));
+                load_tile(&map_dy, base + kTileBytes, row_of(t), bar(bars->x_full));
                 if (t + 1 < tiles) {                                 // the next tile's rows into L2 meanwhile
-                    const int next = row0 + (int)gridDim.x * kTileM;
-                    prefetch_tile(&map_x, next);
-                    prefetch_tile(&map_dy, next);
+                    prefetch_tile(&map_x, row_of(t + 1));
+                    prefetch_tile(&map_dy, row_of(t + 1));
                 }
             }
             if (t > 0) mbar_wait(bar(bars->x_full), (uint32_t)(t - 1) & 1u);
         }
     } else if (warp == 2) {
         // (no part in this kernel)
+    } else if (warp == 1 && rank == 1) {
+        // ------------------------------------------------------------------ rank 1: tells rank 0 what has come
+        if (lane == 0) {
+            Turn w;
+            uint32_t x_odd = 0;
+            bool ok = true;
+            for (int c = 0, b = 0; c < total && ok && !*abort_flag; ++c, w.next(kStages)) {
+                if (b == 0) {
+                    ok = mbar_wait_relaxed(bar(bars->x_full), x_odd, limit);
+                    if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->x_peer), 0));
+                    x_odd ^= 1u;
+                }
+                ok = ok && mbar_wait_relaxed(bar(bars->w_full[w.at]), w.odd, limit);
+                if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->w_peer[w.at]), 0));
+                if (++b == nb) b = 0;
+            }
+            if (!ok) raise_timeout_pair(bars, p.status, rank);
+        }
+        __syncwarp();
+        mbar_wait_warp(bar(bars->drain), 0);             // the last arrival that rank 0's products send here
     } else if (warp == 1) {
-        // ------------------------------------------------------------------ MMA issuer
-        const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
-                       id_dx = idesc_bf16_f32(128, 128) | kIdescBMn, elected = elect_one();
-        const int total = tiles * nb;
+        // ------------------------------------------------------------------ rank 0: issues the products
+        const uint32_t id_gu = idesc_bf16_f32(256, 128), id_da = idesc_bf16_f32(256, 64) | kIdescBMn,
+                       id_dx = idesc_bf16_f32(256, 128) | kIdescBMn, elected = elect_one();
         Turn w1, w2, buf1, buf2;
         int b1 = 0, b2 = 0;
         uint32_t x_odd = 0, y_odd = 1;
         bool ok = true;
         const uint64_t desc_x = smem_desc_sw128(base), desc_dy = smem_desc_sw128(base + kTileBytes);
+        auto both = [&](const uint64_t& mine, const uint64_t& peer, uint32_t parity) {
+            return mbar_wait_relaxed_warp(smem_u32(&mine), parity, limit) && mbar_wait_relaxed_warp(smem_u32(&peer), parity, limit);
+        };
         for (int c = 0; c < total + 1 && ok; ++c) {
             if (c < total) {
-                if (b1 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->x_full), x_odd, limit); x_odd ^= 1u; }
-                ok = ok && mbar_wait_relaxed_warp(bar(bars->w_full[w1.at]), w1.odd, limit);
+                if (b1 == 0) { ok = both(bars->x_full, bars->x_peer, x_odd); x_odd ^= 1u; }
+                ok = ok && both(bars->w_full[w1.at], bars->w_peer[w1.at], w1.odd);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t w = base + kOffW + w1.at * kStageBytes, d = tmem + 128 + buf1.at * kBufCols;
-                product_128(elected, d, desc_x, smem_desc_sw128(w), id_gu);
-                const uint64_t wd = smem_desc_sw128_mn(w + kTileBytes, kHalfBytes);
+                const uint64_t gu = smem_desc_sw128(w), wd = smem_desc_sw64_mn(w + kGuBytes + kInBytes);
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    mma_pair_by(elected, d, desc_x + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4),
+                                gu + (uint64_t)(((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), id_gu, ks > 0 ? 1u : 0u);
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)                       // dA = dY Wd: Wd's rows run along K
-                    mma_bf16_by(elected, d + 128, desc_dy + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), wd + ks * kStepMn, id_da, ks > 0 ? 1u : 0u);
-                mma_commit_by(elected, bar(bars->acc_full[buf1.at]));
+                    mma_pair_by(elected, d + 128, desc_dy + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), wd + ks * (1024 >> 4), id_da, ks > 0 ? 1u : 0u);
+                mma_commit_pair_by(elected, bar(bars->acc_full[buf1.at]));
                 w1.next(kStages); buf1.next(kBufs);
-                if (++b1 == nb) { b1 = 0; mma_commit_by(elected, bar(bars->x_empty)); }
+                if (++b1 == nb) { b1 = 0; mma_commit_pair_by(elected, bar(bars->x_empty)); }
             }
             if (c >= 1) {
                 ok = mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
                 if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t w = smem_desc_sw128_mn(base + kOffW + w2.at * kStageBytes, kHalfBytes);
+                const uint64_t w = smem_desc_sw128_mn(base + kOffW + w2.at * kStageBytes + kGuBytes, kHalfBytes);
                 const uint32_t a = tmem + 128 + buf2.at * kBufCols;
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)                       // dX += [dG | dU] [Wg; Wu]: their rows run along K
-                    mma_bf16_ta_by(elected, tmem, a + ks * 16, w + ks * kStepMn, id_dx, (b2 | ks) ? 1u : 0u);
-                mma_commit_by(elected, bar(bars->w_empty[w2.at]));
+                    mma_pair_ta_by(elected, tmem, a + ks * 16, w + ks * kStepMn, id_dx, (b2 | ks) ? 1u : 0u);
+                mma_commit_pair_by(elected, bar(bars->w_empty[w2.at]));
                 w2.next(kStages); buf2.next(kBufs);
-                if (++b2 == nb) { b2 = 0; mma_commit_by(elected, bar(bars->y_full)); }
+                if (++b2 == nb) { b2 = 0; mma_commit_pair_by(elected, bar(bars->y_full[y_odd])); }
             }
         }
-        if (!ok) raise_timeout(bars, p.status);
-        mma_commit_by(elected, bar(bars->drain));
+        if (!ok) raise_timeout_pair(bars, p.status, rank);
+        mma_commit_pair_by(elected, bar(bars->drain));
         mbar_wait_warp(bar(bars->drain), 0);
     } else {
         // ------------------------------------------------------------------ epilogue
         // as in the forward kernel: two sets of warps, dX of a tile after the next one's first block
-        const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1, y_part = ew >> 2;
+        const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), 0), y_empty0 = cluster_addr(bar(bars->y_empty), 0);
         Turn buf;
-        uint32_t y_odd = 0;
         bool ok = true;
         int turn = set;
         auto finish = [&](int t) {
-            const int row = ((int)blockIdx.x + t * (int)gridDim.x) * kTileM + quad * 32 + lane;
-            if (!mbar_wait_relaxed_warp(bar(bars->y_full), y_odd, limit)) return false;
-            y_odd ^= 1u;
+            const int row = row_of(t) + quad * 32 + lane;
+            if (!mbar_wait_relaxed_warp(bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
             tc_fence_after();
-            uint32_t y[32];
-            tmem_ld_32x32(tmem + lanes + (uint32_t)(y_part * 32), y);
-            tmem_ld_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(bars->y_empty));
-            if (row < p.n) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t o[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
-                    st_global_v4(p.out + (int64_t)row * p.ldo + y_part * 32 + i * 8, o);
+            for (int c = 0; c < 2; ++c) {
+                uint32_t y[32];
+                tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64 + c * 32), y);
+                tmem_ld_wait();
+                if (c == 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(y_empty0);
                 }
+                if (row < p.n) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
+                        st_global_v4(p.out + (int64_t)row * p.ldo + part * 64 + c * 32 + i * 8, o);
+                    }
+                }
+                __syncwarp();
             }
-            __syncwarp();
             return true;
         };
         for (int t = 0; t < tiles && ok; ++t) {
-            bool open = t > 0;
+            bool open = t > 0 && turn == 0;
             for (int b = 0; b < nb; ++b, buf.next(kBufs), turn ^= 1) {
                 if (turn) continue;
                 ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
@@ -638,24 +723,24 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(bars->a_ready[buf.at]));
+                if (lane == 0) mbar_arrive_cluster(a_ready0 + buf.at * 8);
                 if (open) {
                     open = false;
                     ok = finish(t - 1);
                     if (!ok) break;
                 }
             }
-            if (ok && open) ok = finish(t - 1);
         }
-        ok = ok && finish(tiles - 1);
-        if (!ok) raise_timeout(bars, p.status);
+        if (ok && turn == 0) ok = finish(tiles - 1);
+        if (!ok) raise_timeout_pair(bars, p.status, rank);
     }
 
     tc_fence_before();
     __syncthreads();
+    cluster_sync();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc_pair(tmem, 512);
     }
 }
 
@@ -911,7 +996,7 @@ dg4_status allow_smem(int dev, int bytes) {
     return DG4_OK;
 }
 
-struct Maps { CUtensorMap x, dy, wg, wu, wd, y; };
+struct Maps { CUtensorMap x, dy, wg, wu, wd, y, wd_half; };
 
 int blocks_of(int d_ff) { return (d_ff + kBlock - 1) / kBlock; }
 // Row groups of glu_dw_kernel: as many as the device has SMs for, and no more than there are tiles.
@@ -929,17 +1014,20 @@ dg4_status check_weights(const void* wg, const void* wu, const void* wd, int32_t
     return DG4_OK;
 }
 
-dg4_status weight_maps(Maps* m, const void* wg, const void* wu, const void* wd, int d_ff) {
+dg4_status weight_maps(Maps* m, const void* wg, const void* wu, const void* wd, int d_ff, int wd_rows) {
     CHECK(dg4i_make_row_map(&m->wg, wg, d_ff, 128, kBlock));
     CHECK(dg4i_make_row_map(&m->wu, wu, d_ff, 128, kBlock));
-    CHECK(dg4i_make_map(&m->wd, wd, d_ff, 128, d_ff, 128, 64));
+    CHECK(dg4i_make_map(&m->wd, wd, d_ff, 128, d_ff, wd_rows, 64));
     return DG4_OK;
 }
+
+// CTAs of a kernel that works in pairs; n_tiles counts pairs of tiles
+int pair_grid(const Params& p, int sms) { return 2 * (p.n_tiles < sms / 2 ? p.n_tiles : sms / 2); }
 
 template <int ACT>
 dg4_status launch_fwd(const Maps& m, const Params& p, int dev, int sms, cudaStream_t st) {
     CHECK(allow_smem<glu_fwd_kernel<ACT>>(dev, fwd::kSmem));
-    glu_fwd_kernel<ACT><<<p.n_tiles < sms ? p.n_tiles : sms, kThreads, fwd::kSmem, st>>>(m.x, m.wg, m.wu, m.wd, m.y, p);
+    glu_fwd_kernel<ACT><<<pair_grid(p, sms), kThreads, fwd::kSmem, st>>>(m.x, m.wg, m.wu, m.wd, m.y, p);
     dg4i_count_launch();
     DG4_CUDA_TRY(cudaGetLastError());
     return DG4_OK;
@@ -949,7 +1037,9 @@ template <int ACT>
 dg4_status launch_bwd(const Maps& m, const Params& p, const DwOut& out, int groups, int dev, int sms, cudaStream_t st) {
     if (p.out) {
         CHECK(allow_smem<glu_dx_kernel<ACT>>(dev, dx::kSmem));
-        glu_dx_kernel<ACT><<<p.n_tiles < sms ? p.n_tiles : sms, kThreads, dx::kSmem, st>>>(m.x, m.dy, m.wg, m.wu, m.wd, p);
+        Params q = p;
+        q.n_tiles = (p.n_tiles + 1) / 2;
+        glu_dx_kernel<ACT><<<pair_grid(q, sms), kThreads, dx::kSmem, st>>>(m.x, m.dy, m.wg, m.wu, m.wd_half, q);
         dg4i_count_launch();
         DG4_CUDA_TRY(cudaGetLastError());
     }
@@ -990,10 +1080,11 @@ extern "C" dg4_status dg4_glu_fwd(const dg4_graph* g, const dg4_desc* desc, cons
     int sms;
     CHECK(sm_count(g->device, &sms));
     Maps m;
-    CHECK(weight_maps(&m, W_gate, W_up, W_down, d_ff));
+    CHECK(weight_maps(&m, W_gate, W_up, W_down, d_ff, 64));
     CHECK(dg4i_make_row_map(&m.x, X, g->n, ldx, kTileM));
-    CHECK(dg4i_make_map(&m.y, Y, 128, g->n, ldy, 32, 32));
+    CHECK(dg4i_make_row_map(&m.y, Y, g->n, ldy, 32));
     Params p = make_params(g, d_ff);
+    p.n_tiles = (p.n_tiles + 1) / 2;
     p.R = res ? (const __nv_bfloat16*)H_res : nullptr; p.ldr = ldh;
     const cudaStream_t st = (cudaStream_t)stream;
     if (activation == DG4_ACT_SILU) return launch_fwd<DG4_ACT_SILU>(m, p, g->device, sms, st);
@@ -1038,7 +1129,8 @@ extern "C" dg4_status dg4_glu_bwd(const dg4_graph* g, const dg4_desc* desc, cons
         out.wg = (__nv_bfloat16*)dW_gate; out.wu = (__nv_bfloat16*)dW_up; out.wd = (__nv_bfloat16*)dW_down;
     }
     Maps m;
-    CHECK(weight_maps(&m, W_gate, W_up, W_down, d_ff));
+    CHECK(weight_maps(&m, W_gate, W_up, W_down, d_ff, 128));
+    CHECK(dg4i_make_map(&m.wd_half, W_down, d_ff, 128, d_ff, 128, 32));
     CHECK(dg4i_make_row_map(&m.x, X, g->n, ldx, kTileM));
     CHECK(dg4i_make_row_map(&m.dy, dY, g->n, lddy, kTileM));
     Params p = make_params(g, d_ff);
