@@ -218,12 +218,14 @@ constexpr uint64_t kStepMn = 2048 >> 4;            // sixteen K of an MN-major o
 namespace fwd {
 constexpr int kStages = 6, kBufs = 3;
 constexpr int kGuBytes = kBlock * 256, kWdBytes = 64 * 128;       // this CTA's half of [Wg; Wu], and of Wd
-constexpr int kOffGu = 2 * kTileBytes, kOffD = kOffGu + kStages * kGuBytes, kOffBars = kOffD + kStages * kWdBytes;
+constexpr int kStageBytes = kGuBytes + kWdBytes, kOffW = 2 * kTileBytes, kOffBars = kOffW + kStages * kStageBytes;
 struct Bars {
-    uint64_t x_full[2], x_peer[2], x_empty[2];                    // *_peer: rank 0's, rank 1's loads have come
-    uint64_t gu_full[kStages], gu_peer[kStages], gu_empty[kStages], d_full[kStages], d_peer[kStages], d_empty[kStages];
-    uint64_t acc_full[kBufs], a_ready[kBufs];                     // a_ready and y_empty: rank 0's, both CTAs arrive
-    uint64_t y_full[2], y_empty, drain;                           // y_full in turn: a set of warps may see every other tile
+    uint64_t x_full[2], x_empty[2], w_full[kStages], w_empty[kStages];
+    // rank 0's, both CTAs arrive: a block's weights have come (for a tile's first block X too), its activations are there, Y
+    // has been read
+    uint64_t ready[kStages], a_ready[kBufs], y_empty;
+    uint64_t acc_full[kBufs];
+    uint64_t y_full[2], drain;                                    // y_full in turn: a set of warps may see every other tile
     uint32_t tmem_base, abort_flag;
 };
 constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;        // 1024: the base is aligned by hand
@@ -246,11 +248,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_peer[i]), 1); mbar_init(bar(bars->x_empty[i]), kSetWarps); }
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(bar(bars->gu_full[i]), 1); mbar_init(bar(bars->gu_peer[i]), 1); mbar_init(bar(bars->gu_empty[i]), 1);
-            mbar_init(bar(bars->d_full[i]), 1); mbar_init(bar(bars->d_peer[i]), 1); mbar_init(bar(bars->d_empty[i]), 1);
-        }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), kSetWarps); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); mbar_init(bar(bars->ready[i]), 2); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
         mbar_init(bar(bars->y_full[0]), 1); mbar_init(bar(bars->y_full[1]), 1); mbar_init(bar(bars->y_empty), 2 * kSetWarps); mbar_init(bar(bars->drain), 1);
         bars->abort_flag = 0;
@@ -270,33 +269,38 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     const uint32_t limit = p.poll_limit;
 
     if (warp == 0) {
-        // ------------------------------------------------------------------ Wg or Wu
+        // ------------------------------------------------------------------ weights: Wg or Wu, half of Wd's outputs
         if (lane == 0) {
             const CUtensorMap* map = rank == 0 ? &map_wg : &map_wu;
             Turn w;
             int c = 0, b = 0;
             for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
-                if (c >= kStages && !mbar_wait_relaxed(bar(bars->gu_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
-                mbar_expect_tx(bar(bars->gu_full[w.at]), kGuBytes);
-                for (int h = 0; h < 2; ++h)
-                    tma_load_2d(base + kOffGu + w.at * kGuBytes + h * kBlock * 128, map, h * 64, b * kBlock, bar(bars->gu_full[w.at]));
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
+                const uint32_t dst = base + kOffW + w.at * kStageBytes, full = bar(bars->w_full[w.at]);
+                mbar_expect_tx(full, kStageBytes);
+                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kBlock * 128, map, h * 64, b * kBlock, full);
+                tma_load_2d(dst + kGuBytes, &map_wd, b * kBlock, (int)rank * 64, full);
                 if (++b == nb) b = 0;
             }
             // leave with no copy still landing in shared memory (these waits keep the default limit)
-            for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->gu_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+            for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->w_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
         }
     } else if (warp == 2) {
-        // ------------------------------------------------------------------ Wd
+        // ------------------------------------------------------------------ tells rank 0 what has come
         if (lane == 0) {
-            Turn w;
-            int c = 0, b = 0;
-            for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
-                if (c >= kStages && !mbar_wait_relaxed(bar(bars->d_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
-                mbar_expect_tx(bar(bars->d_full[w.at]), kWdBytes);
-                tma_load_2d(base + kOffD + w.at * kWdBytes, &map_wd, b * kBlock, (int)rank * 64, bar(bars->d_full[w.at]));
+            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), 0);
+            Turn x, w;
+            bool ok = true;
+            for (int c = 0, b = 0; c < total && ok && !*abort_flag; ++c, w.next(kStages)) {
+                if (b == 0) {
+                    ok = mbar_wait_relaxed(bar(bars->x_full[x.at]), x.odd, limit);
+                    x.next(2);
+                }
+                ok = ok && mbar_wait_relaxed(bar(bars->w_full[w.at]), w.odd, limit);
+                if (ok) mbar_arrive_cluster(ready0 + w.at * 8);
                 if (++b == nb) b = 0;
             }
-            for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->d_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+            if (!ok) raise_timeout_pair(bars, p.status, rank);
         }
     } else if (warp == 3) {
         // ------------------------------------------------------------------ X
@@ -310,76 +314,50 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             }
             for (int i = max(0, t - 2); i < t; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
         }
-    } else if (warp == 1 && rank == 1) {
-        // ------------------------------------------------------------------ rank 1: tells rank 0 what has come
-        if (lane == 0) {
-            Turn x, w;
-            bool ok = true;
-            for (int c = 0, b = 0; c < total && ok && !*abort_flag; ++c, w.next(kStages)) {
-                if (b == 0) {
-                    ok = mbar_wait_relaxed(bar(bars->x_full[x.at]), x.odd, limit);
-                    if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->x_peer[x.at]), 0));
-                    x.next(2);
-                }
-                ok = ok && mbar_wait_relaxed(bar(bars->gu_full[w.at]), w.odd, limit);
-                if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->gu_peer[w.at]), 0));
-                ok = ok && mbar_wait_relaxed(bar(bars->d_full[w.at]), w.odd, limit);
-                if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->d_peer[w.at]), 0));
-                if (++b == nb) b = 0;
-            }
-            if (!ok) raise_timeout_pair(bars, p.status, rank);
-        }
-        __syncwarp();
-        mbar_wait_warp(bar(bars->drain), 0);             // the last arrival that rank 0's products send here
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ rank 0: issues the products
-        const uint32_t idesc = idesc_bf16_f32(256, 128), elected = elect_one();
-        Turn x, gu, d, buf1, buf2;
+        // The tensor cores hold some sixteen products of a pair in waiting; what this warp does between them is hidden as long
+        // as a block's issue takes less than its products, so it waits for as few barriers as can be.
+        const uint32_t idesc = idesc_bf16_f32(256, 128), elected = elect_one(), high = desc_high(smem_desc_sw128(0));
+        const uint32_t low_x = desc_low(smem_desc_sw128(base)), low_w = desc_low(smem_desc_sw128(base + kOffW));
+        Turn x, w1, w2, buf1, buf2;
         int b1 = 0, b2 = 0;                              // blocks within their tiles
         uint32_t y_odd = 1;
         bool ok = true;
-        auto both = [&](const uint64_t& mine, const uint64_t& peer, uint32_t parity) {
-            return mbar_wait_relaxed_warp(smem_u32(&mine), parity, limit) && mbar_wait_relaxed_warp(smem_u32(&peer), parity, limit);
-        };
         // First products run two blocks ahead of second ones.  (One where a tile is one block: the tile two further on
         // takes the place of X that this tile's epilogue leaves, which comes after this tile's second product.)
         const int ahead = nb == 1 ? 1 : 2;
         for (int c = 0; c < total + ahead && ok; ++c) {
             if (c < total) {
-                if (b1 == 0) ok = both(bars->x_full[x.at], bars->x_peer[x.at], x.odd);
-                ok = ok && both(bars->gu_full[gu.at], bars->gu_peer[gu.at], gu.odd);
+                ok = mbar_wait_relaxed_warp(bar(bars->ready[w1.at]), w1.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t dx = smem_desc_sw128(base + x.at * kTileBytes), dw = smem_desc_sw128(base + kOffGu + gu.at * kGuBytes);
-                const uint32_t to = tmem + 128 + buf1.at * 128;
+                const uint32_t dx = low_x + x.at * (kTileBytes >> 4), dw = low_w + w1.at * (kStageBytes >> 4), to = tmem + 128 + buf1.at * 128;
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
-                    mma_pair_by(elected, to, dx + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4),
-                                dw + (uint64_t)(((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), idesc, ks > 0 ? 1u : 0u);
+                    mma_pair_by(elected, to, dx + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
+                                dw + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, idesc, ks > 0 ? 1u : 0u);
                 mma_commit_pair_by(elected, bar(bars->acc_full[buf1.at]));
-                mma_commit_pair_by(elected, bar(bars->gu_empty[gu.at]));
-                gu.next(kStages); buf1.next(kBufs);
+                w1.next(kStages); buf1.next(kBufs);
                 if (++b1 == nb) { b1 = 0; x.next(2); }
             }
             if (c >= ahead) {
-                ok = both(bars->d_full[d.at], bars->d_peer[d.at], d.odd) && mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                ok = mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
                 if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
                 if (!ok) break;
                 tc_fence_after();
-                const int steps = min(4, (p.d_ff - b2 * kBlock + 15) / 16);
-                const uint64_t wd = smem_desc_sw128(base + kOffD + d.at * kWdBytes);
+                const uint32_t wd = low_w + ((w2.at * kStageBytes + kGuBytes) >> 4), a = tmem + 128 + buf2.at * 128;
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
-                    if (ks < steps) mma_pair_ta_by(elected, tmem, tmem + 128 + buf2.at * 128 + ks * 16, wd + ks * 2, idesc, (b2 | ks) ? 1u : 0u);
-                mma_commit_pair_by(elected, bar(bars->d_empty[d.at]));
-                d.next(kStages); buf2.next(kBufs);
+                for (int ks = 0; ks < 4; ++ks) mma_pair_ta_by(elected, tmem, a + ks * 16, wd + ks * 2, high, idesc, (b2 | ks) ? 1u : 0u);
+                mma_commit_pair_by(elected, bar(bars->w_empty[w2.at]));
+                w2.next(kStages); buf2.next(kBufs);
                 if (++b2 == nb) { b2 = 0; mma_commit_pair_by(elected, bar(bars->y_full[y_odd])); }
             }
         }
         if (!ok) raise_timeout_pair(bars, p.status, rank);
         mma_commit_pair_by(elected, bar(bars->drain));   // tensor memory is freed below: every product must be done
         mbar_wait_warp(bar(bars->drain), 0);
-    } else {
+    } else if (warp >= kCtrlWarps) {
         // ------------------------------------------------------------------ epilogue
         // Two sets of warps take the blocks in turn, so that one computes while the other waits.  A warp has 32 rows and 32 of
         // a block's 64 columns.  A tile's Y is taken by the set that has the next tile's first block, after that block: its
@@ -489,6 +467,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 
     tc_fence_before();
     __syncthreads();
+    if (warp == 1 && rank == 1) mbar_wait_warp(bar(bars->drain), 0);   // the last arrival that rank 0's products send here
     cluster_sync();                                  // no product reads this CTA's memory any more, no arrival is on its way
     if (warp == 1) {
         tc_fence_after();
@@ -509,10 +488,9 @@ constexpr int kGuBytes = kBlock * 256, kInBytes = 2 * kBlock * 128, kWdBytes = k
 constexpr int kStageBytes = kGuBytes + kInBytes + kWdBytes;
 constexpr int kOffW = 2 * kTileBytes, kOffBars = kOffW + kStages * kStageBytes;
 struct Bars {
-    uint64_t x_full, x_peer, x_empty;
-    uint64_t w_full[kStages], w_peer[kStages], w_empty[kStages];
-    uint64_t acc_full[kBufs], a_ready[kBufs];
-    uint64_t y_full[2], y_empty, drain;                           // y_full in turn: a set of warps may see every other tile
+    uint64_t x_full, x_empty, w_full[kStages], w_empty[kStages];
+    uint64_t ready[kStages], a_ready[kBufs], y_empty;             // rank 0's, both CTAs arrive
+    uint64_t acc_full[kBufs], y_full[2], drain;
     uint32_t tmem_base, abort_flag;
 };
 constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;
@@ -535,8 +513,8 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
 
     if (threadIdx.x == 0) {
-        mbar_init(bar(bars->x_full), 1); mbar_init(bar(bars->x_peer), 1); mbar_init(bar(bars->x_empty), 1);
-        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_peer[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); }
+        mbar_init(bar(bars->x_full), 1); mbar_init(bar(bars->x_empty), 1);
+        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); mbar_init(bar(bars->ready[i]), 2); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
         mbar_init(bar(bars->y_full[0]), 1); mbar_init(bar(bars->y_full[1]), 1); mbar_init(bar(bars->y_empty), 2 * kSetWarps); mbar_init(bar(bars->drain), 1);
         bars->abort_flag = 0;
@@ -590,54 +568,48 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             if (t > 0) mbar_wait(bar(bars->x_full), (uint32_t)(t - 1) & 1u);
         }
     } else if (warp == 2) {
-        // (no part in this kernel)
-    } else if (warp == 1 && rank == 1) {
-        // ------------------------------------------------------------------ rank 1: tells rank 0 what has come
+        // ------------------------------------------------------------------ tells rank 0 what has come
         if (lane == 0) {
+            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), 0);
             Turn w;
             uint32_t x_odd = 0;
             bool ok = true;
             for (int c = 0, b = 0; c < total && ok && !*abort_flag; ++c, w.next(kStages)) {
                 if (b == 0) {
                     ok = mbar_wait_relaxed(bar(bars->x_full), x_odd, limit);
-                    if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->x_peer), 0));
                     x_odd ^= 1u;
                 }
                 ok = ok && mbar_wait_relaxed(bar(bars->w_full[w.at]), w.odd, limit);
-                if (ok) mbar_arrive_cluster(cluster_addr(bar(bars->w_peer[w.at]), 0));
+                if (ok) mbar_arrive_cluster(ready0 + w.at * 8);
                 if (++b == nb) b = 0;
             }
             if (!ok) raise_timeout_pair(bars, p.status, rank);
         }
-        __syncwarp();
-        mbar_wait_warp(bar(bars->drain), 0);             // the last arrival that rank 0's products send here
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ rank 0: issues the products
         const uint32_t id_gu = idesc_bf16_f32(256, 128), id_da = idesc_bf16_f32(256, 64) | kIdescBMn,
                        id_dx = idesc_bf16_f32(256, 128) | kIdescBMn, elected = elect_one();
+        const uint32_t high = desc_high(smem_desc_sw128(0)), high_wd = desc_high(smem_desc_sw64_mn(0));
+        const uint32_t low_x = desc_low(smem_desc_sw128(base)), low_dy = low_x + (kTileBytes >> 4), low_gu = desc_low(smem_desc_sw128(base + kOffW)),
+                       low_in = desc_low(smem_desc_sw128_mn(base + kOffW + kGuBytes, kHalfBytes)), low_wd = desc_low(smem_desc_sw64_mn(base + kOffW + kGuBytes + kInBytes));
         Turn w1, w2, buf1, buf2;
         int b1 = 0, b2 = 0;
-        uint32_t x_odd = 0, y_odd = 1;
+        uint32_t y_odd = 1;
         bool ok = true;
-        const uint64_t desc_x = smem_desc_sw128(base), desc_dy = smem_desc_sw128(base + kTileBytes);
-        auto both = [&](const uint64_t& mine, const uint64_t& peer, uint32_t parity) {
-            return mbar_wait_relaxed_warp(smem_u32(&mine), parity, limit) && mbar_wait_relaxed_warp(smem_u32(&peer), parity, limit);
-        };
         for (int c = 0; c < total + 1 && ok; ++c) {
             if (c < total) {
-                if (b1 == 0) { ok = both(bars->x_full, bars->x_peer, x_odd); x_odd ^= 1u; }
-                ok = ok && both(bars->w_full[w1.at], bars->w_peer[w1.at], w1.odd);
+                ok = mbar_wait_relaxed_warp(bar(bars->ready[w1.at]), w1.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t w = base + kOffW + w1.at * kStageBytes, d = tmem + 128 + buf1.at * kBufCols;
-                const uint64_t gu = smem_desc_sw128(w), wd = smem_desc_sw64_mn(w + kGuBytes + kInBytes);
+                const uint32_t w = w1.at * (kStageBytes >> 4), d = tmem + 128 + buf1.at * kBufCols;
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)
-                    mma_pair_by(elected, d, desc_x + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4),
-                                gu + (uint64_t)(((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), id_gu, ks > 0 ? 1u : 0u);
+                    mma_pair_by(elected, d, low_x + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
+                                low_gu + w + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, id_gu, ks > 0 ? 1u : 0u);
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)                       // dA = dY Wd: Wd's rows run along K
-                    mma_pair_by(elected, d + 128, desc_dy + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), wd + ks * (1024 >> 4), id_da, ks > 0 ? 1u : 0u);
+                    mma_pair_by(elected, d + 128, low_dy + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
+                                low_wd + w + ks * (1024 >> 4), high_wd, id_da, ks > 0 ? 1u : 0u);
                 mma_commit_pair_by(elected, bar(bars->acc_full[buf1.at]));
                 w1.next(kStages); buf1.next(kBufs);
                 if (++b1 == nb) { b1 = 0; mma_commit_pair_by(elected, bar(bars->x_empty)); }
@@ -647,11 +619,10 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t w = smem_desc_sw128_mn(base + kOffW + w2.at * kStageBytes + kGuBytes, kHalfBytes);
-                const uint32_t a = tmem + 128 + buf2.at * kBufCols;
+                const uint32_t w = low_in + w2.at * (kStageBytes >> 4), a = tmem + 128 + buf2.at * kBufCols;
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks)                       // dX += [dG | dU] [Wg; Wu]: their rows run along K
-                    mma_pair_ta_by(elected, tmem, a + ks * 16, w + ks * kStepMn, id_dx, (b2 | ks) ? 1u : 0u);
+                    mma_pair_ta_by(elected, tmem, a + ks * 16, w + ks * (2048 >> 4), high, id_dx, (b2 | ks) ? 1u : 0u);
                 mma_commit_pair_by(elected, bar(bars->w_empty[w2.at]));
                 w2.next(kStages); buf2.next(kBufs);
                 if (++b2 == nb) { b2 = 0; mma_commit_pair_by(elected, bar(bars->y_full[y_odd])); }
@@ -660,7 +631,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         if (!ok) raise_timeout_pair(bars, p.status, rank);
         mma_commit_pair_by(elected, bar(bars->drain));
         mbar_wait_warp(bar(bars->drain), 0);
-    } else {
+    } else if (warp >= kCtrlWarps) {
         // ------------------------------------------------------------------ epilogue
         // as in the forward kernel: two sets of warps, dX of a tile after the next one's first block
         const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1;
@@ -737,6 +708,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 
     tc_fence_before();
     __syncthreads();
+    if (warp == 1 && rank == 1) mbar_wait_warp(bar(bars->drain), 0);
     cluster_sync();
     if (warp == 1) {
         tc_fence_after();
