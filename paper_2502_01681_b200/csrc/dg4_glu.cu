@@ -50,8 +50,8 @@ struct Turn {
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, const uint32_t* r) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-__device__ __forceinline__ void ld_global_v4(const void* p, uint32_t* r) {
-    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p) : "memory");
+__device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t* r) {
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void st_global_v4(void* p, const uint32_t* r) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
@@ -161,7 +161,7 @@ __device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t
 
 struct Params {
     int32_t n, d_ff, n_tiles, n_blocks;
-    const __nv_bfloat16* R; int64_t ldr;     // forward: nullable residual
+    int32_t has_res;                         // forward: a residual is added
     __nv_bfloat16* out; int64_t ldo;         // backward: dX
     int32_t* status;
     uint32_t poll_limit;
@@ -171,6 +171,18 @@ template <class Bars>
 __device__ __forceinline__ void raise_timeout(Bars* bars, int32_t* status) {
     atomicExch(&bars->abort_flag, 1u);
     if (status) atomicCAS(status, 0, (int)DG4_ERR_TIMEOUT);
+}
+
+// Whether a phase has completed, for a converged warp: a third of a waiting instruction's time, of which the loops below would
+// spend more than the products take.
+__device__ __forceinline__ bool has_come(uint32_t bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_test(bar, parity) ? 1 : 0) != 0;
+}
+template <class Bars>
+__device__ __forceinline__ bool await(Bars* bars, uint32_t bar, uint32_t parity, uint32_t limit) {
+    if (has_come(bar, parity)) return true;
+    if (__any_sync(0xffffffffu, *(volatile uint32_t*)&bars->abort_flag != 0)) return false;
+    return mbar_wait_relaxed_warp(bar, parity, limit);
 }
 
 // The pair's form: the other CTA's roles are told too.
@@ -216,11 +228,11 @@ constexpr uint64_t kStepMn = 2048 >> 4;            // sixteen K of an MN-major o
 // run ahead of the epilogue of a third.  The activations of a block overwrite its G, 16 values in 8 of the columns they were
 // computed from.
 namespace fwd {
-constexpr int kStages = 6, kBufs = 3;
+constexpr int kStages = 5, kBufs = 3;
 constexpr int kGuBytes = kBlock * 256, kWdBytes = 64 * 128;       // this CTA's half of [Wg; Wu], and of Wd
-constexpr int kStageBytes = kGuBytes + kWdBytes, kOffW = 2 * kTileBytes, kOffBars = kOffW + kStages * kStageBytes;
+constexpr int kStageBytes = kGuBytes + kWdBytes, kOffW = 2 * kTileBytes, kOffR = kOffW + kStages * kStageBytes, kOffBars = kOffR + kTileBytes;
 struct Bars {
-    uint64_t x_full[2], x_empty[2], w_full[kStages], w_empty[kStages];
+    uint64_t x_full[2], x_empty[2], r_full, r_empty, w_full[kStages], w_empty[kStages];
     // rank 0's, both CTAs arrive: a block's weights have come (for a tile's first block X too), its activations are there, Y
     // has been read
     uint64_t ready[kStages], a_ready[kBufs], y_empty;
@@ -236,7 +248,7 @@ template <int ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_wg,
                const __grid_constant__ CUtensorMap map_wu, const __grid_constant__ CUtensorMap map_wd,
-               const __grid_constant__ CUtensorMap map_y, Params p) {
+               const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_y, Params p) {
     using namespace fwd;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -248,7 +260,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), kSetWarps); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), 1); }
+        mbar_init(bar(bars->r_full), 1); mbar_init(bar(bars->r_empty), kSetWarps);
         for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); mbar_init(bar(bars->ready[i]), 2); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
         mbar_init(bar(bars->y_full[0]), 1); mbar_init(bar(bars->y_full[1]), 1); mbar_init(bar(bars->y_empty), 2 * kSetWarps); mbar_init(bar(bars->drain), 1);
@@ -303,16 +316,31 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             if (!ok) raise_timeout_pair(bars, p.status, rank);
         }
     } else if (warp == 3) {
-        // ------------------------------------------------------------------ X
+        // ------------------------------------------------------------------ X, and the residual of the tile before
         if (lane == 0) {
-            Turn x;
-            int t = 0;
-            for (; t < tiles && !*abort_flag; ++t, x.next(2)) {
-                if (t >= 2 && !mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
-                mbar_expect_tx(bar(bars->x_full[x.at]), kTileBytes);
-                load_tile(&map_x, base + x.at * kTileBytes, row_of(t), bar(bars->x_full[x.at]));
+            int armed_x = 0, armed_r = 0;
+            bool ok = true;
+            for (int t = 0; t <= tiles && ok && !*abort_flag; ++t) {
+                if (t < tiles) {
+                    ok = t < 2 || mbar_wait_relaxed(bar(bars->x_empty[t & 1]), (uint32_t)(t / 2 - 1) & 1u, limit);
+                    if (ok) {
+                        mbar_expect_tx(bar(bars->x_full[t & 1]), kTileBytes);
+                        load_tile(&map_x, base + (t & 1) * kTileBytes, row_of(t), bar(bars->x_full[t & 1]));
+                        armed_x = t + 1;
+                    }
+                }
+                if (ok && t >= 1 && p.has_res) {                     // its place is free when the rows before have been stored
+                    ok = t < 2 || mbar_wait_relaxed(bar(bars->r_empty), (uint32_t)t & 1u, limit);
+                    if (ok) {
+                        mbar_expect_tx(bar(bars->r_full), kTileBytes);
+                        load_tile(&map_r, base + kOffR, row_of(t - 1), bar(bars->r_full));
+                        armed_r = t;
+                    }
+                }
             }
-            for (int i = max(0, t - 2); i < t; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
+            if (!ok) raise_timeout_pair(bars, p.status, rank);
+            for (int i = max(0, armed_x - 2); i < armed_x; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
+            if (armed_r > 0) mbar_wait(bar(bars->r_full), (uint32_t)(armed_r - 1) & 1u);
         }
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ rank 0: issues the products
@@ -324,12 +352,14 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         int b1 = 0, b2 = 0;                              // blocks within their tiles
         uint32_t y_odd = 1;
         bool ok = true;
-        // First products run two blocks ahead of second ones.  (One where a tile is one block: the tile two further on
-        // takes the place of X that this tile's epilogue leaves, which comes after this tile's second product.)
-        const int ahead = nb == 1 ? 1 : 2;
+        const int ahead = 2;                             // first products run two blocks ahead of second ones
         for (int c = 0; c < total + ahead && ok; ++c) {
-            if (c < total) {
-                ok = mbar_wait_relaxed_warp(bar(bars->ready[w1.at]), w1.odd, limit);
+            // both of the barriers in one go where both have completed, as they mostly have
+            const bool first = c < total, second = c >= ahead;
+            const bool r1 = mbar_test(bar(bars->ready[w1.at]), w1.odd), r2 = mbar_test(bar(bars->a_ready[buf2.at]), buf2.odd);
+            const uint32_t come = __reduce_and_sync(0xffffffffu, (r1 ? 1u : 0u) | (r2 ? 2u : 0u));
+            if (first) {
+                if (!(come & 1u)) ok = await(bars, bar(bars->ready[w1.at]), w1.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t dx = low_x + x.at * (kTileBytes >> 4), dw = low_w + w1.at * (kStageBytes >> 4), to = tmem + 128 + buf1.at * 128;
@@ -339,11 +369,11 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                                 dw + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, idesc, ks > 0 ? 1u : 0u);
                 mma_commit_pair_by(elected, bar(bars->acc_full[buf1.at]));
                 w1.next(kStages); buf1.next(kBufs);
-                if (++b1 == nb) { b1 = 0; x.next(2); }
+                if (++b1 == nb) { b1 = 0; mma_commit_pair_by(elected, bar(bars->x_empty[x.at])); x.next(2); }
             }
-            if (c >= ahead) {
-                ok = mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
-                if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
+            if (second) {
+                if (!(come & 2u)) ok = await(bars, bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                if (ok && b2 == 0) { ok = await(bars, bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t wd = low_w + ((w2.at * kStageBytes + kGuBytes) >> 4), a = tmem + 128 + buf2.at * 128;
@@ -364,29 +394,26 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         // last product has long been done then.
         const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const uint32_t stage_at = base + part * kHalfBytes + quad * 4096;          // in X's place
+        const uint32_t stage = base + kOffR + part * kHalfBytes + quad * 4096;
         const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), 0), y_empty0 = cluster_addr(bar(bars->y_empty), 0);
         Turn buf;
         bool ok = true;
         int turn = set;                                              // 0: the next block is this set's
-        // Y of tile t: X's products are done, so its place stages the rows
+        // Y of tile t, with the residual's rows where there are some, staged in their place
         auto finish = [&](int t) {
-            const int row0 = row_of(t) + quad * 32;
-            const bool res = p.R != nullptr && row0 + lane < p.n;
-            const uint32_t stage = stage_at + (t & 1) * kTileBytes;
+            // y_full first: where it has come, tile t - 1 has been through here, and the parities below are not those of t - 2
+            if (!await(bars, bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
+            if (p.has_res ? !await(bars, bar(bars->r_full), (uint32_t)t & 1u, limit)
+                          : t > 0 && !await(bars, bar(bars->r_empty), (uint32_t)(t - 1) & 1u, limit)) return false;
+            tc_fence_after();
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                uint32_t r[16];
-                if (res) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) ld_global_v4(p.R + (int64_t)(row0 + lane) * p.ldr + part * 64 + c * 32 + i * 8, r + 4 * i);
-                }
-                if (c == 0) {
-                    if (!mbar_wait_relaxed_warp(bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
-                    tc_fence_after();
-                }
-                uint32_t y[32];
+                uint32_t y[32], r[16];
                 tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64 + c * 32), y);
+                if (p.has_res) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ld_shared_v4(stage + sw128_offset(lane, c * 4 + i), r + 4 * i);
+                }
                 tmem_ld_wait();
                 if (c == 1) {
                     tc_fence_before();
@@ -399,7 +426,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float lo = __uint_as_float(y[8 * i + 2 * e]), hi = __uint_as_float(y[8 * i + 2 * e + 1]);
-                        if (res) {
+                        if (p.has_res) {
                             lo += __uint_as_float(r[4 * i + e] << 16);
                             hi += __uint_as_float(r[4 * i + e] & 0xffff0000u);
                         }
@@ -410,26 +437,27 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             }
             fence_proxy_async_smem();
             __syncwarp();
+            const int row0 = row_of(t) + quad * 32;
             if (lane == 0 && row0 < p.n) {
                 tma_store_2d(&map_y, part * 64, row0, stage);
                 bulk_commit();
             }
             return true;
         };
-        int owed = -1;                                               // the tile whose rows have not yet left their place
+        bool owed = false;                                           // rows that have not yet left their place
         auto leave = [&]() {
-            if (owed >= 0 && lane == 0) {
+            if (owed && lane == 0) {
                 bulk_wait_read0();
-                mbar_arrive(bar(bars->x_empty[owed & 1]));
+                mbar_arrive(bar(bars->r_empty));
             }
-            owed = -1;
+            owed = false;
         };
         for (int t = 0; t < tiles && ok; ++t) {
             leave();
             bool open = t > 0 && turn == 0;                          // the tile before is this set's to finish
             for (int b = 0; b < nb; ++b, buf.next(kBufs), turn ^= 1) {
                 if (turn) continue;
-                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
+                ok = await(bars, bar(bars->acc_full[buf.at]), buf.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
@@ -456,10 +484,11 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     open = false;
                     ok = finish(t - 1);
                     if (!ok) break;
-                    owed = t - 1;
+                    owed = true;
                 }
             }
         }
+        leave();
         if (ok && turn == 0) ok = finish(tiles - 1);
         if (!ok) raise_timeout_pair(bars, p.status, rank);
         if (lane == 0) bulk_wait_all();
@@ -597,8 +626,10 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         uint32_t y_odd = 1;
         bool ok = true;
         for (int c = 0; c < total + 1 && ok; ++c) {
+            const bool r1 = mbar_test(bar(bars->ready[w1.at]), w1.odd), r2 = mbar_test(bar(bars->a_ready[buf2.at]), buf2.odd);
+            const uint32_t come = __reduce_and_sync(0xffffffffu, (r1 ? 1u : 0u) | (r2 ? 2u : 0u));
             if (c < total) {
-                ok = mbar_wait_relaxed_warp(bar(bars->ready[w1.at]), w1.odd, limit);
+                if (!(come & 1u)) ok = await(bars, bar(bars->ready[w1.at]), w1.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t w = w1.at * (kStageBytes >> 4), d = tmem + 128 + buf1.at * kBufCols;
@@ -615,8 +646,8 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 if (++b1 == nb) { b1 = 0; mma_commit_pair_by(elected, bar(bars->x_empty)); }
             }
             if (c >= 1) {
-                ok = mbar_wait_relaxed_warp(bar(bars->a_ready[buf2.at]), buf2.odd, limit);
-                if (ok && b2 == 0) { ok = mbar_wait_relaxed_warp(bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
+                if (!(come & 2u)) ok = await(bars, bar(bars->a_ready[buf2.at]), buf2.odd, limit);
+                if (ok && b2 == 0) { ok = await(bars, bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t w = low_in + w2.at * (kStageBytes >> 4), a = tmem + 128 + buf2.at * kBufCols;
@@ -642,7 +673,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         int turn = set;
         auto finish = [&](int t) {
             const int row = row_of(t) + quad * 32 + lane;
-            if (!mbar_wait_relaxed_warp(bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
+            if (!await(bars, bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
             tc_fence_after();
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -671,7 +702,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             bool open = t > 0 && turn == 0;
             for (int b = 0; b < nb; ++b, buf.next(kBufs), turn ^= 1) {
                 if (turn) continue;
-                ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full[buf.at]), buf.odd, limit);
+                ok = await(bars, bar(bars->acc_full[buf.at]), buf.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
 #pragma unroll
@@ -968,7 +999,7 @@ dg4_status allow_smem(int dev, int bytes) {
     return DG4_OK;
 }
 
-struct Maps { CUtensorMap x, dy, wg, wu, wd, y, wd_half; };
+struct Maps { CUtensorMap x, dy, wg, wu, wd, r, y, wd_half; };
 
 int blocks_of(int d_ff) { return (d_ff + kBlock - 1) / kBlock; }
 // Row groups of glu_dw_kernel: as many as the device has SMs for, and no more than there are tiles.
@@ -999,7 +1030,7 @@ int pair_grid(const Params& p, int sms) { return 2 * (p.n_tiles < sms / 2 ? p.n_
 template <int ACT>
 dg4_status launch_fwd(const Maps& m, const Params& p, int dev, int sms, cudaStream_t st) {
     CHECK(allow_smem<glu_fwd_kernel<ACT>>(dev, fwd::kSmem));
-    glu_fwd_kernel<ACT><<<pair_grid(p, sms), kThreads, fwd::kSmem, st>>>(m.x, m.wg, m.wu, m.wd, m.y, p);
+    glu_fwd_kernel<ACT><<<pair_grid(p, sms), kThreads, fwd::kSmem, st>>>(m.x, m.wg, m.wu, m.wd, m.r, m.y, p);
     dg4i_count_launch();
     DG4_CUDA_TRY(cudaGetLastError());
     return DG4_OK;
@@ -1057,7 +1088,9 @@ extern "C" dg4_status dg4_glu_fwd(const dg4_graph* g, const dg4_desc* desc, cons
     CHECK(dg4i_make_row_map(&m.y, Y, g->n, ldy, 32));
     Params p = make_params(g, d_ff);
     p.n_tiles = (p.n_tiles + 1) / 2;
-    p.R = res ? (const __nv_bfloat16*)H_res : nullptr; p.ldr = ldh;
+    p.has_res = res;
+    m.r = m.x;
+    if (res) CHECK(dg4i_make_row_map(&m.r, H_res, g->n, ldh, kTileM));
     const cudaStream_t st = (cudaStream_t)stream;
     if (activation == DG4_ACT_SILU) return launch_fwd<DG4_ACT_SILU>(m, p, g->device, sms, st);
     if (activation == DG4_ACT_GELU) return launch_fwd<DG4_ACT_GELU>(m, p, g->device, sms, st);
