@@ -232,12 +232,12 @@ constexpr int kStages = 5, kBufs = 3;
 constexpr int kGuBytes = kBlock * 256, kWdBytes = 64 * 128;       // this CTA's half of [Wg; Wu], and of Wd
 constexpr int kStageBytes = kGuBytes + kWdBytes, kOffW = 2 * kTileBytes, kOffR = kOffW + kStages * kStageBytes, kOffBars = kOffR + kTileBytes;
 struct Bars {
-    uint64_t x_full[2], x_empty[2], r_full, r_empty, w_full[kStages], w_empty[kStages];
+    uint64_t x_full[2], x_empty[2], r_full[2], r_empty[2], w_full[kStages], w_empty[kStages];
     // rank 0's, both CTAs arrive: a block's weights have come (for a tile's first block X too), its activations are there, Y
     // has been read
     uint64_t ready[kStages], a_ready[kBufs], y_empty;
     uint64_t acc_full[kBufs];
-    uint64_t y_full[2], drain;                                    // y_full in turn: a set of warps may see every other tile
+    uint64_t y_full[2], drain;                                    // those of two tiles in turn: a set of warps may see every other one
     uint32_t tmem_base, abort_flag;
 };
 constexpr int kSmem = kOffBars + (int)sizeof(Bars) + 1024;        // 1024: the base is aligned by hand
@@ -261,7 +261,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), 1); }
-        mbar_init(bar(bars->r_full), 1); mbar_init(bar(bars->r_empty), kSetWarps);
+        for (int i = 0; i < 2; ++i) { mbar_init(bar(bars->r_full[i]), 1); mbar_init(bar(bars->r_empty[i]), kSetWarps); }
         for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); mbar_init(bar(bars->ready[i]), 2); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
         mbar_init(bar(bars->y_full[0]), 1); mbar_init(bar(bars->y_full[1]), 1); mbar_init(bar(bars->y_empty), 2 * kSetWarps); mbar_init(bar(bars->drain), 1);
@@ -330,17 +330,18 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     }
                 }
                 if (ok && t >= 1 && p.has_res) {                     // its place is free when the rows before have been stored
-                    ok = t < 2 || mbar_wait_relaxed(bar(bars->r_empty), (uint32_t)t & 1u, limit);
+                    ok = t < 2 || mbar_wait_relaxed(bar(bars->r_empty[t & 1]), (uint32_t)(t / 2 - 1) & 1u, limit);
                     if (ok) {
-                        mbar_expect_tx(bar(bars->r_full), kTileBytes);
-                        load_tile(&map_r, base + kOffR, row_of(t - 1), bar(bars->r_full));
+                        const uint32_t full = bar(bars->r_full[(t - 1) & 1]);
+                        mbar_expect_tx(full, kTileBytes);
+                        load_tile(&map_r, base + kOffR, row_of(t - 1), full);
                         armed_r = t;
                     }
                 }
             }
             if (!ok) raise_timeout_pair(bars, p.status, rank);
             for (int i = max(0, armed_x - 2); i < armed_x; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
-            if (armed_r > 0) mbar_wait(bar(bars->r_full), (uint32_t)(armed_r - 1) & 1u);
+            if (armed_r > 0) mbar_wait(bar(bars->r_full[(armed_r - 1) & 1]), (uint32_t)((armed_r - 1) >> 1) & 1u);
         }
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ rank 0: issues the products
@@ -353,39 +354,56 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         uint32_t y_odd = 1;
         bool ok = true;
         const int ahead = 2;                             // first products run two blocks ahead of second ones
+        auto second = [&]() {                            // Y += activations Wd^T of the next block
+            if (b2 == 0) {
+                ok = await(bars, bar(bars->y_empty), y_odd, limit);
+                y_odd ^= 1u;
+                if (!ok) return;
+            }
+            tc_fence_after();
+            const uint32_t wd = low_w + ((w2.at * kStageBytes + kGuBytes) >> 4), a = tmem + 128 + buf2.at * 128;
+            if (elected) {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) mma_pair_ta(tmem, a + ks * 16, wd + ks * 2, high, idesc, (b2 | ks) ? 1u : 0u);
+                if (b2 + 1 == nb) mma_commit_pair(bar(bars->y_full[y_odd]));
+                mma_commit_pair(bar(bars->w_empty[w2.at]));
+            }
+            __syncwarp();
+            w2.next(kStages); buf2.next(kBufs);
+            if (++b2 == nb) b2 = 0;
+        };
         for (int c = 0; c < total + ahead && ok; ++c) {
             // both of the barriers in one go where both have completed, as they mostly have
-            const bool first = c < total, second = c >= ahead;
             const bool r1 = mbar_test(bar(bars->ready[w1.at]), w1.odd), r2 = mbar_test(bar(bars->a_ready[buf2.at]), buf2.odd);
             const uint32_t come = __reduce_and_sync(0xffffffffu, (r1 ? 1u : 0u) | (r2 ? 2u : 0u));
-            if (first) {
+            // a tile's first second product waits for the tile before to be read: what can go before it goes before it
+            const bool early = c >= ahead && (come & 2u) && b2 != 0;
+            if (early) second();
+            if (c < total) {
                 if (!(come & 1u)) ok = await(bars, bar(bars->ready[w1.at]), w1.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t dx = low_x + x.at * (kTileBytes >> 4), dw = low_w + w1.at * (kStageBytes >> 4), to = tmem + 128 + buf1.at * 128;
+                if (elected) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    mma_pair_by(elected, to, dx + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
-                                dw + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, idesc, ks > 0 ? 1u : 0u);
-                mma_commit_pair_by(elected, bar(bars->acc_full[buf1.at]));
+                    for (int ks = 0; ks < 8; ++ks)
+                        mma_pair(to, dx + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
+                                 dw + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, idesc, ks > 0 ? 1u : 0u);
+                    mma_commit_pair(bar(bars->acc_full[buf1.at]));
+                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->x_empty[x.at]));
+                }
+                __syncwarp();
                 w1.next(kStages); buf1.next(kBufs);
-                if (++b1 == nb) { b1 = 0; mma_commit_pair_by(elected, bar(bars->x_empty[x.at])); x.next(2); }
+                if (++b1 == nb) { b1 = 0; x.next(2); }
             }
-            if (second) {
+            if (c >= ahead && !early) {
                 if (!(come & 2u)) ok = await(bars, bar(bars->a_ready[buf2.at]), buf2.odd, limit);
-                if (ok && b2 == 0) { ok = await(bars, bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t wd = low_w + ((w2.at * kStageBytes + kGuBytes) >> 4), a = tmem + 128 + buf2.at * 128;
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks) mma_pair_ta_by(elected, tmem, a + ks * 16, wd + ks * 2, high, idesc, (b2 | ks) ? 1u : 0u);
-                mma_commit_pair_by(elected, bar(bars->w_empty[w2.at]));
-                w2.next(kStages); buf2.next(kBufs);
-                if (++b2 == nb) { b2 = 0; mma_commit_pair_by(elected, bar(bars->y_full[y_odd])); }
+                if (ok) second();
             }
         }
         if (!ok) raise_timeout_pair(bars, p.status, rank);
-        mma_commit_pair_by(elected, bar(bars->drain));   // tensor memory is freed below: every product must be done
+        if (elected) mma_commit_pair(bar(bars->drain));  // tensor memory is freed below: every product must be done
+        __syncwarp();
         mbar_wait_warp(bar(bars->drain), 0);
     } else if (warp >= kCtrlWarps) {
         // ------------------------------------------------------------------ epilogue
@@ -401,39 +419,27 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         int turn = set;                                              // 0: the next block is this set's
         // Y of tile t, with the residual's rows where there are some, staged in their place
         auto finish = [&](int t) {
-            // y_full first: where it has come, tile t - 1 has been through here, and the parities below are not those of t - 2
             if (!await(bars, bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
-            if (p.has_res ? !await(bars, bar(bars->r_full), (uint32_t)t & 1u, limit)
-                          : t > 0 && !await(bars, bar(bars->r_empty), (uint32_t)(t - 1) & 1u, limit)) return false;
             tc_fence_after();
+            uint32_t y[64];
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64), y);
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64 + 32), y + 32);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(y_empty0);
+            if (p.has_res ? !await(bars, bar(bars->r_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)
+                          : t > 0 && !await(bars, bar(bars->r_empty[(t - 1) & 1]), (uint32_t)((t - 1) >> 1) & 1u, limit)) return false;
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t y[32], r[16];
-                tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64 + c * 32), y);
-                if (p.has_res) {
+            for (int i = 0; i < 8; ++i) {
+                uint32_t o[4], r[4] = {0u, 0u, 0u, 0u};
+                const uint32_t at = stage + sw128_offset(lane, i);
+                if (p.has_res) ld_shared_v4(at, r);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) ld_shared_v4(stage + sw128_offset(lane, c * 4 + i), r + 4 * i);
-                }
-                tmem_ld_wait();
-                if (c == 1) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(y_empty0);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t o[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float lo = __uint_as_float(y[8 * i + 2 * e]), hi = __uint_as_float(y[8 * i + 2 * e + 1]);
-                        if (p.has_res) {
-                            lo += __uint_as_float(r[4 * i + e] << 16);
-                            hi += __uint_as_float(r[4 * i + e] & 0xffff0000u);
-                        }
-                        o[e] = pack_bf16(lo, hi);
-                    }
-                    st_shared_v4(stage + sw128_offset(lane, c * 4 + i), o);
-                }
+                for (int e = 0; e < 4; ++e)
+                    o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]) + __uint_as_float(r[e] << 16),
+                                     __uint_as_float(y[8 * i + 2 * e + 1]) + __uint_as_float(r[e] & 0xffff0000u));
+                st_shared_v4(at, o);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -444,13 +450,13 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             }
             return true;
         };
-        bool owed = false;                                           // rows that have not yet left their place
+        int owed = -1;                                               // the tile whose rows have not yet left their place
         auto leave = [&]() {
-            if (owed && lane == 0) {
+            if (owed >= 0 && lane == 0) {
                 bulk_wait_read0();
-                mbar_arrive(bar(bars->r_empty));
+                mbar_arrive(bar(bars->r_empty[owed & 1]));
             }
-            owed = false;
+            owed = -1;
         };
         for (int t = 0; t < tiles && ok; ++t) {
             leave();
@@ -484,7 +490,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     open = false;
                     ok = finish(t - 1);
                     if (!ok) break;
-                    owed = true;
+                    owed = t - 1;
                 }
             }
         }
@@ -633,17 +639,21 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t w = w1.at * (kStageBytes >> 4), d = tmem + 128 + buf1.at * kBufCols;
+                if (elected) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    mma_pair_by(elected, d, low_x + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
-                                low_gu + w + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, id_gu, ks > 0 ? 1u : 0u);
+                    for (int ks = 0; ks < 8; ++ks)
+                        mma_pair(d, low_x + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
+                                 low_gu + w + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, id_gu, ks > 0 ? 1u : 0u);
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)                       // dA = dY Wd: Wd's rows run along K
-                    mma_pair_by(elected, d + 128, low_dy + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
-                                low_wd + w + ks * (1024 >> 4), high_wd, id_da, ks > 0 ? 1u : 0u);
-                mma_commit_pair_by(elected, bar(bars->acc_full[buf1.at]));
+                    for (int ks = 0; ks < 8; ++ks)                   // dA = dY Wd: Wd's rows run along K
+                        mma_pair(d + 128, low_dy + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
+                                 low_wd + w + ks * (1024 >> 4), high_wd, id_da, ks > 0 ? 1u : 0u);
+                    mma_commit_pair(bar(bars->acc_full[buf1.at]));
+                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->x_empty));
+                }
+                __syncwarp();
                 w1.next(kStages); buf1.next(kBufs);
-                if (++b1 == nb) { b1 = 0; mma_commit_pair_by(elected, bar(bars->x_empty)); }
+                if (++b1 == nb) b1 = 0;
             }
             if (c >= 1) {
                 if (!(come & 2u)) ok = await(bars, bar(bars->a_ready[buf2.at]), buf2.odd, limit);
@@ -651,16 +661,21 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t w = low_in + w2.at * (kStageBytes >> 4), a = tmem + 128 + buf2.at * kBufCols;
+                if (elected) {
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)                       // dX += [dG | dU] [Wg; Wu]: their rows run along K
-                    mma_pair_ta_by(elected, tmem, a + ks * 16, w + ks * (2048 >> 4), high, id_dx, (b2 | ks) ? 1u : 0u);
-                mma_commit_pair_by(elected, bar(bars->w_empty[w2.at]));
+                    for (int ks = 0; ks < 8; ++ks)                   // dX += [dG | dU] [Wg; Wu]: their rows run along K
+                        mma_pair_ta(tmem, a + ks * 16, w + ks * (2048 >> 4), high, id_dx, (b2 | ks) ? 1u : 0u);
+                    if (b2 + 1 == nb) mma_commit_pair(bar(bars->y_full[y_odd]));
+                    mma_commit_pair(bar(bars->w_empty[w2.at]));
+                }
+                __syncwarp();
                 w2.next(kStages); buf2.next(kBufs);
-                if (++b2 == nb) { b2 = 0; mma_commit_pair_by(elected, bar(bars->y_full[y_odd])); }
+                if (++b2 == nb) b2 = 0;
             }
         }
         if (!ok) raise_timeout_pair(bars, p.status, rank);
-        mma_commit_pair_by(elected, bar(bars->drain));
+        if (elected) mma_commit_pair(bar(bars->drain));
+        __syncwarp();
         mbar_wait_warp(bar(bars->drain), 0);
     } else if (warp >= kCtrlWarps) {
         // ------------------------------------------------------------------ epilogue

@@ -271,25 +271,23 @@ __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t cols)
 }
 // Descriptors are given by their low words (start address and leading offset), all that differs between the tiles of a
 // kernel; `high` is the rest.
-__device__ __forceinline__ void mma_pair_by(uint32_t elected, uint32_t d_tmem, uint32_t a_low, uint32_t a_high, uint32_t b_low, uint32_t b_high, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint32_t a_low, uint32_t a_high, uint32_t b_low, uint32_t b_high, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p, e;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 e, %7, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
-        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_low), "r"(a_high), "r"(b_low), "r"(b_high), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_low), "r"(a_high), "r"(b_low), "r"(b_high), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void mma_pair_ta_by(uint32_t elected, uint32_t d_tmem, uint32_t a_tmem, uint32_t b_low, uint32_t b_high, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_pair_ta(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_low, uint32_t b_high, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p, e;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 e, %6, 0;\n\tmov.b64 b, {%2, %3};\n\t"
-        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %4, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "r"(b_low), "r"(b_high), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_low), "r"(b_high), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ uint32_t desc_low(uint64_t desc) { return (uint32_t)desc; }
 __device__ __forceinline__ uint32_t desc_high(uint64_t desc) { return (uint32_t)(desc >> 32); }
-__device__ __forceinline__ void mma_commit_pair_by(uint32_t elected, uint32_t bar) {
-    asm volatile(
-        "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %1, 0;\n\t"
-        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
-        ::"r"(bar), "r"(elected), "h"((unsigned short)3) : "memory");
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((unsigned short)3) : "memory");
 }
 // A value that all lanes hold alike, told to the compiler.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
