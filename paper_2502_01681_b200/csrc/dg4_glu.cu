@@ -206,14 +206,6 @@ __device__ __forceinline__ void prefetch_tile(const CUtensorMap* map, int row0) 
     for (int h = 0; h < 2; ++h)
         asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(map), "r"(h * 64), "r"(row0) : "memory");
 }
-// d = A B^T over 128 inputs, both K-major in two panels of 64
-__device__ __forceinline__ void product_128(uint32_t elected, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-        const uint64_t off = (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4);
-        mma_bf16_by(elected, d, a + off, b + off, idesc, ks > 0 ? 1u : 0u);
-    }
-}
 constexpr uint64_t kStepMn = 2048 >> 4;            // sixteen K of an MN-major operand, in descriptor units
 
 // ---------------------------------------------------------------------------------------------------
@@ -687,30 +679,26 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         bool ok = true;
         int turn = set;
         auto finish = [&](int t) {
-            const int row = row_of(t) + quad * 32 + lane;
             if (!await(bars, bar(bars->y_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)) return false;
             tc_fence_after();
+            uint32_t y[64];
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64), y);
+            tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64 + 32), y + 32);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(y_empty0);
+            const int row = row_of(t) + quad * 32 + lane;
+            if (row < p.n) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t y[32];
-                tmem_ld_32x32(tmem + lanes + (uint32_t)(part * 64 + c * 32), y);
-                tmem_ld_wait();
-                if (c == 1) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(y_empty0);
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
+                    st_global_v4(p.out + (int64_t)row * p.ldo + part * 64 + i * 8, o);
                 }
-                if (row < p.n) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t o[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
-                        st_global_v4(p.out + (int64_t)row * p.ldo + part * 64 + c * 32 + i * 8, o);
-                    }
-                }
-                __syncwarp();
             }
+            __syncwarp();
             return true;
         };
         for (int t = 0; t < tiles && ok; ++t) {
@@ -774,7 +762,7 @@ constexpr int kStages = 2;
 constexpr int kOffX = kTileBytes + kHalfBytes, kOffA = kOffX + kStages * 2 * kTileBytes, kOffBars = kOffA + 3 * kHalfBytes;
 constexpr int kPart = 3 * kBlock * 128;            // fp32 values of a CTA's accumulators: dWg, dWu, dWd^T, [unit][128] each
 struct Bars {
-    uint64_t w_full, x_full[kStages], x_empty[kStages];
+    uint64_t w_full, x_full[kStages], x_empty[kStages], dy_full[kStages], dy_empty[kStages];
     uint64_t acc_full, acc_empty, a_full, a_empty, w_done;
     uint64_t drain;
     uint32_t tmem_base, abort_flag;
@@ -804,7 +792,10 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 
     if (threadIdx.x == 0) {
         mbar_init(bar(bars->w_full), 1);
-        for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), 1); }
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(bar(bars->x_full[i]), 1); mbar_init(bar(bars->x_empty[i]), 1);
+            mbar_init(bar(bars->dy_full[i]), 1); mbar_init(bar(bars->dy_empty[i]), 1);
+        }
         mbar_init(bar(bars->acc_full), 1); mbar_init(bar(bars->acc_empty), kEpiWarps);
         mbar_init(bar(bars->a_full), kEpiWarps); mbar_init(bar(bars->a_empty), 1);
         mbar_init(bar(bars->w_done), 1); mbar_init(bar(bars->drain), 1);
@@ -820,76 +811,83 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const int tiles = (p.n_tiles - group + groups - 1) / groups;     // at least one: groups <= n_tiles
     const uint32_t limit = p.poll_limit;
 
-    if (warp == 0) {
-        // ------------------------------------------------------------------ producer
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------------ X (with the block's weights), dY
         if (lane == 0) {
-            mbar_expect_tx(bar(bars->w_full), kTileBytes + kHalfBytes);
-            load_gu(&map_wg, &map_wu, base, block, bar(bars->w_full));
-            tma_load_2d(base + kTileBytes, &map_wd, block * kBlock, 0, bar(bars->w_full));
+            const bool dy = warp == 2;
+            const CUtensorMap* map = dy ? &map_dy : &map_x;
+            uint64_t *full = dy ? bars->dy_full : bars->x_full, *empty = dy ? bars->dy_empty : bars->x_empty;
+            if (!dy) {
+                mbar_expect_tx(bar(bars->w_full), kTileBytes + kHalfBytes);
+                load_gu(&map_wg, &map_wu, base, block, bar(bars->w_full));
+                tma_load_2d(base + kTileBytes, &map_wd, block * kBlock, 0, bar(bars->w_full));
+            }
             Turn x;
-            int armed = 0;
-            bool ok = true;
-            for (int t = 0; t < tiles && ok; ++t, x.next(kStages)) {
-                ok = !*abort_flag && (t < kStages || mbar_wait_relaxed(bar(bars->x_empty[x.at]), x.odd ^ 1u, limit));
-                if (!ok) break;
-                const uint32_t dst = base + kOffX + x.at * 2 * kTileBytes;
+            int t = 0;
+            for (; t < tiles && !*abort_flag; ++t, x.next(kStages)) {
+                if (t >= kStages && !mbar_wait(bar(empty[x.at]), x.odd ^ 1u, limit)) { raise_timeout(bars, p.status); break; }
                 const int row0 = (group + t * groups) * kTileM;
-                mbar_expect_tx(bar(bars->x_full[x.at]), 2 * kTileBytes);
-                load_tile(&map_x, dst, row0, bar(bars->x_full[x.at]));
-                load_tile(&map_dy, dst + kTileBytes, row0, bar(bars->x_full[x.at]));
-                ++armed;
+                mbar_expect_tx(bar(full[x.at]), kTileBytes);
+                load_tile(map, base + kOffX + (2 * x.at + (dy ? 1 : 0)) * kTileBytes, row0, bar(full[x.at]));
                 // the rows of two tiles on into L2: every block's CTA of the group wants them, one asks
                 const int next = row0 + 2 * groups * kTileM;
-                if (next < p.n && t % (int)gridDim.x == block) {
-                    prefetch_tile(&map_x, next);
-                    prefetch_tile(&map_dy, next);
-                }
+                if (next < p.n && t % (int)gridDim.x == block) prefetch_tile(map, next);
             }
-            if (!ok) raise_timeout(bars, p.status);
-            mbar_wait(bar(bars->w_full), 0);
-            for (int i = max(0, armed - kStages); i < armed; ++i) mbar_wait(bar(bars->x_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
+            if (!dy) mbar_wait(bar(bars->w_full), 0);
+            for (int i = max(0, t - kStages); i < t; ++i) mbar_wait(bar(full[i % kStages]), (uint32_t)(i / kStages) & 1u);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         const uint32_t id_gu = idesc_bf16_f32(128, 128), id_da = idesc_bf16_f32(128, 64) | kIdescBMn,
                        id_w = idesc_bf16_f32(128, 128) | kIdescAMn | kIdescBMn, id_wd = idesc_bf16_f32(128, 64) | kIdescAMn | kIdescBMn,
                        elected = elect_one();
+        const uint64_t desc_gu = smem_desc_sw128(base), desc_wd = smem_desc_sw128_mn(base + kTileBytes, kHalfBytes),
+                       desc_a = smem_desc_sw128_mn(base + kOffA, kHalfBytes);
         Turn x1, x2;
         uint32_t acc_odd = 1, a_odd = 0, polls = 0;
         bool ok = mbar_wait_relaxed_warp(bar(bars->w_full), 0, limit);
-        const uint64_t desc_gu = smem_desc_sw128(base), desc_wd = smem_desc_sw128_mn(base + kTileBytes, kHalfBytes),
-                       desc_a = smem_desc_sw128_mn(base + kOffA, kHalfBytes);
-        auto here = [](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity) ? 1 : 0) != 0; };
         // Whichever can go first: the next tile's first products (its rows have come, the epilogue has taken its values) or
         // this tile's second ones.  With a fixed order the tensor cores would wait for rows that can only come when second
-        // products have left a stage.
+        // products have left a stage.  X leaves its place before dY, and G|U begins before dY has come.
+        bool half = false;                                           // G|U of tile t1 has been issued, dA not yet
         for (int t1 = 0, t2 = 0; t2 < tiles && ok;) {
-            if (t1 < tiles && here(bar(bars->x_full[x1.at]), x1.odd) && here(bar(bars->acc_empty), acc_odd)) {
-                acc_odd ^= 1u;
-                tc_fence_after();
-                const uint32_t x = base + kOffX + x1.at * 2 * kTileBytes, d = tmem + 192;
-                product_128(elected, d, smem_desc_sw128(x), desc_gu, id_gu);
-                const uint64_t dy = smem_desc_sw128(x + kTileBytes);
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    mma_bf16_by(elected, d + 128, dy + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), desc_wd + ks * kStepMn, id_da, ks > 0 ? 1u : 0u);
-                mma_commit_by(elected, bar(bars->acc_full));
-                x1.next(kStages);
-                ++t1;
-                polls = 0;
-            } else if (t2 < t1 && here(bar(bars->a_full), a_odd)) {
+            if (t2 < t1 && has_come(bar(bars->a_full), a_odd)) {
                 a_odd ^= 1u;
                 tc_fence_after();
                 const uint64_t x = smem_desc_sw128_mn(base + kOffX + x2.at * 2 * kTileBytes, kHalfBytes), dy = x + (kTileBytes >> 4);
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {                     // sixteen rows at a time
+                for (int ks = 0; ks < 8; ++ks)                       // sixteen rows at a time
                     mma_bf16_by(elected, tmem, x + ks * kStepMn, desc_a + ks * kStepMn, id_w, t2 > 0 || ks > 0 ? 1u : 0u);
-                    mma_bf16_by(elected, tmem + 128, dy + ks * kStepMn, desc_a + (2 * kHalfBytes >> 4) + ks * kStepMn, id_wd, t2 > 0 || ks > 0 ? 1u : 0u);
-                }
-                mma_commit_by(elected, bar(bars->a_empty));
                 mma_commit_by(elected, bar(bars->x_empty[x2.at]));
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    mma_bf16_by(elected, tmem + 128, dy + ks * kStepMn, desc_a + (2 * kHalfBytes >> 4) + ks * kStepMn, id_wd, t2 > 0 || ks > 0 ? 1u : 0u);
+                mma_commit_by(elected, bar(bars->dy_empty[x2.at]));
+                mma_commit_by(elected, bar(bars->a_empty));
                 x2.next(kStages);
                 ++t2;
+                polls = 0;
+            } else if (!half && t1 < tiles && has_come(bar(bars->x_full[x1.at]), x1.odd) && has_come(bar(bars->acc_empty), acc_odd)) {
+                acc_odd ^= 1u;
+                tc_fence_after();
+                const uint64_t x = smem_desc_sw128(base + kOffX + x1.at * 2 * kTileBytes);
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks) {
+                    const uint64_t off = (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4);
+                    mma_bf16_by(elected, tmem + 192, x + off, desc_gu + off, id_gu, ks > 0 ? 1u : 0u);
+                }
+                half = true;
+                polls = 0;
+            } else if (half && has_come(bar(bars->dy_full[x1.at]), x1.odd)) {
+                tc_fence_after();
+                const uint64_t dy = smem_desc_sw128(base + kOffX + (x1.at * 2 + 1) * kTileBytes);
+#pragma unroll
+                for (int ks = 0; ks < 8; ++ks)
+                    mma_bf16_by(elected, tmem + 320, dy + (uint64_t)(((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), desc_wd + ks * kStepMn, id_da, ks > 0 ? 1u : 0u);
+                mma_commit_by(elected, bar(bars->acc_full));
+                half = false;
+                x1.next(kStages);
+                ++t1;
                 polls = 0;
             } else {
                 ok = !__any_sync(0xffffffffu, *abort_flag != 0) && ++polls <= limit;
@@ -909,7 +907,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         bool ok = true;
         for (int t = 0; t < tiles && ok; ++t, odd ^= 1u) {
             const bool in = (group + t * groups) * kTileM + quad * 32 + lane < p.n;
-            ok = !__any_sync(0xffffffffu, *abort_flag != 0) && mbar_wait_relaxed_warp(bar(bars->acc_full), odd, limit);
+            ok = await(bars, bar(bars->acc_full), odd, limit);
             if (!ok) break;
             tc_fence_after();
             const uint32_t at = tmem + lanes + (uint32_t)(192 + part * kEl);
@@ -928,7 +926,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 #pragma unroll
                 for (int i = 0; i < kEl / 2; ++i) if (!in || 2 * i >= valid) v[0][i] = v[1][i] = v[2][i] = 0u;
             }
-            ok = mbar_wait_relaxed_warp(bar(bars->a_empty), odd ^ 1u, limit);
+            ok = await(bars, bar(bars->a_empty), odd ^ 1u, limit);
             if (!ok) break;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
