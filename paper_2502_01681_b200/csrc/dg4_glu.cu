@@ -19,6 +19,7 @@
 #include <atomic>
 
 #include "dg4_internal.h"
+#include "dg4_launch.cuh"
 #include "dg4_pairs.cuh"
 #include "dg4_sm100.cuh"
 
@@ -549,6 +550,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy); tma_prefetch_desc(&map_wg); tma_prefetch_desc(&map_wu);
         tma_prefetch_desc(&map_wd);
     }
+    let_next_begin();                                // glu_dw_kernel needs nothing of this one: few rows leave SMs for it
     if (warp == 1) tmem_alloc_pair(smem_u32(&bars->tmem_base), 512);
     tc_fence_before();
     __syncthreads();
@@ -803,6 +805,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         mbar_fence_init();
         tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy);
     }
+    let_next_begin();                                // glu_reduce_kernel, which waits
     if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
     tc_fence_before();
     __syncthreads();
@@ -948,14 +951,20 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 uint32_t w[kEl];
                 tmem_ld_32x16(tmem + lanes + (uint32_t)(m * 64 + part * kEl), w);
                 tmem_ld_wait();
+                if (sums) {
 #pragma unroll
-                for (int i = 0; i < kEl; ++i) {
-                    const float f = __uint_as_float(w[i]);
-                    const int unit = block * kBlock + part * kEl + i;
-                    if (sums) sums[(m * kBlock + part * kEl + i) * 128 + col] = f;
-                    else if (i < valid) {
-                        if (m == 2) out.wd[(int64_t)col * p.d_ff + unit] = __float2bfloat16(f);
-                        else (m == 0 ? out.wg : out.wu)[(int64_t)unit * 128 + col] = __float2bfloat16(f);
+                    for (int i = 0; i < kEl; ++i) sums[(m * kBlock + part * kEl + i) * 128 + col] = __uint_as_float(w[i]);
+                } else if (m < 2) {
+                    __nv_bfloat16* to = (m == 0 ? out.wg : out.wu) + (int64_t)(block * kBlock + part * kEl) * 128 + col;
+#pragma unroll
+                    for (int i = 0; i < kEl; ++i) if (i < valid) to[i * 128] = __float2bfloat16(__uint_as_float(w[i]));
+                } else {                                             // d_ff is a multiple of 8, and so are the units that exist
+#pragma unroll
+                    for (int i = 0; i < kEl; i += 8) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = pack_bf16(__uint_as_float(w[i + 2 * e]), __uint_as_float(w[i + 2 * e + 1]));
+                        if (i < valid) st_global_v4(out.wd + (int64_t)col * p.d_ff + block * kBlock + part * kEl + i, o);
                     }
                 }
             }
@@ -971,11 +980,13 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+    if (threadIdx.x == 0) wait_for_previous();       // glu_dx_kernel ends before this one does
 }
 
 // One CTA per hidden unit and matrix, one thread per input or output: the groups' sums in the order of the groups.
 __global__ void glu_reduce_kernel(DwOut out, int d_ff, int n_blocks, int groups) {
     const int unit = blockIdx.x, m = blockIdx.y, col = threadIdx.x;
+    wait_for_previous();
     const float* src = out.part + (int64_t)(unit / kBlock) * dw::kPart + (m * kBlock + unit % kBlock) * 128 + col;
     float f = 0.f;
     for (int g = 0; g < groups; ++g) f += src[(int64_t)g * n_blocks * dw::kPart];
@@ -1043,9 +1054,7 @@ int pair_grid(const Params& p, int sms) { return 2 * (p.n_tiles < sms / 2 ? p.n_
 template <int ACT>
 dg4_status launch_fwd(const Maps& m, const Params& p, int dev, int sms, cudaStream_t st) {
     CHECK(allow_smem<glu_fwd_kernel<ACT>>(dev, fwd::kSmem));
-    glu_fwd_kernel<ACT><<<pair_grid(p, sms), kThreads, fwd::kSmem, st>>>(m.x, m.wg, m.wu, m.wd, m.r, m.y, p);
-    dg4i_count_launch();
-    DG4_CUDA_TRY(cudaGetLastError());
+    CHECK(dg4i_launch(glu_fwd_kernel<ACT>, dim3(pair_grid(p, sms)), kThreads, fwd::kSmem, st, false, m.x, m.wg, m.wu, m.wd, m.r, m.y, p));
     return DG4_OK;
 }
 
@@ -1055,20 +1064,12 @@ dg4_status launch_bwd(const Maps& m, const Params& p, const DwOut& out, int grou
         CHECK(allow_smem<glu_dx_kernel<ACT>>(dev, dx::kSmem));
         Params q = p;
         q.n_tiles = (p.n_tiles + 1) / 2;
-        glu_dx_kernel<ACT><<<pair_grid(q, sms), kThreads, dx::kSmem, st>>>(m.x, m.dy, m.wg, m.wu, m.wd_half, q);
-        dg4i_count_launch();
-        DG4_CUDA_TRY(cudaGetLastError());
+        CHECK(dg4i_launch(glu_dx_kernel<ACT>, dim3(pair_grid(q, sms)), kThreads, dx::kSmem, st, false, m.x, m.dy, m.wg, m.wu, m.wd_half, q));
     }
     if (out.wg) {
         CHECK(allow_smem<glu_dw_kernel<ACT>>(dev, dw::kSmem));
-        glu_dw_kernel<ACT><<<dim3(p.n_blocks, groups), kThreads, dw::kSmem, st>>>(m.x, m.dy, m.wg, m.wu, m.wd, p, out);
-        dg4i_count_launch();
-        DG4_CUDA_TRY(cudaGetLastError());
-        if (out.part) {
-            glu_reduce_kernel<<<dim3(p.d_ff, 3), 128, 0, st>>>(out, p.d_ff, p.n_blocks, groups);
-            dg4i_count_launch();
-            DG4_CUDA_TRY(cudaGetLastError());
-        }
+        CHECK(dg4i_launch(glu_dw_kernel<ACT>, dim3(p.n_blocks, groups), kThreads, dw::kSmem, st, p.out != nullptr, m.x, m.dy, m.wg, m.wu, m.wd, p, out));
+        if (out.part) CHECK(dg4i_launch(glu_reduce_kernel, dim3(p.d_ff, 3), 128, 0, st, true, out, p.d_ff, p.n_blocks, groups));
     }
     return DG4_OK;
 }

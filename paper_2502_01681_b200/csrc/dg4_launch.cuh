@@ -1,11 +1,13 @@
-// How many blocks of a kernel the current device holds at once, asked of the runtime once per kernel and device (the
-// question costs about 2 us, a quarter of a small call).
+// Launching kernels.
 #pragma once
 
 #include <atomic>
+#include <utility>
 
 #include "dg4_internal.h"
 
+// How many blocks of a kernel the current device holds at once, asked of the runtime once per kernel and device (the
+// question costs about 2 us, a quarter of a small call).
 template <auto kKernel>
 dg4_status dg4i_resident_blocks(int threads, int* out) {
     static std::atomic<int> known[64];         // 0 = not asked yet
@@ -23,3 +25,23 @@ dg4_status dg4i_resident_blocks(int threads, int* out) {
     *out = blocks;
     return DG4_OK;
 }
+
+// Launches a kernel.  `early`: it may begin while the kernel enqueued before it on the stream is still running, once all of
+// that one's CTAs have called let_next_begin(); it calls wait_for_previous() before it reads what that one writes, and
+// before it ends in any case, so that the stream's order holds for whatever comes behind.
+template <class... Params, class... Args>
+dg4_status dg4i_launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t st, bool early, Args&&... args) {
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid; c.blockDim = dim3((unsigned)threads); c.dynamicSmemBytes = (size_t)smem; c.stream = st;
+    cudaLaunchAttribute at = {};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &at; c.numAttrs = early ? 1 : 0;
+    DG4_CUDA_TRY(cudaLaunchKernelEx(&c, kernel, std::forward<Args>(args)...));
+    dg4i_count_launch();
+    return DG4_OK;
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+#endif
