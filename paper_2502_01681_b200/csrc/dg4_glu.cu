@@ -805,7 +805,6 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         mbar_fence_init();
         tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy);
     }
-    let_next_begin();                                // glu_reduce_kernel, which waits
     if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
     tc_fence_before();
     __syncthreads();
@@ -942,6 +941,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             if (lane == 0) mbar_arrive(bar(bars->a_full));
         }
         ok = ok && mbar_wait_relaxed_warp(bar(bars->w_done), 0, limit);
+        let_next_begin();                            // glu_reduce_kernel, which waits
         if (ok) {
             tc_fence_after();
             const int col = quad * 32 + lane;                        // an input (dWg, dWu) or an output (dWd)
