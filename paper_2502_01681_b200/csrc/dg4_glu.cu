@@ -1094,6 +1094,8 @@ extern "C" dg4_status dg4_glu_fwd(const dg4_graph* g, const dg4_desc* desc, cons
     const bool res = (desc->flags & DG4_FLAG_RESIDUAL) && H_res;
     if (res) CHECK(dg4i_check_tensor("H_res", H_res, ldh, 2, 128));
     CHECK(dg4i_check_tensor("Y", Y, ldy, 2, 128));
+    if ((Y == X && ldy != ldx) || (res && Y == H_res && ldy != ldh))
+        DG4_FAIL(DG4_ERR_INVALID_ARG, "Y in the place of X or H_res has another leading dimension");
     int sms;
     CHECK(sm_count(g->device, &sms));
     Maps m;
@@ -1128,6 +1130,8 @@ extern "C" dg4_status dg4_glu_bwd(const dg4_graph* g, const dg4_desc* desc, cons
     CHECK(check_weights(W_gate, W_up, W_down, d_ff, activation));
     CHECK(dg4i_check_tensor("dY", dY, lddy, 2, 128));
     if (dX) CHECK(dg4i_check_tensor("dX", dX, lddx, 2, 128));
+    if (dX && ((dX == X && lddx != ldx) || (dX == dY && lddx != lddy)))
+        DG4_FAIL(DG4_ERR_INVALID_ARG, "dX in the place of X or dY has another leading dimension");
     const bool weights = dW_gate || dW_up || dW_down;
     if (!dX && !weights) DG4_FAIL(DG4_ERR_INVALID_ARG, "neither dX nor the weights' gradients are asked for");
     int sms;

@@ -252,6 +252,8 @@ extern "C" dg4_status dg4_add_norm_fwd(const dg4_graph* g, const dg4_desc* desc,
     if (Z) CHECK(dg4i_check_tensor("Z", Z, ldz, es, 128));
     CHECK(dg4i_check_tensor("Y", Y, ldy, es, 128));
     if (Z == Y) DG4_FAIL(DG4_ERR_INVALID_ARG, "Z and Y are the same buffer");
+    if ((Z && Z == X && ldz != ldx) || (Z && Z == R && ldz != ldr) || (Y == X && ldy != ldx) || (Y == R && ldy != ldr))
+        DG4_FAIL(DG4_ERR_INVALID_ARG, "an output in the place of X or R has another leading dimension");
     const FwdArgs a = {X, ldx * es, R, ldr * es, Z, ldz * es, Y, ldy * es, gamma, beta, g->n, eps};
     const bool rms = (desc->flags & DG4_FLAG_RMS_NORM) != 0;
     const cudaStream_t st = (cudaStream_t)stream;
@@ -283,6 +285,8 @@ extern "C" dg4_status dg4_norm_bwd(const dg4_graph* g, const dg4_desc* desc, con
     CHECK(check_vec("dbeta", dbeta, true));
     const bool sums = dgamma || dbeta, rms = (desc->flags & DG4_FLAG_RMS_NORM) != 0;
     if (!dZ && !sums) DG4_FAIL(DG4_ERR_INVALID_ARG, "none of dZ, dgamma and dbeta is asked for");
+    if (dZ && ((dZ == Z && lddz != ldz) || (dZ == dY && lddz != lddy) || (dZ == D_res && lddz != lddr)))
+        DG4_FAIL(DG4_ERR_INVALID_ARG, "dZ in the place of Z, dY or D_res has another leading dimension");
     if (dgamma && dgamma == dbeta) DG4_FAIL(DG4_ERR_INVALID_ARG, "dgamma and dbeta are the same buffer");
     int ctas;
     CHECK(bwd_ctas(es == 2, rms, g->n, &ctas));
