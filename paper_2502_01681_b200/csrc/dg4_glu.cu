@@ -67,33 +67,35 @@ __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32
 
 // SiLU x * sigmoid(x), GELU by its tanh form x * sigmoid(2 sqrt(2/pi) (x + 0.044715 x^3)), ReLU max(0, x).
 constexpr float kLog2e = 1.4426950408889634f, kGelu1 = 1.5957691216057308f, kGelu3 = 0.07135481282052f;
-// sigmoid(p(g)) of eight values.  The special-function unit is what bounds the epilogues (an exponential and a reciprocal
-// per value: 1024 clocks per block and SM, the products 768), so four values share a reciprocal: 1/x = y / (xy).  Where the
-// exponentials are too large for that (2^31: g below -21 or so), and for NaN, which would reach the other values, each has
-// its own.
+// sigmoid(p(g)) of eight values.  The special-function unit is what would bound the epilogues (an exponential and a reciprocal
+// per value: 1024 clocks per block and SM, the products of the forward pass 768), so four values share a reciprocal:
+// 1/x = y / (xy).  Where the product of the four is too large for that (2^126; four gates near -22, or one below -87), and for
+// NaN, which would reach the other values, each has its own.
 template <int ACT>
 __device__ __forceinline__ void sigmoid8(const float* g, float* s) {
-    float e[8], d[8];
-    float top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-        const Pair x = pair(g[i], g[i + 1]);
-        Pair p;
-        if (ACT == DG4_ACT_SILU) p = mul2(x, pair(-kLog2e, -kLog2e));
-        else p = mul2(x, fma2(mul2(x, x), pair(-kLog2e * kGelu3, -kLog2e * kGelu3), pair(-kLog2e * kGelu1, -kLog2e * kGelu1)));
-        split(p, e[i], e[i + 1]);
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(e[i]));
-        asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(e[i + 1]));
-        split(add2(pair(ex2(e[i]), ex2(e[i + 1])), pair(1.f, 1.f)), d[i], d[i + 1]);
-    }
+    float e[8];
+    bool each = false;
 #pragma unroll
     for (int i = 0; i < 8; i += 4) {
-        const float d01 = d[i] * d[i + 1], d23 = d[i + 2] * d[i + 3], r = rcp(d01 * d23);
-        const Pair r01 = mul2(pair(r, r), pair(d23, d23)), r23 = mul2(pair(r, r), pair(d01, d01));
-        split(mul2(r01, pair(d[i + 1], d[i])), s[i], s[i + 1]);
-        split(mul2(r23, pair(d[i + 3], d[i + 2])), s[i + 2], s[i + 3]);
+        Pair d[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const Pair x = pair(g[i + 2 * j], g[i + 2 * j + 1]);
+            Pair p;
+            if (ACT == DG4_ACT_SILU) p = mul2(x, pair(-kLog2e, -kLog2e));
+            else p = mul2(x, fma2(mul2(x, x), pair(-kLog2e * kGelu3, -kLog2e * kGelu3), pair(-kLog2e * kGelu1, -kLog2e * kGelu1)));
+            split(p, e[i + 2 * j], e[i + 2 * j + 1]);
+            d[j] = add2(pair(ex2(e[i + 2 * j]), ex2(e[i + 2 * j + 1])), pair(1.f, 1.f));
+        }
+        float d0, d1, d2, d3;
+        split(d[0], d0, d1);
+        split(d[1], d2, d3);
+        const float d01 = d0 * d1, d23 = d2 * d3, all = d01 * d23, r = rcp(all);
+        each = each || !(all <= 0x1p126f);
+        const float r01 = r * d23, r23 = r * d01;
+        s[i] = r01 * d1; s[i + 1] = r01 * d0; s[i + 2] = r23 * d3; s[i + 3] = r23 * d2;
     }
-    if (!(top <= 31.f)) {
+    if (each) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] = rcp(1.f + ex2(e[i]));
     }
@@ -138,14 +140,16 @@ __device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t
             } else {
                 const Pair x = pair(g[i], g[i + 1]), ss = pair(s[i], s[i + 1]);
                 act = mul2(x, ss);
-                Pair t = mul2(act, fma2(ss, pair(-1.f, -1.f), pair(1.f, 1.f)));
+                const Pair rest = fma2(ss, pair(-1.f, -1.f), pair(1.f, 1.f));
                 if (ACT == DG4_ACT_GELU) {
                     // beyond |g| = 1000 s or 1 - s is zero: p' is kept finite there
                     float x0, x1;
                     split(mul2(x, x), x0, x1);
-                    t = mul2(t, fma2(pair(fminf(x0, 1e6f), fminf(x1, 1e6f)), pair(3.f * kGelu3, 3.f * kGelu3), pair(kGelu1, kGelu1)));
+                    const Pair dp = fma2(pair(fminf(x0, 1e6f), fminf(x1, 1e6f)), pair(3.f * kGelu3, 3.f * kGelu3), pair(kGelu1, kGelu1));
+                    slope = fma2(mul2(act, rest), dp, ss);
+                } else {
+                    slope = fma2(act, rest, ss);
                 }
-                slope = add2(t, ss);
             }
             float lo, hi;
             split(mul2(hh, act), lo, hi);
