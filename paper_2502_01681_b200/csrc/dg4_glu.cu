@@ -512,16 +512,18 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
 // ---------------------------------------------------------------------------------------------------
 // Pairs of CTAs as in the forward kernel.  Of a block each fetches Wg or Wu (for G|U), its half of the inputs of both (for
 // dX) and its half of the hidden units of Wd (for dA).
-// Tensor memory: dX in columns 0..127, two buffers of G | U | dA behind it.  dG overwrites G, dU overwrites U, 16 values in 8
-// of the columns they were computed from.
+// Tensor memory: dX in columns 0..127, two buffers of G | U | dA behind it.  dG and dU overwrite dA, 16 values of each in the
+// 16 columns of dA they were computed from; G and U are free for the next product once they have been read.
 namespace dx {
 constexpr int kStages = 4, kBufs = 2, kBufCols = 192;
 constexpr int kGuBytes = kBlock * 256, kInBytes = 2 * kBlock * 128, kWdBytes = kTileM * 64;
 constexpr int kStageBytes = kGuBytes + kInBytes + kWdBytes;
 constexpr int kOffW = 2 * kTileBytes, kOffBars = kOffW + kStages * kStageBytes;
 struct Bars {
-    uint64_t x_full, x_empty, w_full[kStages], w_empty[kStages];
-    uint64_t ready[kStages], a_ready[kBufs], y_empty;             // rank 0's, both CTAs arrive
+    uint64_t x_full, x_empty, dy_full, dy_empty, w_full[kStages], w_empty[kStages];
+    // rank 0's, both CTAs arrive: a block's weights (and X) have come, dY has, G and U have been read, dG and dU are there, dX
+    // has been read
+    uint64_t ready[kStages], dy_ready, gu_read[kBufs], a_ready[kBufs], y_empty;
     uint64_t acc_full[kBufs], y_full[2], drain;
     uint32_t tmem_base, abort_flag;
 };
@@ -546,8 +548,9 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 
     if (threadIdx.x == 0) {
         mbar_init(bar(bars->x_full), 1); mbar_init(bar(bars->x_empty), 1);
+        mbar_init(bar(bars->dy_full), 1); mbar_init(bar(bars->dy_empty), 1); mbar_init(bar(bars->dy_ready), 2);
         for (int i = 0; i < kStages; ++i) { mbar_init(bar(bars->w_full[i]), 1); mbar_init(bar(bars->w_empty[i]), 1); mbar_init(bar(bars->ready[i]), 2); }
-        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
+        for (int i = 0; i < kBufs; ++i) { mbar_init(bar(bars->acc_full[i]), 1); mbar_init(bar(bars->gu_read[i]), 2 * kSetWarps); mbar_init(bar(bars->a_ready[i]), 2 * kSetWarps); }
         mbar_init(bar(bars->y_full[0]), 1); mbar_init(bar(bars->y_full[1]), 1); mbar_init(bar(bars->y_empty), 2 * kSetWarps); mbar_init(bar(bars->drain), 1);
         bars->abort_flag = 0;
         mbar_fence_init();
@@ -587,23 +590,32 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     } else if (warp == 3) {
         // ------------------------------------------------------------------ X and dY
         if (lane == 0) {
-            int t = 0;
-            for (; t < tiles && !*abort_flag; ++t) {
-                if (t > 0 && !mbar_wait_relaxed(bar(bars->x_empty), (uint32_t)(t - 1) & 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
-                mbar_expect_tx(bar(bars->x_full), 2 * kTileBytes);
+            int armed_x = 0, armed_dy = 0;
+            bool ok = true;
+            for (int t = 0; t < tiles && ok && !*abort_flag; ++t) {
+                ok = t == 0 || mbar_wait_relaxed(bar(bars->x_empty), (uint32_t)(t - 1) & 1u, limit);
+                if (!ok) break;
+                mbar_expect_tx(bar(bars->x_full), kTileBytes);
                 load_tile(&map_x, base, row_of(t), bar(bars->x_full));
-                load_tile(&map_dy, base + kTileBytes, row_of(t), bar(bars->x_full));
+                armed_x = t + 1;
+                ok = t == 0 || mbar_wait_relaxed(bar(bars->dy_empty), (uint32_t)(t - 1) & 1u, limit);
+                if (!ok) break;
+                mbar_expect_tx(bar(bars->dy_full), kTileBytes);
+                load_tile(&map_dy, base + kTileBytes, row_of(t), bar(bars->dy_full));
+                armed_dy = t + 1;
                 if (t + 1 < tiles) {                                 // the next tile's rows into L2 meanwhile
                     prefetch_tile(&map_x, row_of(t + 1));
                     prefetch_tile(&map_dy, row_of(t + 1));
                 }
             }
-            if (t > 0) mbar_wait(bar(bars->x_full), (uint32_t)(t - 1) & 1u);
+            if (!ok) raise_timeout_pair(bars, p.status, rank);
+            if (armed_x > 0) mbar_wait(bar(bars->x_full), (uint32_t)(armed_x - 1) & 1u);
+            if (armed_dy > 0) mbar_wait(bar(bars->dy_full), (uint32_t)(armed_dy - 1) & 1u);
         }
     } else if (warp == 2) {
         // ------------------------------------------------------------------ tells rank 0 what has come
         if (lane == 0) {
-            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), 0);
+            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), 0), dy_ready0 = cluster_addr(bar(bars->dy_ready), 0);
             Turn w;
             uint32_t x_odd = 0;
             bool ok = true;
@@ -614,6 +626,10 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 }
                 ok = ok && mbar_wait_relaxed(bar(bars->w_full[w.at]), w.odd, limit);
                 if (ok) mbar_arrive_cluster(ready0 + w.at * 8);
+                if (b == 0) {
+                    ok = ok && mbar_wait_relaxed(bar(bars->dy_full), x_odd ^ 1u, limit);
+                    if (ok) mbar_arrive_cluster(dy_ready0);
+                }
                 if (++b == nb) b = 0;
             }
             if (!ok) raise_timeout_pair(bars, p.status, rank);
@@ -627,48 +643,64 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                        low_in = desc_low(smem_desc_sw128_mn(base + kOffW + kGuBytes, kHalfBytes)), low_wd = desc_low(smem_desc_sw64_mn(base + kOffW + kGuBytes + kInBytes));
         Turn w1, w2, buf1, buf2;
         int b1 = 0, b2 = 0;
-        uint32_t y_odd = 1;
+        uint32_t y_odd = 1, dy_odd = 0;
         bool ok = true;
-        for (int c = 0; c < total + 1 && ok; ++c) {
-            const bool r1 = mbar_test(bar(bars->ready[w1.at]), w1.odd), r2 = mbar_test(bar(bars->a_ready[buf2.at]), buf2.odd);
+        // Per block: G|U as soon as the epilogue has read the block before the last out of this buffer, then dX's product of that
+        // block, then this one's dA in the place of that one's dG and dU.  (With G|U behind dX's product too, a block's
+        // products wait for the whole epilogue of the block before the last: 119 us instead of 113 on 208 384 rows.)
+        for (int c = 0; c < total + 2 && ok; ++c) {
+            const bool r1 = mbar_test(bar(bars->ready[w1.at]), w1.odd) && mbar_test(bar(bars->gu_read[buf1.at]), buf1.odd ^ 1u);
+            const bool r2 = mbar_test(bar(bars->a_ready[buf2.at]), buf2.odd);
             const uint32_t come = __reduce_and_sync(0xffffffffu, (r1 ? 1u : 0u) | (r2 ? 2u : 0u));
+            const uint32_t w = w1.at * (kStageBytes >> 4), d = tmem + 128 + buf1.at * kBufCols;
             if (c < total) {
-                if (!(come & 1u)) ok = await(bars, bar(bars->ready[w1.at]), w1.odd, limit);
+                if (!(come & 1u)) ok = await(bars, bar(bars->ready[w1.at]), w1.odd, limit) && await(bars, bar(bars->gu_read[buf1.at]), buf1.odd ^ 1u, limit);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t w = w1.at * (kStageBytes >> 4), d = tmem + 128 + buf1.at * kBufCols;
                 if (elected) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)
                         mma_pair(d, low_x + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
                                  low_gu + w + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, id_gu, ks > 0 ? 1u : 0u);
-#pragma unroll
-                    for (int ks = 0; ks < 8; ++ks)                   // dA = dY Wd: Wd's rows run along K
-                        mma_pair(d + 128, low_dy + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
-                                 low_wd + w + ks * (1024 >> 4), high_wd, id_da, ks > 0 ? 1u : 0u);
-                    mma_commit_pair(bar(bars->acc_full[buf1.at]));
                     if (b1 + 1 == nb) mma_commit_pair(bar(bars->x_empty));
                 }
                 __syncwarp();
-                w1.next(kStages); buf1.next(kBufs);
-                if (++b1 == nb) b1 = 0;
             }
-            if (c >= 1) {
+            if (c >= 2) {
                 if (!(come & 2u)) ok = await(bars, bar(bars->a_ready[buf2.at]), buf2.odd, limit);
                 if (ok && b2 == 0) { ok = await(bars, bar(bars->y_empty), y_odd, limit); y_odd ^= 1u; }
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t w = low_in + w2.at * (kStageBytes >> 4), a = tmem + 128 + buf2.at * kBufCols;
+                const uint32_t in = low_in + w2.at * (kStageBytes >> 4), a = tmem + 128 + buf2.at * kBufCols + 128;
                 if (elected) {
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)                   // dX += [dG | dU] [Wg; Wu]: their rows run along K
-                        mma_pair_ta(tmem, a + ks * 16, w + ks * (2048 >> 4), high, id_dx, (b2 | ks) ? 1u : 0u);
+                        mma_pair_ta(tmem, a + (ks & 3) * 16 + (ks >> 2) * 8, in + ks * (2048 >> 4), high, id_dx, (b2 | ks) ? 1u : 0u);
                     if (b2 + 1 == nb) mma_commit_pair(bar(bars->y_full[y_odd]));
                     mma_commit_pair(bar(bars->w_empty[w2.at]));
                 }
                 __syncwarp();
                 w2.next(kStages); buf2.next(kBufs);
                 if (++b2 == nb) b2 = 0;
+            }
+            if (c < total) {
+                if (b1 == 0) {
+                    ok = await(bars, bar(bars->dy_ready), dy_odd, limit);
+                    dy_odd ^= 1u;
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                if (elected) {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)                   // dA = dY Wd: Wd's rows run along K
+                        mma_pair(d + 128, low_dy + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
+                                 low_wd + w + ks * (1024 >> 4), high_wd, id_da, ks > 0 ? 1u : 0u);
+                    mma_commit_pair(bar(bars->acc_full[buf1.at]));
+                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->dy_empty));
+                }
+                __syncwarp();
+                w1.next(kStages); buf1.next(kBufs);
+                if (++b1 == nb) b1 = 0;
             }
         }
         if (!ok) raise_timeout_pair(bars, p.status, rank);
@@ -680,7 +712,8 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         // as in the forward kernel: two sets of warps, dX of a tile after the next one's first block
         const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), 0), y_empty0 = cluster_addr(bar(bars->y_empty), 0);
+        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), 0), gu_read0 = cluster_addr(bar(bars->gu_read[0]), 0),
+                       y_empty0 = cluster_addr(bar(bars->y_empty), 0);
         Turn buf;
         bool ok = true;
         int turn = set;
@@ -722,14 +755,19 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     tmem_ld_32x16(at + 64, u);
                     tmem_ld_32x16(at + 128, h);
                     tmem_ld_wait();
+                    if (c == 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(gu_read0 + buf.at * 8);
+                    }
                     gated_bwd<ACT, false>(g, u, h, dg, du, nullptr);
                     const int valid = p.d_ff - b * kBlock - part * 32 - c * kEl;
                     if (valid < kEl) {
 #pragma unroll
                         for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) dg[i] = du[i] = 0u;
                     }
-                    tmem_st_32x8(at, dg);
-                    tmem_st_32x8(at + 64, du);
+                    tmem_st_32x8(at + 128, dg);
+                    tmem_st_32x8(at + 136, du);
                 }
                 tmem_st_wait();
                 tc_fence_before();
