@@ -268,6 +268,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         tma_prefetch_desc(&map_wd); tma_prefetch_desc(&map_y);
     }
     if (warp == 1) tmem_alloc_pair(smem_u32(&bars->tmem_base), 512);
+    let_next_begin();
+    wait_for_previous();
     tc_fence_before();
     __syncthreads();
     cluster_sync();                                  // the other CTA's barriers are there too
@@ -557,8 +559,9 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy); tma_prefetch_desc(&map_wg); tma_prefetch_desc(&map_wu);
         tma_prefetch_desc(&map_wd);
     }
-    let_next_begin();                                // glu_dw_kernel needs nothing of this one: few rows leave SMs for it
     if (warp == 1) tmem_alloc_pair(smem_u32(&bars->tmem_base), 512);
+    wait_for_previous();
+    let_next_begin();                                // glu_dw_kernel needs nothing of this one: few rows leave SMs for it
     tc_fence_before();
     __syncthreads();
     cluster_sync();
@@ -816,6 +819,7 @@ static_assert(kSmem <= kSmemLimit, "shared memory");
 }  // namespace dw
 
 struct DwOut {
+    int32_t beside_dx;                             // the kernel before is dX's, which has waited for what came before it
     float* part;                                   // [groups][blocks][kPart], or null: one group, straight to bf16
     __nv_bfloat16 *wg, *wu, *wd;
 };
@@ -848,6 +852,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         tma_prefetch_desc(&map_x); tma_prefetch_desc(&map_dy);
     }
     if (warp == 1) tmem_alloc(smem_u32(&bars->tmem_base), 512);
+    if (!out.beside_dx) wait_for_previous();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -1028,6 +1033,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 // One CTA per hidden unit and matrix, one thread per input or output: the groups' sums in the order of the groups.
 __global__ void glu_reduce_kernel(DwOut out, int d_ff, int n_blocks, int groups) {
     const int unit = blockIdx.x, m = blockIdx.y, col = threadIdx.x;
+    let_next_begin();
     wait_for_previous();
     const float* src = out.part + (int64_t)(unit / kBlock) * dw::kPart + (m * kBlock + unit % kBlock) * 128 + col;
     float f = 0.f;
@@ -1096,7 +1102,7 @@ int pair_grid(const Params& p, int sms) { return 2 * (p.n_tiles < sms / 2 ? p.n_
 template <int ACT>
 dg4_status launch_fwd(const Maps& m, const Params& p, int dev, int sms, cudaStream_t st) {
     CHECK(allow_smem<glu_fwd_kernel<ACT>>(dev, fwd::kSmem));
-    CHECK(dg4i_launch(glu_fwd_kernel<ACT>, dim3(pair_grid(p, sms)), kThreads, fwd::kSmem, st, false, m.x, m.wg, m.wu, m.wd, m.r, m.y, p));
+    CHECK(dg4i_launch(glu_fwd_kernel<ACT>, dim3(pair_grid(p, sms)), kThreads, fwd::kSmem, st, true, m.x, m.wg, m.wu, m.wd, m.r, m.y, p));
     return DG4_OK;
 }
 
@@ -1106,11 +1112,11 @@ dg4_status launch_bwd(const Maps& m, const Params& p, const DwOut& out, int grou
         CHECK(allow_smem<glu_dx_kernel<ACT>>(dev, dx::kSmem));
         Params q = p;
         q.n_tiles = (p.n_tiles + 1) / 2;
-        CHECK(dg4i_launch(glu_dx_kernel<ACT>, dim3(pair_grid(q, sms)), kThreads, dx::kSmem, st, false, m.x, m.dy, m.wg, m.wu, m.wd_half, q));
+        CHECK(dg4i_launch(glu_dx_kernel<ACT>, dim3(pair_grid(q, sms)), kThreads, dx::kSmem, st, true, m.x, m.dy, m.wg, m.wu, m.wd_half, q));
     }
     if (out.wg) {
         CHECK(allow_smem<glu_dw_kernel<ACT>>(dev, dw::kSmem));
-        CHECK(dg4i_launch(glu_dw_kernel<ACT>, dim3(p.n_blocks, groups), kThreads, dw::kSmem, st, p.out != nullptr, m.x, m.dy, m.wg, m.wu, m.wd, p, out));
+        CHECK(dg4i_launch(glu_dw_kernel<ACT>, dim3(p.n_blocks, groups), kThreads, dw::kSmem, st, true, m.x, m.dy, m.wg, m.wu, m.wd, p, out));
         if (out.part) CHECK(dg4i_launch(glu_reduce_kernel, dim3(p.d_ff, 3), 128, 0, st, true, out, p.d_ff, p.n_blocks, groups));
     }
     return DG4_OK;
@@ -1179,6 +1185,7 @@ extern "C" dg4_status dg4_glu_bwd(const dg4_graph* g, const dg4_desc* desc, cons
     int sms;
     CHECK(sm_count(g->device, &sms));
     DwOut out = {};
+    out.beside_dx = dX != nullptr;
     const int groups = groups_of(g, d_ff, sms);
     if (weights) {
         CHECK(dg4i_check_tensor("dW_gate", dW_gate, 128, 2, 128));

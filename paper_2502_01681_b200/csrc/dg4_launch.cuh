@@ -27,8 +27,10 @@ dg4_status dg4i_resident_blocks(int threads, int* out) {
 }
 
 // Launches a kernel.  `early`: it may begin while the kernel enqueued before it on the stream is still running, once all of
-// that one's CTAs have called let_next_begin(); it calls wait_for_previous() before it reads what that one writes, and
-// before it ends in any case, so that the stream's order holds for whatever comes behind.
+// that one's CTAs have called let_next_begin() (a kernel that does not call it lets the next begin when it has ended).  All
+// its threads call wait_for_previous() before they touch global memory, which leaves the launch and the set-up to overlap: a
+// few us of a small call.  A kernel that needs nothing of the one before may call it later, but before it ends, so that the
+// stream's order holds for whatever comes behind; that one lets it begin behind its own wait.
 template <class... Params, class... Args>
 dg4_status dg4i_launch(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t st, bool early, Args&&... args) {
     cudaLaunchConfig_t c = {};

@@ -54,6 +54,8 @@ template <bool BF16, bool RMS>
 __global__ void __launch_bounds__(kThreads, 2) add_norm_kernel(FwdArgs a) {
     __shared__ float4 vec[2][32];
     const int lane = threadIdx.x & 31, sub = lane & (kLanes - 1), grp = lane / kLanes;
+    let_next_begin();
+    wait_for_previous();
     if (threadIdx.x < 64) stage_vec<BF16>(vec[threadIdx.x >> 5], threadIdx.x < 32 ? a.gamma : a.beta, 0.f, threadIdx.x & 31);
     __syncthreads();
     const uint32_t n = (uint32_t)a.n, step = gridDim.x * kWarps * kRows;
@@ -86,6 +88,8 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_kernel(BwdArgs a) {
     __shared__ float4 vec[32];
     __shared__ float4 sum[kWarps][2][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane & (kLanes - 1), grp = lane / kLanes;
+    let_next_begin();
+    wait_for_previous();
     if (threadIdx.x < 32) stage_vec<BF16>(vec, a.gamma, 1.f, threadIdx.x);
     __syncthreads();
     const uint32_t n = (uint32_t)a.n, step = gridDim.x * kWarps * kRows;
@@ -149,7 +153,6 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_kernel(BwdArgs a) {
         }
         if (a.dZ && in) Raw<BF16>::store((char*)a.dZ + (int64_t)row * a.lddz, sub, t);
     }
-    let_next_begin();                                                // norm_reduce_kernel, which waits
     if (!a.sums) return;
 #pragma unroll
     for (int i = 0; i < kPairs / 2; ++i) {
@@ -178,6 +181,7 @@ __global__ void __launch_bounds__(kThreads, 2) norm_bwd_kernel(BwdArgs a) {
 // 32 of the 256 sums per CTA, a warp per 32nd CTA of norm_bwd_kernel.
 __global__ void __launch_bounds__(1024) norm_reduce_kernel(const float* part, int ctas, float* dgamma, float* dbeta) {
     __shared__ float sum[32][33];
+    let_next_begin();
     wait_for_previous();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = blockIdx.x * 32 + lane;
     float f = 0.f;
@@ -205,10 +209,7 @@ template <bool BF16, bool RMS>
 dg4_status launch_fwd(const FwdArgs& a, cudaStream_t st) {
     int resident;
     CHECK((dg4i_resident_blocks<add_norm_kernel<BF16, RMS>>(kThreads, &resident)));
-    add_norm_kernel<BF16, RMS><<<ctas_of(a.n, resident), kThreads, 0, st>>>(a);
-    dg4i_count_launch();
-    DG4_CUDA_TRY(cudaGetLastError());
-    return DG4_OK;
+    return dg4i_launch(add_norm_kernel<BF16, RMS>, dim3(ctas_of(a.n, resident)), kThreads, 0, st, true, a);
 }
 
 // CTAs of the backward kernel: one where its sums are to be final, else as many as the device holds.
@@ -226,7 +227,7 @@ dg4_status bwd_ctas(bool bf16, bool rms, int n, int* out) {
 
 template <bool BF16, bool RMS>
 dg4_status launch_bwd(const BwdArgs& a, int ctas, cudaStream_t st) {
-    CHECK(dg4i_launch(norm_bwd_kernel<BF16, RMS>, dim3(ctas), kThreads, 0, st, false, a));
+    CHECK(dg4i_launch(norm_bwd_kernel<BF16, RMS>, dim3(ctas), kThreads, 0, st, true, a));
     if (a.part) CHECK(dg4i_launch(norm_reduce_kernel, dim3(8), 1024, 0, st, true, (const float*)a.part, ctas, a.dgamma, a.dbeta));
     return DG4_OK;
 }
