@@ -54,6 +54,9 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, const uint32_t* r) {
 __device__ __forceinline__ void ld_shared_v4(uint32_t addr, uint32_t* r) {
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void ld_global_v4(const void* p, uint32_t* r) {
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p) : "memory");
+}
 __device__ __forceinline__ void st_global_v4(void* p, const uint32_t* r) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
@@ -166,8 +169,9 @@ __device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t
 
 struct Params {
     int32_t n, d_ff, n_tiles, n_blocks;
-    int32_t has_res;                         // forward: a residual is added
-    __nv_bfloat16* out; int64_t ldo;         // backward: dX
+    int32_t splits;                          // pairs of CTAs that share a tile's blocks: 1, 2 or 4
+    const __nv_bfloat16* R; int64_t ldr;     // forward: nullable residual
+    __nv_bfloat16* out; int64_t ldo;         // Y, or dX
     int32_t* status;
     uint32_t poll_limit;
 };
@@ -192,10 +196,75 @@ __device__ __forceinline__ bool await(Bars* bars, uint32_t bar, uint32_t parity,
 
 // The pair's form: the other CTA's roles are told too.
 template <class Bars>
-__device__ __forceinline__ void raise_timeout_pair(Bars* bars, int32_t* status, uint32_t rank) {
+__device__ __forceinline__ void raise_timeout_pair(Bars* bars, int32_t* status, uint32_t in_cluster) {
     raise_timeout(bars, status);
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(&bars->abort_flag), rank ^ 1u)), "r"(1u) : "memory");
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(smem_u32(&bars->abort_flag), in_cluster ^ 1u)), "r"(1u) : "memory");
 }
+
+// Few rows: the pairs of a cluster share a tile, each with every `splits`-th block, and their sums are joined through
+// distributed shared memory, each pair finishing 128 / splits of the columns.  The epilogue warps send the others' columns of
+// the sum (tensor memory, columns 0..127) into the first 64 KB of their CTAs' shared memory, which nothing uses any more
+// (`send`); behind a barrier of the cluster each pair adds the parts up in the order of the pairs (`collect`).
+struct Split {
+    int splits, split, part, quad, lane;                         // part: 32 of the 128 columns
+    uint32_t tmem, base, rank;
+    __device__ __forceinline__ int owner() const { return part * splits / 4; }
+    // 128 rows of 32 columns in fp32, the 16-byte pieces of a row swizzled
+    __device__ __forceinline__ uint32_t slot(int from, int piece) const {
+        const int row = quad * 32 + lane, at = from * (4 / splits) + part % (4 / splits);
+        return base + (uint32_t)(at * 16384 + row * 128 + ((piece ^ (row & 7)) << 4));
+    }
+    __device__ __forceinline__ void load(uint32_t* y) const {
+        tmem_ld_32x32(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(part * 32), y);
+        tmem_ld_wait();
+    }
+    __device__ __forceinline__ void send() const {
+        if (owner() == split) return;
+        uint32_t y[32];
+        load(y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(cluster_addr(slot(split, i), (uint32_t)owner() * 2 + rank)),
+                         "r"(y[4 * i]), "r"(y[4 * i + 1]), "r"(y[4 * i + 2]), "r"(y[4 * i + 3]) : "memory");
+    }
+    // `row`: this lane's row of the tensors, -1 if there is none.  R (nullable): its 32 values are fetched by `residual`.
+    __device__ __forceinline__ void residual(uint32_t* r, int64_t row, const __nv_bfloat16* R, int64_t ldr) const {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r[i] = 0u;
+        if (owner() != split || row < 0 || !R) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ld_global_v4(R + row * ldr + part * 32 + i * 8, r + 4 * i);
+    }
+    __device__ __forceinline__ void collect(int64_t row, const uint32_t* r, __nv_bfloat16* out, int64_t ldo) const {
+        if (owner() != split) return;
+        uint32_t own[32];
+        load(own);
+        if (row < 0) return;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {                             // eight columns
+            float f[8] = {};
+            for (int q = 0; q < splits; ++q) {
+                uint32_t v[8];
+                if (q != split) {
+                    ld_shared_v4(slot(q, i), v);
+                    ld_shared_v4(slot(q, i + 1), v + 4);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] += __uint_as_float(q != split ? v[e] : own[4 * i + e]);
+            }
+            const int64_t col = part * 32 + i * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[2 * e] += __uint_as_float(r[2 * i + e] << 16);
+                f[2 * e + 1] += __uint_as_float(r[2 * i + e] & 0xffff0000u);
+            }
+            uint32_t o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = pack_bf16(f[2 * e], f[2 * e + 1]);
+            st_global_v4(out + row * ldo + col, o);
+        }
+    }
+};
 
 // One block's Wg and Wu: two panels of 64 inputs, each 64 rows of Wg and 64 of Wu.
 __device__ __forceinline__ void load_gu(const CUtensorMap* wg, const CUtensorMap* wu, uint32_t dst, int block, uint32_t bar) {
@@ -242,7 +311,7 @@ static_assert(kSmem <= kSmemLimit, "shared memory");
 }  // namespace fwd
 
 template <int ACT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_wg,
                const __grid_constant__ CUtensorMap map_wu, const __grid_constant__ CUtensorMap map_wd,
                const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_y, Params p) {
@@ -251,8 +320,9 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
     const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int nb = p.n_blocks;
-    const uint32_t rank = cluster_rank();
+    const uint32_t in_cluster = cluster_rank(), rank = in_cluster & 1u, lead = in_cluster & ~1u, mask = 3u << lead;
+    const int splits = p.splits, split = (int)(in_cluster >> 1), nb = (p.n_blocks - split + splits - 1) / splits;   // this pair's blocks
+    auto unit_of = [&](int b) { return (b * splits + split) * kBlock; };                                           // and their first units
     volatile uint32_t* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
 
@@ -275,10 +345,11 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     cluster_sync();                                  // the other CTA's barriers are there too
     tc_fence_after();
     const uint32_t tmem = uniform(bars->tmem_base);
-    const int pairs = (int)gridDim.x / 2, pair0 = (int)blockIdx.x / 2;
+    const int pairs = (int)gridDim.x / (2 * splits), pair0 = (int)blockIdx.x / (2 * splits);
     const int tiles = (p.n_tiles - pair0 + pairs - 1) / pairs, total = tiles * nb;
     auto row_of = [&](int t) { return (pair0 + t * pairs) * 2 * kTileM + (int)rank * kTileM; };
     const uint32_t limit = p.poll_limit;
+    const bool has_res = p.R != nullptr && splits == 1;          // through shared memory
 
     if (warp == 0) {
         // ------------------------------------------------------------------ weights: Wg or Wu, half of Wd's outputs
@@ -287,11 +358,11 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             Turn w;
             int c = 0, b = 0;
             for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
-                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, in_cluster); break; }
                 const uint32_t dst = base + kOffW + w.at * kStageBytes, full = bar(bars->w_full[w.at]);
                 mbar_expect_tx(full, kStageBytes);
-                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kBlock * 128, map, h * 64, b * kBlock, full);
-                tma_load_2d(dst + kGuBytes, &map_wd, b * kBlock, (int)rank * 64, full);
+                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kBlock * 128, map, h * 64, unit_of(b), full);
+                tma_load_2d(dst + kGuBytes, &map_wd, unit_of(b), (int)rank * 64, full);
                 if (++b == nb) b = 0;
             }
             // leave with no copy still landing in shared memory (these waits keep the default limit)
@@ -300,7 +371,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     } else if (warp == 2) {
         // ------------------------------------------------------------------ tells rank 0 what has come
         if (lane == 0) {
-            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), 0);
+            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), lead);
             Turn x, w;
             bool ok = true;
             for (int c = 0, b = 0; c < total && ok && !*abort_flag; ++c, w.next(kStages)) {
@@ -312,7 +383,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 if (ok) mbar_arrive_cluster(ready0 + w.at * 8);
                 if (++b == nb) b = 0;
             }
-            if (!ok) raise_timeout_pair(bars, p.status, rank);
+            if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
         }
     } else if (warp == 3) {
         // ------------------------------------------------------------------ X, and the residual of the tile before
@@ -328,7 +399,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                         armed_x = t + 1;
                     }
                 }
-                if (ok && t >= 1 && p.has_res) {                     // its place is free when the rows before have been stored
+                if (ok && t >= 1 && has_res) {                     // its place is free when the rows before have been stored
                     ok = t < 2 || mbar_wait_relaxed(bar(bars->r_empty[t & 1]), (uint32_t)(t / 2 - 1) & 1u, limit);
                     if (ok) {
                         const uint32_t full = bar(bars->r_full[(t - 1) & 1]);
@@ -338,7 +409,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     }
                 }
             }
-            if (!ok) raise_timeout_pair(bars, p.status, rank);
+            if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
             for (int i = max(0, armed_x - 2); i < armed_x; ++i) mbar_wait(bar(bars->x_full[i & 1]), (uint32_t)(i >> 1) & 1u);
             if (armed_r > 0) mbar_wait(bar(bars->r_full[(armed_r - 1) & 1]), (uint32_t)((armed_r - 1) >> 1) & 1u);
         }
@@ -364,8 +435,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             if (elected) {
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks) mma_pair_ta(tmem, a + ks * 16, wd + ks * 2, high, idesc, (b2 | ks) ? 1u : 0u);
-                if (b2 + 1 == nb) mma_commit_pair(bar(bars->y_full[y_odd]));
-                mma_commit_pair(bar(bars->w_empty[w2.at]));
+                if (b2 + 1 == nb) mma_commit_pair(bar(bars->y_full[y_odd]), mask);
+                mma_commit_pair(bar(bars->w_empty[w2.at]), mask);
             }
             __syncwarp();
             w2.next(kStages); buf2.next(kBufs);
@@ -388,8 +459,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     for (int ks = 0; ks < 8; ++ks)
                         mma_pair(to, dx + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
                                  dw + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, idesc, ks > 0 ? 1u : 0u);
-                    mma_commit_pair(bar(bars->acc_full[buf1.at]));
-                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->x_empty[x.at]));
+                    mma_commit_pair(bar(bars->acc_full[buf1.at]), mask);
+                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->x_empty[x.at]), mask);
                 }
                 __syncwarp();
                 w1.next(kStages); buf1.next(kBufs);
@@ -400,8 +471,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 if (ok) second();
             }
         }
-        if (!ok) raise_timeout_pair(bars, p.status, rank);
-        if (elected) mma_commit_pair(bar(bars->drain));  // tensor memory is freed below: every product must be done
+        if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
+        if (elected) mma_commit_pair(bar(bars->drain), mask);  // tensor memory is freed below: every product must be done
         __syncwarp();
         mbar_wait_warp(bar(bars->drain), 0);
     } else if (warp >= kCtrlWarps) {
@@ -412,7 +483,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
         const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const uint32_t stage = base + kOffR + part * kHalfBytes + quad * 4096;
-        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), 0), y_empty0 = cluster_addr(bar(bars->y_empty), 0);
+        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), lead), y_empty0 = cluster_addr(bar(bars->y_empty), lead);
         Turn buf;
         bool ok = true;
         int turn = set;                                              // 0: the next block is this set's
@@ -427,13 +498,13 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(y_empty0);
-            if (p.has_res ? !await(bars, bar(bars->r_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)
+            if (has_res ? !await(bars, bar(bars->r_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)
                           : t > 0 && !await(bars, bar(bars->r_empty[(t - 1) & 1]), (uint32_t)((t - 1) >> 1) & 1u, limit)) return false;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 uint32_t o[4], r[4] = {0u, 0u, 0u, 0u};
                 const uint32_t at = stage + sw128_offset(lane, i);
-                if (p.has_res) ld_shared_v4(at, r);
+                if (has_res) ld_shared_v4(at, r);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]) + __uint_as_float(r[e] << 16),
@@ -473,7 +544,7 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                     tmem_ld_32x16(at + 64, u);
                     tmem_ld_wait();
                     gated<ACT>(g, u, a);
-                    const int valid = p.d_ff - b * kBlock - part * 32 - c * kEl;   // hidden units past the last: zero
+                    const int valid = p.d_ff - unit_of(b) - part * 32 - c * kEl;   // hidden units past the last: zero
                     if (valid < kEl) {
 #pragma unroll
                         for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) a[i] = 0u;
@@ -494,8 +565,8 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             }
         }
         leave();
-        if (ok && turn == 0) ok = finish(tiles - 1);
-        if (!ok) raise_timeout_pair(bars, p.status, rank);
+        if (ok && turn == 0 && splits == 1) ok = finish(tiles - 1);
+        if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
         if (lane == 0) bulk_wait_all();
     }
 
@@ -503,6 +574,22 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
     __syncthreads();
     if (warp == 1 && rank == 1) mbar_wait_warp(bar(bars->drain), 0);   // the last arrival that rank 0's products send here
     cluster_sync();                                  // no product reads this CTA's memory any more, no arrival is on its way
+    if (splits > 1) {                                // uniform: all CTAs of the cluster go through its barriers
+        const int ew = warp - kCtrlWarps, row = row_of(0) + (warp & 3) * 32 + lane;
+        const Split s = {splits, split, ew >> 2, warp & 3, lane, tmem, base, rank};
+        uint32_t r[16];
+        tc_fence_after();
+        if (ew >= 0) {
+            s.residual(r, row < p.n ? row : -1, p.R, p.ldr);
+            s.send();
+        }
+        __syncwarp();
+        cluster_sync();
+        if (ew >= 0) s.collect(row < p.n ? row : -1, r, p.out, p.ldo);
+        __syncwarp();
+        tc_fence_before();
+        __syncthreads();
+    }
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc_pair(tmem, 512);
@@ -534,7 +621,7 @@ static_assert(kSmem <= kSmemLimit, "shared memory");
 }  // namespace dx
 
 template <int ACT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_dy,
               const __grid_constant__ CUtensorMap map_wg, const __grid_constant__ CUtensorMap map_wu,
               const __grid_constant__ CUtensorMap map_wd, Params p) {
@@ -543,8 +630,9 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     Bars* bars = reinterpret_cast<Bars*>(smem_raw + (base - smem_u32(smem_raw)) + kOffBars);
     const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-    const int nb = p.n_blocks;
-    const uint32_t rank = cluster_rank();
+    const uint32_t in_cluster = cluster_rank(), rank = in_cluster & 1u, lead = in_cluster & ~1u, mask = 3u << lead;
+    const int splits = p.splits, split = (int)(in_cluster >> 1), nb = (p.n_blocks - split + splits - 1) / splits;   // this pair's blocks
+    auto unit_of = [&](int b) { return (b * splits + split) * kBlock; };                                           // and their first units
     volatile uint32_t* abort_flag = &bars->abort_flag;
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
 
@@ -567,7 +655,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = uniform(bars->tmem_base);
-    const int pairs = (int)gridDim.x / 2, pair0 = (int)blockIdx.x / 2;
+    const int pairs = (int)gridDim.x / (2 * splits), pair0 = (int)blockIdx.x / (2 * splits);
     const int tiles = (p.n_tiles - pair0 + pairs - 1) / pairs, total = tiles * nb;
     auto row_of = [&](int t) { return (pair0 + t * pairs) * 2 * kTileM + (int)rank * kTileM; };
     const uint32_t limit = p.poll_limit;
@@ -579,13 +667,13 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             Turn w;
             int c = 0, b = 0;
             for (; c < total && !*abort_flag; ++c, w.next(kStages)) {
-                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, rank); break; }
+                if (c >= kStages && !mbar_wait_relaxed(bar(bars->w_empty[w.at]), w.odd ^ 1u, limit)) { raise_timeout_pair(bars, p.status, in_cluster); break; }
                 const uint32_t dst = base + kOffW + w.at * kStageBytes, full = bar(bars->w_full[w.at]);
                 mbar_expect_tx(full, kStageBytes);
-                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kBlock * 128, map, h * 64, b * kBlock, full);
-                tma_load_2d(dst + kGuBytes, &map_wg, (int)rank * 64, b * kBlock, full);
-                tma_load_2d(dst + kGuBytes + kBlock * 128, &map_wu, (int)rank * 64, b * kBlock, full);
-                tma_load_2d(dst + kGuBytes + kInBytes, &map_wd, b * kBlock + (int)rank * 32, 0, full);
+                for (int h = 0; h < 2; ++h) tma_load_2d(dst + h * kBlock * 128, map, h * 64, unit_of(b), full);
+                tma_load_2d(dst + kGuBytes, &map_wg, (int)rank * 64, unit_of(b), full);
+                tma_load_2d(dst + kGuBytes + kBlock * 128, &map_wu, (int)rank * 64, unit_of(b), full);
+                tma_load_2d(dst + kGuBytes + kInBytes, &map_wd, unit_of(b) + (int)rank * 32, 0, full);
                 if (++b == nb) b = 0;
             }
             for (int i = max(0, c - kStages); i < c; ++i) mbar_wait(bar(bars->w_full[i % kStages]), (uint32_t)(i / kStages) & 1u);
@@ -611,14 +699,14 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     prefetch_tile(&map_dy, row_of(t + 1));
                 }
             }
-            if (!ok) raise_timeout_pair(bars, p.status, rank);
+            if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
             if (armed_x > 0) mbar_wait(bar(bars->x_full), (uint32_t)(armed_x - 1) & 1u);
             if (armed_dy > 0) mbar_wait(bar(bars->dy_full), (uint32_t)(armed_dy - 1) & 1u);
         }
     } else if (warp == 2) {
         // ------------------------------------------------------------------ tells rank 0 what has come
         if (lane == 0) {
-            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), 0), dy_ready0 = cluster_addr(bar(bars->dy_ready), 0);
+            const uint32_t ready0 = cluster_addr(bar(bars->ready[0]), lead), dy_ready0 = cluster_addr(bar(bars->dy_ready), lead);
             Turn w;
             uint32_t x_odd = 0;
             bool ok = true;
@@ -635,7 +723,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 }
                 if (++b == nb) b = 0;
             }
-            if (!ok) raise_timeout_pair(bars, p.status, rank);
+            if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
         }
     } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ rank 0: issues the products
@@ -665,7 +753,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     for (int ks = 0; ks < 8; ++ks)
                         mma_pair(d, low_x + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
                                  low_gu + w + (((ks >> 2) * kBlock * 128 + (ks & 3) * 32) >> 4), high, id_gu, ks > 0 ? 1u : 0u);
-                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->x_empty));
+                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->x_empty), mask);
                 }
                 __syncwarp();
             }
@@ -679,8 +767,8 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 #pragma unroll
                     for (int ks = 0; ks < 8; ++ks)                   // dX += [dG | dU] [Wg; Wu]: their rows run along K
                         mma_pair_ta(tmem, a + (ks & 3) * 16 + (ks >> 2) * 8, in + ks * (2048 >> 4), high, id_dx, (b2 | ks) ? 1u : 0u);
-                    if (b2 + 1 == nb) mma_commit_pair(bar(bars->y_full[y_odd]));
-                    mma_commit_pair(bar(bars->w_empty[w2.at]));
+                    if (b2 + 1 == nb) mma_commit_pair(bar(bars->y_full[y_odd]), mask);
+                    mma_commit_pair(bar(bars->w_empty[w2.at]), mask);
                 }
                 __syncwarp();
                 w2.next(kStages); buf2.next(kBufs);
@@ -698,16 +786,16 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     for (int ks = 0; ks < 8; ++ks)                   // dA = dY Wd: Wd's rows run along K
                         mma_pair(d + 128, low_dy + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), high,
                                  low_wd + w + ks * (1024 >> 4), high_wd, id_da, ks > 0 ? 1u : 0u);
-                    mma_commit_pair(bar(bars->acc_full[buf1.at]));
-                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->dy_empty));
+                    mma_commit_pair(bar(bars->acc_full[buf1.at]), mask);
+                    if (b1 + 1 == nb) mma_commit_pair(bar(bars->dy_empty), mask);
                 }
                 __syncwarp();
                 w1.next(kStages); buf1.next(kBufs);
                 if (++b1 == nb) b1 = 0;
             }
         }
-        if (!ok) raise_timeout_pair(bars, p.status, rank);
-        if (elected) mma_commit_pair(bar(bars->drain));
+        if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
+        if (elected) mma_commit_pair(bar(bars->drain), mask);
         __syncwarp();
         mbar_wait_warp(bar(bars->drain), 0);
     } else if (warp >= kCtrlWarps) {
@@ -715,8 +803,8 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         // as in the forward kernel: two sets of warps, dX of a tile after the next one's first block
         const int ew = warp - kCtrlWarps, quad = warp & 3, set = ew / kSetWarps, part = (ew >> 2) & 1;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), 0), gu_read0 = cluster_addr(bar(bars->gu_read[0]), 0),
-                       y_empty0 = cluster_addr(bar(bars->y_empty), 0);
+        const uint32_t a_ready0 = cluster_addr(bar(bars->a_ready[0]), lead), gu_read0 = cluster_addr(bar(bars->gu_read[0]), lead),
+                       y_empty0 = cluster_addr(bar(bars->y_empty), lead);
         Turn buf;
         bool ok = true;
         int turn = set;
@@ -764,7 +852,7 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                         if (lane == 0) mbar_arrive_cluster(gu_read0 + buf.at * 8);
                     }
                     gated_bwd<ACT, false>(g, u, h, dg, du, nullptr);
-                    const int valid = p.d_ff - b * kBlock - part * 32 - c * kEl;
+                    const int valid = p.d_ff - unit_of(b) - part * 32 - c * kEl;
                     if (valid < kEl) {
 #pragma unroll
                         for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) dg[i] = du[i] = 0u;
@@ -783,14 +871,30 @@ glu_dx_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 }
             }
         }
-        if (ok && turn == 0) ok = finish(tiles - 1);
-        if (!ok) raise_timeout_pair(bars, p.status, rank);
+        if (ok && turn == 0 && splits == 1) ok = finish(tiles - 1);
+        if (!ok) raise_timeout_pair(bars, p.status, in_cluster);
     }
 
     tc_fence_before();
     __syncthreads();
     if (warp == 1 && rank == 1) mbar_wait_warp(bar(bars->drain), 0);
     cluster_sync();
+    if (splits > 1) {                                // uniform: all CTAs of the cluster go through its barriers
+        const int ew = warp - kCtrlWarps, row = row_of(0) + (warp & 3) * 32 + lane;
+        const Split s = {splits, split, ew >> 2, warp & 3, lane, tmem, base, rank};
+        uint32_t r[16];
+        tc_fence_after();
+        if (ew >= 0) {
+            s.residual(r, row < p.n ? row : -1, nullptr, 0);
+            s.send();
+        }
+        __syncwarp();
+        cluster_sync();
+        if (ew >= 0) s.collect(row < p.n ? row : -1, r, p.out, p.ldo);
+        __syncwarp();
+        tc_fence_before();
+        __syncthreads();
+    }
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc_pair(tmem, 512);
@@ -1096,23 +1200,48 @@ dg4_status weight_maps(Maps* m, const void* wg, const void* wu, const void* wd, 
     return DG4_OK;
 }
 
-// CTAs of a kernel that works in pairs; n_tiles counts pairs of tiles
-int pair_grid(const Params& p, int sms) { return 2 * (p.n_tiles < sms / 2 ? p.n_tiles : sms / 2); }
+// Pairs of CTAs that share a tile's blocks, for a kernel that works in pairs on tiles of 256 rows: two from `least` blocks on,
+// four from twice as many, where the device holds that many at once on `sms` SMs.  A block costs one pair 0.58 us forward and
+// 0.83 for dX; joining two pairs' sums costs 3.2 us, four pairs' 6.5 (most of it the launch of the larger cluster).  One row by
+// one, two and four pairs, us: forward 9.2, 10.1, 11.4 for 8 blocks, 13.7, 12.5, 12.9 for 16, 22.9, 17.1, 15.2 for 32, 41.3, 26.4,
+// 19.8 for 64; dX 11.0, 11.4, 12.0, then 17.6, 15.0, 14.2, then 31.0, 21.6, 17.5, then 57.7, 35.0, 24.2.
+constexpr int kSplitFwd = 12, kSplitDx = 8;
+template <auto kKernel>
+dg4_status splits_of(int tiles, int n_blocks, int least, int smem, int sms, int* out) {
+    *out = 1;
+    for (int s = 4; s > 1; s /= 2) {
+        int clusters;
+        if (n_blocks < least * (s / 2) || (int64_t)tiles * 2 * s > sms) continue;
+        CHECK(dg4i_resident_clusters<kKernel>(2 * s, kThreads, smem, &clusters));
+        if (tiles <= clusters) {
+            *out = s;
+            break;
+        }
+    }
+    return DG4_OK;
+}
+// `p` with n_tiles counting tiles of 256 rows
+template <auto kKernel, class... Args>
+dg4_status launch_pairs(Params p, int least, int smem, int sms, int free_sms, cudaStream_t st, const Args&... maps) {
+    p.n_tiles = (p.n_tiles + 1) / 2;
+    CHECK(splits_of<kKernel>(p.n_tiles, p.n_blocks, least, smem, free_sms, &p.splits));
+    const int pairs = p.splits > 1 || p.n_tiles < sms / 2 ? p.n_tiles : sms / 2;
+    return dg4i_launch_clusters(kKernel, dim3(2 * p.splits * pairs), 2 * p.splits, kThreads, smem, st, true, maps..., p);
+}
 
 template <int ACT>
 dg4_status launch_fwd(const Maps& m, const Params& p, int dev, int sms, cudaStream_t st) {
     CHECK(allow_smem<glu_fwd_kernel<ACT>>(dev, fwd::kSmem));
-    CHECK(dg4i_launch(glu_fwd_kernel<ACT>, dim3(pair_grid(p, sms)), kThreads, fwd::kSmem, st, true, m.x, m.wg, m.wu, m.wd, m.r, m.y, p));
-    return DG4_OK;
+    return launch_pairs<glu_fwd_kernel<ACT>>(p, kSplitFwd, fwd::kSmem, sms, sms, st, m.x, m.wg, m.wu, m.wd, m.r, m.y);
 }
 
 template <int ACT>
 dg4_status launch_bwd(const Maps& m, const Params& p, const DwOut& out, int groups, int dev, int sms, cudaStream_t st) {
     if (p.out) {
         CHECK(allow_smem<glu_dx_kernel<ACT>>(dev, dx::kSmem));
-        Params q = p;
-        q.n_tiles = (p.n_tiles + 1) / 2;
-        CHECK(dg4i_launch(glu_dx_kernel<ACT>, dim3(pair_grid(q, sms)), kThreads, dx::kSmem, st, true, m.x, m.dy, m.wg, m.wu, m.wd_half, q));
+        // what the weights' kernel leaves, which begins beside this one
+        const int free_sms = out.wg ? sms - p.n_blocks * groups : sms;
+        CHECK(launch_pairs<glu_dx_kernel<ACT>>(p, kSplitDx, dx::kSmem, sms, free_sms, st, m.x, m.dy, m.wg, m.wu, m.wd_half));
     }
     if (out.wg) {
         CHECK(allow_smem<glu_dw_kernel<ACT>>(dev, dw::kSmem));
@@ -1151,8 +1280,8 @@ extern "C" dg4_status dg4_glu_fwd(const dg4_graph* g, const dg4_desc* desc, cons
     CHECK(dg4i_make_row_map(&m.x, X, g->n, ldx, kTileM));
     CHECK(dg4i_make_row_map(&m.y, Y, g->n, ldy, 32));
     Params p = make_params(g, d_ff);
-    p.n_tiles = (p.n_tiles + 1) / 2;
-    p.has_res = res;
+    p.R = res ? (const __nv_bfloat16*)H_res : nullptr; p.ldr = ldh;
+    p.out = (__nv_bfloat16*)Y; p.ldo = ldy;
     m.r = m.x;
     if (res) CHECK(dg4i_make_row_map(&m.r, H_res, g->n, ldh, kTileM));
     const cudaStream_t st = (cudaStream_t)stream;

@@ -246,8 +246,9 @@ __device__ __forceinline__ void mma_commit_by(uint32_t elected, uint32_t bar) {
         ::"r"(bar), "r"(elected) : "memory");
 }
 // ---- pairs of CTAs (cta_group::2) ----------------------------------------------------------------
-// Two CTAs of a cluster multiply together: each holds its own 128 rows of A and of D (256 rows in all) and one half of B's
-// rows, which both tensor cores read.  The CTA of rank 0 issues; a commit arrives on the barrier of both.
+// Two CTAs of a cluster (ranks 2i and 2i + 1) multiply together: each holds its own 128 rows of A and of D (256 rows in all)
+// and one half of B's rows, which both tensor cores read.  The CTA of the even rank issues; a commit arrives on the barrier of
+// both.
 __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -285,9 +286,10 @@ __device__ __forceinline__ void mma_pair_ta(uint32_t d_tmem, uint32_t a_tmem, ui
 }
 __device__ __forceinline__ uint32_t desc_low(uint64_t desc) { return (uint32_t)desc; }
 __device__ __forceinline__ uint32_t desc_high(uint64_t desc) { return (uint32_t)(desc >> 32); }
-__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
+// `mask`: the pair's ranks in the cluster
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar, uint32_t mask) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((unsigned short)3) : "memory");
+                 ::"r"(bar), "h"((unsigned short)mask) : "memory");
 }
 // A value that all lanes hold alike, told to the compiler.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }

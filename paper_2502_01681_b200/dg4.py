@@ -563,11 +563,11 @@ def _opt(t):
 def _glu_weights(W_gate, W_up, W_down):
     """Pointers of a gated sub-layer's weights (or of their gradients), and d_ff."""
     d_ff = W_gate.shape[0]
-    if tuple(W_gate.shape) != (d_ff, 128) or tuple(W_up.shape) != (d_ff, 128) or tuple(W_down.shape) != (128, d_ff):
+    if W_gate.shape != (d_ff, 128) or W_up.shape != (d_ff, 128) or W_down.shape != (128, d_ff):
         raise ValueError("a gated sub-layer's weights are [d_ff, 128], [d_ff, 128] and [128, d_ff]")
-    bf16 = _torch().bfloat16
+    bf16 = (_torch_module or _torch()).bfloat16
     for t in (W_gate, W_up, W_down):
-        if t.dtype != bf16 or not t.is_contiguous() or not t.is_cuda:
+        if t.dtype is not bf16 or not t.is_contiguous() or not t.is_cuda:
             raise ValueError("a gated sub-layer's weights and their gradients are contiguous CUDA bf16 tensors")
     return W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), d_ff
 

@@ -99,7 +99,8 @@ def glu_ref(x, wg, wu, wd, kind, res=None):
 
 SHAPES = [  # rows, d_ff: one row, one block, ragged rows and blocks, several tiles and one, two, three blocks to a pair of CTAs
     (1, 8), (1, 512), (2, 64), (127, 64), (128, 72), (129, 200), (255, 128), (256, 344), (257, 520), (2051, 512), (2000, 1032),
-    (19000, 64), (38001, 64), (57001, 128), (57001, 192), (60001, 40), (40001, 320), (700, 8192)]
+    (19000, 64), (38001, 64), (57001, 128), (57001, 192), (60001, 40), (40001, 320), (700, 8192),
+    (1, 2048), (1, 768), (300, 776), (513, 1544), (256, 2056), (3000, 896), (900, 4096)]       # few rows: pairs share a tile's blocks
 
 
 @pytest.mark.parametrize("kind", ["silu", "gelu", "relu"])
@@ -221,6 +222,28 @@ def test_glu_in_place():
         args = (over, dy) if torch.equal(over, x) else (x, over)
         dg4.dg4_glu_bwd(g, d, args[0], wg, wu, wd, ACT["gelu"], args[1], over, None, None, None)
         assert torch.equal(over, out[0])
+
+
+def test_glu_few_rows_in_place_and_with_wide_strides():
+    for n, d_ff in ((5, 2048), (700, 1000)):                             # four pairs to a tile, and two
+        x, wg, wu, wd = glu_case(35, n, d_ff)
+        res, dy = normal(36, (n, 128)), normal(37, (n, 128))
+        g, d = edgeless(n), desc(residual=True)
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        dg4.dg4_glu_fwd(g, d, x, wg, wu, wd, ACT["silu"], res, y)
+        dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["silu"], dy, dx, None, None, None)
+        xs, rs, dys, out = strided(x, 200, 8), strided(res, 136, 16), strided(dy, 144, 8), strided(x, 1000, 24)
+        dg4.dg4_glu_fwd(g, d, xs, wg, wu, wd, ACT["silu"], rs, out)
+        assert torch.equal(out, y)
+        assert n == 1 or bool(torch.isnan(out.as_strided((n - 1, 24), (1000, 1), out.storage_offset() + 128)).all())
+        dg4.dg4_glu_fwd(g, d, xs, wg, wu, wd, ACT["silu"], rs, rs)
+        assert torch.equal(rs, y)
+        dg4.dg4_glu_bwd(g, d, xs, wg, wu, wd, ACT["silu"], dys, out, None, None, None)
+        assert torch.equal(out, dx)
+        dg4.dg4_glu_bwd(g, d, xs, wg, wu, wd, ACT["silu"], dys, dys, None, None, None)
+        assert torch.equal(dys, dx)
+        dg4.dg4_glu_fwd(g, d, xs, wg, wu, wd, ACT["silu"], res, xs)
+        assert torch.equal(xs, y)
 
 
 def test_glu_parts_of_the_gradients_are_the_same_bits_every_time():
@@ -589,7 +612,7 @@ def test_calls_one_after_the_other_see_one_another():
         assert all(torch.equal(p, q) for p, q in zip(got, want))
 
 
-@pytest.mark.parametrize("n,d_ff", [(1, 8), (700, 200), (40001, 512)])
+@pytest.mark.parametrize("n,d_ff", [(1, 8), (700, 200), (40001, 512), (10, 2048), (600, 800)])
 def test_waits_that_run_out_are_reported_and_leave_the_calls_usable(n, d_ff):
     s = SubLayer(n, d_ff, 140)
     s.step()
