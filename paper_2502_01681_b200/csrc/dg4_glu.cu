@@ -37,7 +37,7 @@ constexpr int kCtrlWarps = 4;                      // warp 0, 2, 3: loads, warp 
 constexpr int kThreads = (kCtrlWarps + kEpiWarps) * 32;
 constexpr int kSetWarps = kEpiWarps / 2;           // forward and dX: half of the epilogue warps take every other block
 constexpr int kSmemLimit = 232448;                 // what one CTA may hold
-constexpr int kMaxDff = 8192;                      // at most as many blocks as SMs (glu_dw_kernel)
+constexpr int kMaxDff = 8192;                      // 128 blocks: glu_dw_kernel has a CTA for each at least
 
 // A place in a ring of n and the parity of its present round.
 struct Turn {
@@ -501,15 +501,21 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
             if (has_res ? !await(bars, bar(bars->r_full[t & 1]), (uint32_t)(t >> 1) & 1u, limit)
                           : t > 0 && !await(bars, bar(bars->r_empty[(t - 1) & 1]), (uint32_t)((t - 1) >> 1) & 1u, limit)) return false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                uint32_t o[4], r[4] = {0u, 0u, 0u, 0u};
-                const uint32_t at = stage + sw128_offset(lane, i);
-                if (has_res) ld_shared_v4(at, r);
+            for (int c = 0; c < 2; ++c) {
+                uint32_t r[16] = {};
+                if (has_res) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    o[e] = pack_bf16(__uint_as_float(y[8 * i + 2 * e]) + __uint_as_float(r[e] << 16),
-                                     __uint_as_float(y[8 * i + 2 * e + 1]) + __uint_as_float(r[e] & 0xffff0000u));
-                st_shared_v4(at, o);
+                    for (int i = 0; i < 4; ++i) ld_shared_v4(stage + sw128_offset(lane, c * 4 + i), r + 4 * i);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[e] = pack_bf16(__uint_as_float(y[c * 32 + 8 * i + 2 * e]) + __uint_as_float(r[4 * i + e] << 16),
+                                         __uint_as_float(y[c * 32 + 8 * i + 2 * e + 1]) + __uint_as_float(r[4 * i + e] & 0xffff0000u));
+                    st_shared_v4(stage + sw128_offset(lane, c * 4 + i), o);
+                }
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -536,20 +542,21 @@ glu_fwd_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant_
                 ok = await(bars, bar(bars->acc_full[buf.at]), buf.odd, limit);
                 if (!ok) break;
                 tc_fence_after();
+                const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * 128 + part * 32);
+                uint32_t g[32], u[32];
+                tmem_ld_32x32(at, g);
+                tmem_ld_32x32(at + 64, u);
+                tmem_ld_wait();
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const uint32_t at = tmem + lanes + (uint32_t)(128 + buf.at * 128 + part * 32 + c * kEl);
-                    uint32_t g[kEl], u[kEl], a[kEl / 2];
-                    tmem_ld_32x16(at, g);
-                    tmem_ld_32x16(at + 64, u);
-                    tmem_ld_wait();
-                    gated<ACT>(g, u, a);
+                    uint32_t a[kEl / 2];
+                    gated<ACT>(g + c * kEl, u + c * kEl, a);
                     const int valid = p.d_ff - unit_of(b) - part * 32 - c * kEl;   // hidden units past the last: zero
                     if (valid < kEl) {
 #pragma unroll
                         for (int i = 0; i < kEl / 2; ++i) if (2 * i >= valid) a[i] = 0u;
                     }
-                    tmem_st_32x8(at, a);
+                    tmem_st_32x8(at + c * kEl, a);
                 }
                 tmem_st_wait();
                 tc_fence_before();
@@ -983,8 +990,7 @@ glu_dw_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 mbar_expect_tx(bar(full[x.at]), kTileBytes);
                 load_tile(map, base + kOffX + (2 * x.at + (dy ? 1 : 0)) * kTileBytes, row0, bar(full[x.at]));
                 // the rows of two tiles on into L2: every block's CTA of the group wants them, one asks
-                const int next = row0 + 2 * groups * kTileM;
-                if (next < p.n && t % (int)gridDim.x == block) prefetch_tile(map, next);
+                if (t + 2 < tiles && t % (int)gridDim.x == block) prefetch_tile(map, row0 + 2 * groups * kTileM);
             }
             if (!dy) mbar_wait(bar(bars->w_full), 0);
             for (int i = max(0, t - kStages); i < t; ++i) mbar_wait(bar(full[i % kStages]), (uint32_t)(i / kStages) & 1u);
@@ -1320,8 +1326,12 @@ extern "C" dg4_status dg4_glu_bwd(const dg4_graph* g, const dg4_desc* desc, cons
         CHECK(dg4i_check_tensor("dW_gate", dW_gate, 128, 2, 128));
         CHECK(dg4i_check_tensor("dW_up", dW_up, 128, 2, 128));
         CHECK(dg4i_check_tensor("dW_down", dW_down, d_ff, 2, d_ff));
-        // dX's kernel is done with X and dY before the weights' kernel reads them again
+        // the kernels of dX and of the weights run side by side, and each reads everything
         if (dX && (dX == X || dX == dY)) DG4_FAIL(DG4_ERR_INVALID_ARG, "dX must not be X or dY when the weights' gradients are asked for");
+        const void *in[3] = {W_gate, W_up, W_down}, *made[3] = {dW_gate, dW_up, dW_down};
+        for (int i = 0; i < 3; ++i)
+            for (int j = 0; j < 3; ++j)
+                if (made[i] == in[j] || (i < j && made[i] == made[j])) DG4_FAIL(DG4_ERR_INVALID_ARG, "a weight's gradient lies over a weight or another gradient");
         const size_t need = dg4_glu_bwd_workspace_bytes(g, desc, d_ff);
         if (need && (!workspace || workspace_bytes < need))
             DG4_FAIL(DG4_ERR_INVALID_ARG, "workspace too small: %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);

@@ -669,6 +669,9 @@ def test_refusals():
         (INV, lambda: dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, silu, y, x, *grads[1:], ws)),
         (INV, lambda: dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, silu, y, y, *grads[1:], ws)),
         (UNS, lambda: dg4.dg4_glu_bwd(g, f32, x, wg, wu, wd, silu, y, *grads, ws)),
+        (INV, lambda: dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, silu, y, grads[0], wg, *grads[2:], ws)),
+        (INV, lambda: dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, silu, y, grads[0], grads[1], grads[1], grads[3], ws)),
+        (INV, lambda: dg4.dg4_glu_fwd(g, d, x, wg, wu, wd, silu, None, x.as_strided((n // 2, 128), (256, 1)))),
         (INV, lambda: dg4.dg4_add_norm_fwd(g, d, x, None, vec, None, -1.0, None, y)),
         (INV, lambda: dg4.dg4_add_norm_fwd(g, d, x, None, vec, None, nan, None, y)),
         (INV, lambda: dg4.dg4_add_norm_fwd(g, d, x, None, None, None, EPS, None, y)),
