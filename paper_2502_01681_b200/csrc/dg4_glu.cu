@@ -77,6 +77,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return pk;
 }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float relu(float x) { float y; asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // SiLU x * sigmoid(x), GELU by its tanh form x * sigmoid(2 sqrt(2/pi) (x + 0.044715 x^3)), ReLU max(0, x).
@@ -125,7 +126,7 @@ __device__ __forceinline__ void gated(const uint32_t* g_bits, const uint32_t* u_
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             Pair x = pair(g[i], g[i + 1]);
-            if (ACT == DG4_ACT_RELU) x = pair(fmaxf(g[i], 0.f), fmaxf(g[i + 1], 0.f));
+            if (ACT == DG4_ACT_RELU) x = pair(relu(g[i]), relu(g[i + 1]));
             else x = mul2(x, pair(s[i], s[i + 1]));
             float lo, hi;
             split(mul2(x, pair(u[i], u[i + 1])), lo, hi);
@@ -149,7 +150,7 @@ __device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t
             const Pair uu = pair(u[i], u[i + 1]), hh = pair(h[i], h[i + 1]);
             Pair act, slope;
             if (ACT == DG4_ACT_RELU) {
-                act = pair(fmaxf(g[i], 0.f), fmaxf(g[i + 1], 0.f));
+                act = pair(relu(g[i]), relu(g[i + 1]));
                 slope = pair(g[i] > 0.f ? 1.f : 0.f, g[i + 1] > 0.f ? 1.f : 0.f);
             } else {
                 const Pair x = pair(g[i], g[i + 1]), ss = pair(s[i], s[i + 1]);

@@ -342,6 +342,22 @@ def test_glu_values_stay_in_their_rows_and_units():
     assert bool(torch.isfinite(outp[2]).all()) and float((outp[2][:, 7].double() - du[0]).abs().max()) <= 2.0 ** -6 * float(du.abs().max())
 
 
+@pytest.mark.parametrize("kind", ["silu", "gelu", "relu"])
+def test_glu_gates_that_are_not_numbers_are_not_lost(kind):
+    n, d_ff = 40, 96
+    x, wg, wu, wd = glu_case(55, n, d_ff)
+    dy = normal(56, (n, 128))
+    g, d = edgeless(n), desc()
+    for unit in (0, 41, 95):
+        wgp = wg.clone()
+        wgp[unit, 5] = math.nan                                          # one gate of every row
+        y, out = torch.empty_like(x), glu_grads(x, wg, wu, wd)
+        dg4.dg4_glu_fwd(g, d, x, wgp, wu, wd, ACT[kind], None, y)
+        assert bool(torch.isnan(y).all())
+        dg4.dg4_glu_bwd(g, d, x, wgp, wu, wd, ACT[kind], dy, *out, workspace(dg4.dg4_glu_bwd_workspace_bytes(g, d, d_ff)))
+        assert bool(torch.isnan(out[2][unit]).all()) and bool(torch.isnan(out[3][:, unit]).all()) and bool(torch.isnan(out[0]).all())
+
+
 def test_glu_offsets_past_32_bits():
     n, ld = 20000, 131072                                                # 5.2 GB from the first row to the last
     x, wg, wu, wd = glu_case(61, n, 64)
