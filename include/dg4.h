@@ -552,7 +552,9 @@ typedef enum {
  *   workspace                 device, dg4_glu_bwd_workspace_bytes() bytes (0 for few rows: NULL then), 16-byte aligned;
  *                             only the weights' gradients need it
  * The activations are computed again from X.  The hidden gradients are rounded to bf16 between the products; the weights'
- * gradients are sums over all rows in fp32, rounded once.
+ * gradients are sums over all rows in fp32, rounded once.  The tensor cores' part of a sum, 131 072 rows at the most, cuts off
+ * where fp32 additions round (up to 1e-3 of a sum of one sign, a quarter of bf16's half step); beyond that many rows the
+ * workspace grows with them: 192 * 128 fp32 values per 64 hidden units and part.
  * Errors: INVALID_ARG, UNSUPPORTED (dtype other than bf16; d_ff; activation), CUDA; a device-side wait that runs out
  * records DG4_ERR_TIMEOUT in the handle's status word.
  */

@@ -1,0 +1,37 @@
+"""GPU tests of the training calls at their edges; the expected values and tolerances are built as in test_gpu_training.py."""
+import math
+
+import pytest
+import torch
+
+from paper_2502_01681_b200 import dg4
+from test_gpu_training import ACT, act64, desc, edgeless, normal, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+def test_sums_over_many_rows_do_not_drift():
+    """Products of one sign: what the tensor cores' accumulators cut off adds up.  They take 16 rows to an addition, each worth a
+    unit of the last place (2^-23 of the sum) at the most in the mean; 131 072 rows are 8 192 additions, and beyond that their
+    number does not grow.  The rounding to bf16 is even to both sides: over 8 192 elements its mean stays below
+    4 * 2^-8 / sqrt(3 * 8192) = 1e-4."""
+    n, d_ff, some = 2000003, 4808, 64                                    # one sum over all rows where their number sets no bound
+    x, dy = normal(1, (n, 128)).abs_(), normal(2, (n, 128)).abs_()
+    wg, wu = normal(3, (d_ff, 128), 0.02).abs_(), normal(4, (d_ff, 128), 0.02).abs_()
+    wd = normal(5, (128, d_ff), 0.02).abs_()
+    g, d = edgeless(n), desc()
+    out = [torch.full_like(t, math.nan) for t in (wg, wu, wd)]
+    ws = workspace(dg4.dg4_glu_bwd_workspace_bytes(g, d, d_ff))
+    dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["silu"], dy, None, *out, ws)
+    want = [torch.zeros((some, 128), dtype=torch.float64, device="cuda") for _ in range(3)]
+    w = [t.double() for t in (wg[-some:], wu[-some:], wd[:, -some:])]
+    for xs, dys in zip(x.split(100000), dy.split(100000)):
+        xs, dys = xs.double(), dys.double()
+        a, da, _ = act64(xs @ w[0].T, "silu")
+        u, h = xs @ w[1].T, dys @ w[2]
+        for to, t, other in zip(want, (h * u * da, h * a, a * u), (xs, xs, dys)):
+            to += t.T @ other
+    for name, got, ref in zip(("dW_gate", "dW_up", "dW_down"), (out[0][-some:], out[1][-some:], out[2][:, -some:].T), want):
+        off = (got.double() - ref) / ref
+        assert abs(float(off.mean())) <= 8192 * 2.0 ** -23 + 1e-4, name
+        assert float(off.abs().max()) <= 2.0 ** -8 + 8192 * 2.0 ** -23 + 1e-4, name
