@@ -554,7 +554,8 @@ typedef enum {
  * The activations are computed again from X.  The hidden gradients are rounded to bf16 between the products; the weights'
  * gradients are sums over all rows in fp32, rounded once.  The tensor cores' part of a sum, 131 072 rows at the most, cuts off
  * where fp32 additions round (up to 1e-3 of a sum of one sign, a quarter of bf16's half step); beyond that many rows the
- * workspace grows with them: 192 * 128 fp32 values per 64 hidden units and part.
+ * workspace grows with them: 192 * 128 fp32 values per 64 hidden units and part.  Neither dX nor the weights' gradients
+ * depend on whether the others are asked for.
  * Errors: INVALID_ARG, UNSUPPORTED (dtype other than bf16; d_ff; activation), CUDA; a device-side wait that runs out
  * records DG4_ERR_TIMEOUT in the handle's status word.
  */

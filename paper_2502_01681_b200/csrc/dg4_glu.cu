@@ -1261,8 +1261,12 @@ template <int ACT>
 dg4_status launch_bwd(const Maps& m, const Params& p, const DwOut& out, int groups, int dev, int sms, cudaStream_t st) {
     if (p.out) {
         CHECK(allow_smem<glu_dx_kernel<ACT>>(dev, dx::kSmem));
-        // what the weights' kernel leaves, which begins beside this one
-        const int free_sms = out.wg ? sms - p.n_blocks * groups : sms;
+        // The weights' kernel begins beside this one: where a pair to each tile fits on what it leaves, the tiles' blocks are
+        // shared among no more pairs than fit there, and elsewhere it has to wait for SMs anyway.  Whether the weights'
+        // gradients are asked for does not enter, or dX would be summed in another order without them.  Gradients of all
+        // (and dX alone), us: (2000 rows, d_ff 512) 17.9 (12.6), where shared blocks would take 21.2 (11.9); (1500, 1024)
+        // 25.9 (14.6), without shared blocks 30.3 (19.3).
+        const int left = sms - p.n_blocks * groups, free_sms = (p.n_tiles + 1) / 2 * 2 <= left ? left : sms;
         CHECK(launch_pairs<glu_dx_kernel<ACT>>(p, kSplitDx, dx::kSmem, sms, free_sms, st, m.x, m.dy, m.wg, m.wu, m.wd_half));
     }
     if (out.wg) {

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2502_01681_b200 import dg4
-from test_gpu_training import ACT, act64, desc, edgeless, normal, workspace
+from test_gpu_training import ACT, act64, desc, edgeless, glu_case, glu_grads, normal, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +35,14 @@ def test_sums_over_many_rows_do_not_drift():
         off = (got.double() - ref) / ref
         assert abs(float(off.mean())) <= 8192 * 2.0 ** -23 + 1e-4, name
         assert float(off.abs().max()) <= 2.0 ** -8 + 8192 * 2.0 ** -23 + 1e-4, name
+
+
+@pytest.mark.parametrize("n,d_ff", [(1500, 1024), (700, 768), (1100, 1544), (2000, 520), (400, 2048), (300, 4096)])
+def test_dx_has_the_same_bits_with_and_without_the_weights_gradients(n, d_ff):
+    x, wg, wu, wd = glu_case(n, n, d_ff)
+    dy = normal(n + 9, (n, 128))
+    g, d = edgeless(n), desc()
+    out, alone = glu_grads(x, wg, wu, wd), torch.full_like(x, math.nan)
+    dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["silu"], dy, *out, workspace(dg4.dg4_glu_bwd_workspace_bytes(g, d, d_ff)))
+    dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["silu"], dy, alone, None, None, None)
+    assert torch.equal(out[0], alone)
