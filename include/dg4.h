@@ -533,7 +533,7 @@ dg4_status dg4_norm_gate_fwd(const dg4_graph* g, const dg4_desc* desc, const voi
 typedef enum {
     DG4_ACT_SILU = 0,          /* x / (1 + exp(-x))                                                           */
     DG4_ACT_GELU = 1,          /* x / 2 * (1 + tanh(sqrt(2 / pi) * (x + 0.044715 x^3)))                        */
-    DG4_ACT_RELU = 2           /* max(0, x); derivative 0 at 0                                                 */
+    DG4_ACT_RELU = 2           /* max(0, x); no gradient to a gate at or below 0, whatever U and dY hold       */
 } dg4_activation;
 
 /*

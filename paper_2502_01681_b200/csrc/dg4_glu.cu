@@ -135,7 +135,8 @@ __device__ __forceinline__ void gated(const uint32_t* g_bits, const uint32_t* u_
     }
 }
 // The same backward, for h = dL/d(act(g) u):  dg = h u act'(g),  du = h act(g),  a = act(g) u (not asked for: null), with
-// act'(g) = s + g s (1 - s) p'(g), s = sigmoid(p(g)).
+// act'(g) = s + g s (1 - s) p'(g), s = sigmoid(p(g)).  ReLU's dg is taken and not multiplied: zero behind a closed gate
+// whatever h and u are, and not a number where the gate is none.
 template <int ACT, bool VALUES>
 __device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t* u_bits, const uint32_t* h_bits, uint32_t* dg,
                                           uint32_t* du, uint32_t* a) {
@@ -151,7 +152,6 @@ __device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t
             Pair act, slope;
             if (ACT == DG4_ACT_RELU) {
                 act = pair(relu(g[i]), relu(g[i + 1]));
-                slope = pair(g[i] > 0.f ? 1.f : 0.f, g[i + 1] > 0.f ? 1.f : 0.f);
             } else {
                 const Pair x = pair(g[i], g[i + 1]), ss = pair(s[i], s[i + 1]);
                 act = mul2(x, ss);
@@ -169,7 +169,13 @@ __device__ __forceinline__ void gated_bwd(const uint32_t* g_bits, const uint32_t
             float lo, hi;
             split(mul2(hh, act), lo, hi);
             du[4 * c + i / 2] = pack_bf16(lo, hi);
-            split(mul2(mul2(hh, uu), slope), lo, hi);
+            if (ACT == DG4_ACT_RELU) {
+                split(mul2(hh, uu), lo, hi);
+                lo = g[i] > 0.f ? lo : relu(g[i]);
+                hi = g[i + 1] > 0.f ? hi : relu(g[i + 1]);
+            } else {
+                split(mul2(mul2(hh, uu), slope), lo, hi);
+            }
             dg[4 * c + i / 2] = pack_bf16(lo, hi);
             if (VALUES) {
                 split(mul2(act, uu), lo, hi);

@@ -46,3 +46,31 @@ def test_dx_has_the_same_bits_with_and_without_the_weights_gradients(n, d_ff):
     dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["silu"], dy, *out, workspace(dg4.dg4_glu_bwd_workspace_bytes(g, d, d_ff)))
     dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["silu"], dy, alone, None, None, None)
     assert torch.equal(out[0], alone)
+
+
+def test_relu_gates_that_are_closed_or_not_numbers_backward():
+    n, d_ff, unit = 40, 96, 41
+    x, wg, wu, wd = glu_case(201, n, d_ff)
+    dy = normal(202, (n, 128))
+    g, d = edgeless(n), desc()
+    ws = workspace(dg4.dg4_glu_bwd_workspace_bytes(g, d, d_ff))
+    wgp = wg.clone()
+    wgp[unit, 5] = math.nan                                              # one gate of every row: its gradients are not numbers
+    out = glu_grads(x, wg, wu, wd)
+    dg4.dg4_glu_bwd(g, d, x, wgp, wu, wd, ACT["relu"], dy, *out, ws)
+    assert bool(torch.isnan(out[1][unit]).all()) and bool(torch.isnan(out[2][unit]).all()) and bool(torch.isnan(out[3][:, unit]).all())
+    keep = torch.arange(d_ff, device="cuda") != unit
+    assert bool(torch.isfinite(out[1][keep]).all()) and bool(torch.isfinite(out[2][keep]).all())
+    # an infinite U behind a closed gate: the gate's gradient is zero (0 * inf stays in act(G) U and so in W_down's gradient)
+    xc = x.clone()
+    xc[:, 5], xc[:, 6] = 1.0, 1.0
+    wgc, wuc = wg.clone(), wu.clone()
+    wgc[unit, 5], wuc[unit, 6] = -1000.0, math.inf
+    out, ref = glu_grads(x, wg, wu, wd), glu_grads(x, wg, wu, wd)
+    dg4.dg4_glu_bwd(g, d, xc, wgc, wuc, wd, ACT["relu"], dy, *out, ws)
+    assert not bool(out[1][unit].any()) and not bool(out[2][unit].any())
+    wuc[unit, 6] = 0.0
+    dg4.dg4_glu_bwd(g, d, xc, wgc, wuc, wd, ACT["relu"], dy, *ref, ws)
+    assert torch.equal(out[1], ref[1]) and torch.equal(out[2][keep], ref[2][keep]) and torch.equal(out[3][:, keep], ref[3][:, keep])
+    # dX: that unit's U row is infinite, and its factor dU = dA * 0 meets it in the last product
+    assert torch.equal(out[0][:, torch.arange(128, device="cuda") != 6], ref[0][:, torch.arange(128, device="cuda") != 6])
