@@ -77,6 +77,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return pk;
 }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float ex2_small(float x) { float y; asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }   // below 2^-126 too
+__device__ __forceinline__ float min_or_nan(float x, float y) { float z; asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y)); return z; }
 __device__ __forceinline__ float relu(float x) { float y; asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
@@ -85,7 +87,8 @@ constexpr float kLog2e = 1.4426950408889634f, kGelu1 = 1.5957691216057308f, kGel
 // sigmoid(p(g)) of eight values.  The special-function unit is what would bound the epilogues (an exponential and a reciprocal
 // per value: 1024 clocks per block and SM, the products of the forward pass 768), so four values share a reciprocal:
 // 1/x = y / (xy).  Where the product of the four is too large for that (2^126; four gates near -22, or one below -87), and for
-// NaN, which would reach the other values, each has its own.
+// NaN, which would reach the other values, each has its own, from t = exp(p): t / (1 + t) keeps subnormal values, which a gate of
+// -90 makes normal numbers of again.
 template <int ACT>
 __device__ __forceinline__ void sigmoid8(const float* g, float* s) {
     float e[8];
@@ -112,7 +115,10 @@ __device__ __forceinline__ void sigmoid8(const float* g, float* s) {
     }
     if (each) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = rcp(1.f + ex2(e[i]));
+        for (int i = 0; i < 8; ++i) {
+            const float t = ex2_small(min_or_nan(-e[i], 126.f));
+            s[i] = t * rcp(1.f + t);
+        }
     }
 }
 // Sixteen values act(g) * u as eight pairs of bf16.

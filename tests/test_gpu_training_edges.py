@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2502_01681_b200 import dg4
-from test_gpu_training import ACT, act64, desc, edgeless, glu_case, glu_grads, normal, workspace
+from test_gpu_training import ACT, BF16, act64, desc, edgeless, glu_case, glu_grads, normal, within, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,33 @@ def test_relu_gates_that_are_closed_or_not_numbers_backward():
     assert torch.equal(out[1], ref[1]) and torch.equal(out[2][keep], ref[2][keep]) and torch.equal(out[3][:, keep], ref[3][:, keep])
     # dX: that unit's U row is infinite, and its factor dU = dA * 0 meets it in the last product
     assert torch.equal(out[0][:, torch.arange(128, device="cuda") != 6], ref[0][:, torch.arange(128, device="cuda") != 6])
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_gates_far_out_keep_what_bf16_can_hold(kind):
+    """act(g) is a normal number some way past the gates whose sigmoid is below 2^-126."""
+    values = [-80.0, -86.0, -87.5, -88.0, -88.5, -89.0, -90.0, -91.0] if kind == "silu" else [-9.5, -9.75, -9.9375, -10.0, -10.0625, -10.125, -10.5]
+    n = len(values)
+    x = torch.zeros((n, 128), dtype=BF16)
+    for k in range(16):                                                  # every value in every place of a group of sixteen
+        x[:, k] = torch.tensor(values).roll(k).to(BF16)
+    x[:, 127] = 1
+    wg, wu, wd = torch.zeros((16, 128)), torch.zeros((16, 128)), torch.zeros((128, 16))
+    for k in range(16):
+        wg[k, k] = wu[k, 127] = wd[k, k] = 1
+    x, wg, wu, wd = x.cuda(), wg.to(BF16).cuda(), wu.to(BF16).cuda(), wd.to(BF16).cuda()
+    y = torch.empty_like(x)
+    dg4.dg4_glu_fwd(edgeless(n), desc(), x, wg, wu, wd, ACT[kind], None, y)
+    g = x[:, :16].double()
+    want = act64(g, kind)[0]
+    # two roundings to bf16; the exponent p(g) is known to 2^-22 of itself, and a sigmoid of 2^-126 >> k to 2^-(23 - k), k < 8
+    c = 2 * math.sqrt(2 / math.pi)
+    size = g.abs() if kind == "silu" else c * (g.abs() + 0.044715 * g.abs() ** 3)
+    part = 2 * 2.0 ** -8 + 2.0 ** -21 * size + 2.0 ** -15
+    within(y[:, :16], want, want.abs() * part + 2.0 ** -126 * 2.0 ** -7, kind)
+    dy, dx = torch.zeros_like(x), torch.empty_like(x)
+    dy[:, :16] = 1
+    dg4.dg4_glu_bwd(edgeless(n), desc(), x, wg, wu, wd, ACT[kind], dy, dx, None, None, None)
+    slope = act64(g, kind)[1]
+    terms = (want / g).abs() + want.abs() * (1 if kind == "silu" else c * (1 + 3 * 0.044715 * g * g))     # s and g s (1 - s) p'
+    within(dx[:, :16], slope, terms * part + 2.0 ** -126 * 2.0 ** -7, kind)
