@@ -232,11 +232,12 @@ def _torch():
     return _torch_module
 
 
-def _stream(stream):
+def _stream(stream, device=None):
+    """The handle of a stream; of the current one (of `device`, or of the current device) if there is none."""
     if stream is None:
         t = _torch_module or _torch()
         try:               # the handle alone, not a public name: 0.4 instead of 3.6 us of a call that takes about 8
-            return t._C._cuda_getCurrentRawStream(t.cuda.current_device())
+            return t._C._cuda_getCurrentRawStream(t.cuda.current_device() if device is None else device)
         except AttributeError:
             return t.cuda.current_stream().cuda_stream
     return int(getattr(stream, "cuda_stream", stream))                      # a raw handle or a torch stream
@@ -487,12 +488,14 @@ def _table(t):
     return _ptr(t), _ld(t)
 
 
-def _vec(t, rows=1):
-    """Pointer of an fp32 vector of 128 (or of `rows` of them), or None."""
+def _vec(t, rows=1, g=None):
+    """Pointer of an fp32 vector of 128 (or of `rows` of them), or None; with a handle: on its GPU."""
     if t is None:
         return None
-    if t.dtype != _torch().float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
+    if t.dtype != (_torch_module or _torch()).float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
         raise ValueError("norm and gate vectors are contiguous CUDA fp32 tensors of 128 elements each")
+    if g is not None and t.get_device() != g.info.device:
+        raise ValueError("norm vectors are on the handle's GPU")
     if rows < 1:
         raise ValueError("a gate tensor has at least one row (None: no gate)")
     return _ptr(t)
@@ -555,31 +558,54 @@ def dg4_norm_gate_fwd(g: Graph, dsc: dg4_desc, S, R, res_scale, gate, seg, post,
                                     _ld(Y) if Y is not None else 0, _stream(stream)))
 
 
-def _opt(t):
-    """Pointer and row distance of a tensor that may be None."""
-    return (_ptr(t), _ld(t)) if t is not None else (None, 0)
+def _row(t, name, shape, dev, dtype):
+    """Pointer and row distance of a call's rows, [n, 128] of one type on the handle's device (a buffer may have more rows; None:
+    a null pointer).  The kernels take them at their word: a shorter or narrower tensor would be read and written past its end."""
+    if t is None:
+        return None, 0
+    if t.dtype is dtype and t.get_device() == dev:
+        if t.shape == shape and t.is_contiguous():                          # mostly; 0.45 us of a call that takes about 8
+            return t.data_ptr(), 128
+        rows, ld = t.shape, t.stride()
+        if len(rows) == 2 and rows[0] >= shape[0] and rows[1] == 128 and ld[1] == 1:
+            return t.data_ptr(), ld[0]
+    raise Dg4Error(DG4_ERR_INVALID_ARG, f"{name} is {list(t.shape)} {t.dtype} on {t.device} with strides {list(t.stride())}, not "
+                                        f"{list(shape)} {dtype} on cuda:{dev} with unit inner stride")
 
 
-def _glu_weights(W_gate, W_up, W_down):
+def _row_type(dsc):
+    t = _torch_module or _torch()
+    return t.bfloat16 if dsc.dtype == DG4_BF16 else t.float32
+
+
+def _glu_weights(g, W_gate, W_up, W_down):
     """Pointers of a gated sub-layer's weights (or of their gradients), and d_ff."""
     d_ff = W_gate.shape[0]
     if W_gate.shape != (d_ff, 128) or W_up.shape != (d_ff, 128) or W_down.shape != (128, d_ff):
         raise ValueError("a gated sub-layer's weights are [d_ff, 128], [d_ff, 128] and [128, d_ff]")
     bf16 = (_torch_module or _torch()).bfloat16
     for t in (W_gate, W_up, W_down):
-        if t.dtype is not bf16 or not t.is_contiguous() or not t.is_cuda:
-            raise ValueError("a gated sub-layer's weights and their gradients are contiguous CUDA bf16 tensors")
+        if t.dtype is not bf16 or not t.is_contiguous() or not t.is_cuda or t.get_device() != g.info.device:
+            raise ValueError("a gated sub-layer's weights and their gradients are contiguous bf16 tensors on the handle's GPU")
     return W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), d_ff
 
 
-def _workspace(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+def _workspace(workspace, dev):
+    if workspace is None:
+        return None, 0
+    size = workspace.numel() * workspace.element_size()
+    if size and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        raise Dg4Error(DG4_ERR_INVALID_ARG, "the workspace is not a contiguous tensor on the handle's device")
+    return workspace.data_ptr(), size
 
 
 def dg4_glu_fwd(g: Graph, dsc: dg4_desc, X, W_gate, W_up, W_down, activation: int, H_res, Y, stream=None):
     """Y = (act(X W_gate^T) * (X W_up^T)) W_down^T, plus H_res if dsc has the residual flag (H_res may be None)."""
-    _check(load().dg4_glu_fwd(g.handle, ctypes.byref(dsc), _ptr(X), _ld(X), *_glu_weights(W_gate, W_up, W_down), activation,
-                              *_opt(H_res), _ptr(Y), _ld(Y), _stream(stream)))
+    weights = _glu_weights(g, W_gate, W_up, W_down)
+    shape, dev, bf16 = (g.info.n_nodes, 128), g.info.device, W_gate.dtype
+    res = _row(H_res, "H_res", shape, dev, bf16) if dsc.flags & DG4_FLAG_RESIDUAL else (None, 0)
+    _check(load().dg4_glu_fwd(g.handle, ctypes.byref(dsc), *_row(X, "X", shape, dev, bf16), *weights, activation, *res,
+                              *_row(Y, "Y", shape, dev, bf16), _stream(stream, dev)))
 
 
 def dg4_glu_bwd_workspace_bytes(g: Graph, dsc: dg4_desc, d_ff: int) -> int:
@@ -589,20 +615,25 @@ def dg4_glu_bwd_workspace_bytes(g: Graph, dsc: dg4_desc, d_ff: int) -> int:
 def dg4_glu_bwd(g: Graph, dsc: dg4_desc, X, W_gate, W_up, W_down, activation: int, dY, dX, dW_gate, dW_up, dW_down,
                 workspace=None, stream=None):
     """The gradients of dg4_glu_fwd's gated sub-layer for dY; dX, or all three weights' gradients, may be None."""
-    weights = _glu_weights(W_gate, W_up, W_down)
+    weights = _glu_weights(g, W_gate, W_up, W_down)
     grads = (None, None, None)
     if dW_gate is not None or dW_up is not None or dW_down is not None:
         if dW_gate is None or dW_up is None or dW_down is None or dW_gate.shape != W_gate.shape:
             raise ValueError("the weights' gradients are given all three, shaped as the weights, or none")
-        grads = _glu_weights(dW_gate, dW_up, dW_down)[:3]
-    _check(load().dg4_glu_bwd(g.handle, ctypes.byref(dsc), _ptr(X), _ld(X), *weights, activation, _ptr(dY), _ld(dY),
-                              *_opt(dX), *grads, *_workspace(workspace), _stream(stream)))
+        grads = _glu_weights(g, dW_gate, dW_up, dW_down)[:3]
+    shape, dev, bf16 = (g.info.n_nodes, 128), g.info.device, W_gate.dtype
+    _check(load().dg4_glu_bwd(g.handle, ctypes.byref(dsc), *_row(X, "X", shape, dev, bf16), *weights, activation,
+                              *_row(dY, "dY", shape, dev, bf16), *_row(dX, "dX", shape, dev, bf16), *grads,
+                              *_workspace(workspace, dev), _stream(stream, dev)))
 
 
 def dg4_add_norm_fwd(g: Graph, dsc: dg4_desc, X, R, gamma, beta, eps, Z, Y, stream=None):
     """Z = X + R, Y = Norm(Z); R, beta and Z may be None."""
-    _check(load().dg4_add_norm_fwd(g.handle, ctypes.byref(dsc), _ptr(X), _ld(X), *_opt(R), _vec(gamma), _vec(beta), eps,
-                                   *_opt(Z), _ptr(Y), _ld(Y), _stream(stream)))
+    vecs = _vec(gamma, 1, g), _vec(beta, 1, g)
+    shape, dev, dtype = (g.info.n_nodes, 128), g.info.device, _row_type(dsc)
+    _check(load().dg4_add_norm_fwd(g.handle, ctypes.byref(dsc), *_row(X, "X", shape, dev, dtype),
+                                   *_row(R, "R", shape, dev, dtype), *vecs, eps, *_row(Z, "Z", shape, dev, dtype),
+                                   *_row(Y, "Y", shape, dev, dtype), _stream(stream, dev)))
 
 
 def dg4_norm_bwd_workspace_bytes(g: Graph, dsc: dg4_desc) -> int:
@@ -611,9 +642,12 @@ def dg4_norm_bwd_workspace_bytes(g: Graph, dsc: dg4_desc) -> int:
 
 def dg4_norm_bwd(g: Graph, dsc: dg4_desc, Z, gamma, eps, dY, D_res, dZ, dgamma, dbeta, workspace=None, stream=None):
     """dZ = D_res + the gradient of Norm at Z for dY, and gamma's and beta's gradients; D_res and each output may be None."""
-    _check(load().dg4_norm_bwd(g.handle, ctypes.byref(dsc), _ptr(Z), _ld(Z), _vec(gamma), eps, _ptr(dY), _ld(dY),
-                               *_opt(D_res), *_opt(dZ), _vec(dgamma), _vec(dbeta), *_workspace(workspace),
-                               _stream(stream)))
+    gamma_, dgamma_, dbeta_ = _vec(gamma, 1, g), _vec(dgamma, 1, g), _vec(dbeta, 1, g)
+    shape, dev, dtype = (g.info.n_nodes, 128), g.info.device, _row_type(dsc)
+    _check(load().dg4_norm_bwd(g.handle, ctypes.byref(dsc), *_row(Z, "Z", shape, dev, dtype), gamma_, eps,
+                               *_row(dY, "dY", shape, dev, dtype), *_row(D_res, "D_res", shape, dev, dtype),
+                               *_row(dZ, "dZ", shape, dev, dtype), dgamma_, dbeta_, *_workspace(workspace, dev),
+                               _stream(stream, dev)))
 
 
 def dg4_debug_set_poll_limit(polls: int):
