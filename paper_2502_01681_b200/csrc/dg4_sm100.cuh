@@ -233,12 +233,6 @@ __device__ __forceinline__ void mma_bf16_by(uint32_t elected, uint32_t d_tmem, u
         "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
 }
-__device__ __forceinline__ void mma_bf16_ta_by(uint32_t elected, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(elected) : "memory");
-}
 __device__ __forceinline__ void mma_commit_by(uint32_t elected, uint32_t bar) {
     asm volatile(
         "{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %1, 0;\n\t"
