@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2502_01681_b200 import dg4
-from test_gpu_training import ACT, BF16, act64, desc, edgeless, glu_case, glu_grads, normal, within, workspace
+from test_gpu_training import ACT, BF16, SubLayer, act64, desc, edgeless, glu_case, glu_grads, normal, within, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -104,3 +104,55 @@ def test_gates_far_out_keep_what_bf16_can_hold(kind):
     slope = act64(g, kind)[1]
     terms = (want / g).abs() + want.abs() * (1 if kind == "silu" else c * (1 + 3 * 0.044715 * g * g))     # s and g s (1 - s) p'
     within(dx[:, :16], slope, terms * part + 2.0 ** -126 * 2.0 ** -7, kind)
+
+
+def test_calls_behind_copies_fills_events_and_joined_streams():
+    """The kernels may begin before what is in front of them on the stream has ended: not before a copy, a fill or another
+    stream's work has."""
+    n, d_ff = 30001, 136
+    s = SubLayer(n, d_ff, 210)
+    h, up = s.h.clone(), s.up.clone()
+    s.step()
+    want = s.results()
+    side, aside = torch.cuda.Stream(), torch.cuda.Stream()
+
+    def spoil():
+        for t in (s.h, s.up, s.norm, s.out, s.dn, s.dh, *s.grads):
+            t.fill_(math.nan)
+
+    def chain():
+        now = torch.cuda.current_stream()
+        spoil()
+        s.h.copy_(h)                                                     # a copy right in front of a call
+        dg4.dg4_add_norm_fwd(s.g, s.d, s.h, None, s.gamma, s.beta, 1e-5, None, s.norm)
+        side.wait_stream(now)
+        aside.wait_stream(now)
+        with torch.cuda.stream(side):                                    # two streams' work is joined in front of the next ones
+            dg4.dg4_glu_fwd(s.g, s.d, s.norm, s.wg, s.wu, s.wd, ACT["silu"], s.h, s.out)
+        with torch.cuda.stream(aside):
+            s.up.fill_(1.0)
+            torch.cuda._sleep(200000)                                    # some 0.1 ms: what comes behind the join has to wait
+            s.up.copy_(up)
+        now.wait_stream(side)
+        now.wait_stream(aside)
+        dg4.dg4_glu_bwd(s.g, s.d, s.norm, s.wg, s.wu, s.wd, ACT["silu"], s.up, s.dn, *s.grads[:3], s.ws)
+        side.wait_stream(now)
+        with torch.cuda.stream(side):                                    # a call behind another stream's weights' kernel
+            dg4.dg4_norm_bwd(s.g, s.d, s.h, s.gamma, 1e-5, s.dn, s.up, s.dh, *s.grads[3:], s.ws2)
+        now.wait_stream(side)
+
+    s.ws2 = workspace(max(dg4.dg4_norm_bwd_workspace_bytes(s.g, s.d), 16))
+    for _ in range(10):
+        chain()
+        got = s.results()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for _ in range(5):
+        spoil()
+        graph.replay()
+        got = s.results()
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+    del graph
