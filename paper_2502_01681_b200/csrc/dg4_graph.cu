@@ -350,18 +350,6 @@ dg4_status dg4i_graph_device_pass(dg4_graph* g, cudaStream_t st, bool sizes_only
 // ------------------------------------------------------------------------------------------------
 namespace {
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard() {
-        if (prev >= 0) cudaSetDevice(prev);
-    }
-};
-
 // Frees the handle.  With `ordered` set, pooled device memory is released in the order of `st` (work enqueued
 // there before may still use it) and nothing waits; otherwise every buffer is released with cudaFree, which
 // waits for the device.

@@ -27,6 +27,19 @@ void dg4_set_error(const char* fmt, ...);
         return (code);               \
     } while (0)
 
+// ---- a device made current for a scope ------------------------------------------------------------
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev) {
+        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
+        ok = cudaSetDevice(dev) == cudaSuccess;
+    }
+    ~DeviceGuard() {
+        if (prev >= 0) cudaSetDevice(prev);
+    }
+};
+
 // ---- argument checks shared by the forward entry points (dg4_layer.cu) -----------------------------
 // INVALID_ARG unless the graph's device is the calling thread's current device: every forward call dereferences
 // the handle's device arrays in its kernels, so a call made with another device current must be refused on the host.

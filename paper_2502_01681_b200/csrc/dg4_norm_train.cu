@@ -264,8 +264,9 @@ extern "C" dg4_status dg4_add_norm_fwd(const dg4_graph* g, const dg4_desc* desc,
 
 extern "C" size_t dg4_norm_bwd_workspace_bytes(const dg4_graph* g, const dg4_desc* desc) {
     int ctas = 0;
-    if (dg4i_check_device(g) != DG4_OK || dg4i_check_desc(desc, false) != DG4_OK ||
-        bwd_ctas(desc->dtype == DG4_BF16, (desc->flags & DG4_FLAG_RMS_NORM) != 0, g->n, &ctas) != DG4_OK) return 0;
+    if (!g || dg4i_check_desc(desc, false) != DG4_OK) return 0;
+    DeviceGuard guard(g->device);                    // the size is the handle's, whichever device is current
+    if (!guard.ok || bwd_ctas(desc->dtype == DG4_BF16, (desc->flags & DG4_FLAG_RMS_NORM) != 0, g->n, &ctas) != DG4_OK) return 0;
     return ctas > 1 ? (size_t)ctas * 256 * sizeof(float) : 0;
 }
 

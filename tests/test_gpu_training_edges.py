@@ -156,3 +156,14 @@ def test_calls_behind_copies_fills_events_and_joined_streams():
         got = s.results()
         assert all(torch.equal(p, q) for p, q in zip(got, want))
     del graph
+
+
+def test_workspace_sizes_are_the_handle_s_whichever_device_is_current():
+    g, d = edgeless(5000), desc()
+    want = dg4.dg4_glu_bwd_workspace_bytes(g, d, 512), dg4.dg4_norm_bwd_workspace_bytes(g, d)
+    assert min(want) > 0
+    dg4.dg4_debug_override_current_device(1)                             # as if another GPU were current on this thread
+    try:
+        assert (dg4.dg4_glu_bwd_workspace_bytes(g, d, 512), dg4.dg4_norm_bwd_workspace_bytes(g, d)) == want
+    finally:
+        dg4.dg4_debug_override_current_device(-1)
