@@ -492,13 +492,14 @@ def _vec(t, rows=1, g=None):
     """Pointer of an fp32 vector of 128 (or of `rows` of them), or None; with a handle: on its GPU."""
     if t is None:
         return None
-    if t.dtype != (_torch_module or _torch()).float32 or not t.is_contiguous() or not t.is_cuda or t.numel() != rows * 128:
+    dev = t.get_device()                                                    # -1: not on a GPU
+    if t.dtype is not (_torch_module or _torch()).float32 or not t.is_contiguous() or dev < 0 or t.numel() != rows * 128:
         raise ValueError("norm and gate vectors are contiguous CUDA fp32 tensors of 128 elements each")
-    if g is not None and t.get_device() != g.info.device:
+    if g is not None and dev != g.info.device:
         raise ValueError("norm vectors are on the handle's GPU")
     if rows < 1:
         raise ValueError("a gate tensor has at least one row (None: no gate)")
-    return _ptr(t)
+    return t.data_ptr()
 
 
 def dg4_qkv_project_adapters(g: Graph, dsc: dg4_desc, X, W_qkv, ad: Adapters, seg, Q, K, V, stream=None):
@@ -585,7 +586,8 @@ def _glu_weights(g, W_gate, W_up, W_down):
         raise ValueError("a gated sub-layer's weights are [d_ff, 128], [d_ff, 128] and [128, d_ff]")
     bf16 = (_torch_module or _torch()).bfloat16
     for t in (W_gate, W_up, W_down):
-        if t.dtype is not bf16 or not t.is_contiguous() or not t.is_cuda or t.get_device() != g.info.device:
+        dev = t.get_device()                                                # -1: not on a GPU
+        if t.dtype is not bf16 or not t.is_contiguous() or dev < 0 or dev != g.info.device:
             raise ValueError("a gated sub-layer's weights and their gradients are contiguous bf16 tensors on the handle's GPU")
     return W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), d_ff
 
@@ -604,7 +606,7 @@ def dg4_glu_fwd(g: Graph, dsc: dg4_desc, X, W_gate, W_up, W_down, activation: in
     weights = _glu_weights(g, W_gate, W_up, W_down)
     shape, dev, bf16 = (g.info.n_nodes, 128), g.info.device, W_gate.dtype
     res = _row(H_res, "H_res", shape, dev, bf16) if dsc.flags & DG4_FLAG_RESIDUAL else (None, 0)
-    _check(load().dg4_glu_fwd(g.handle, ctypes.byref(dsc), *_row(X, "X", shape, dev, bf16), *weights, activation, *res,
+    _check(load().dg4_glu_fwd(g.handle, dsc, *_row(X, "X", shape, dev, bf16), *weights, activation, *res,
                               *_row(Y, "Y", shape, dev, bf16), _stream(stream, dev)))
 
 
@@ -622,7 +624,7 @@ def dg4_glu_bwd(g: Graph, dsc: dg4_desc, X, W_gate, W_up, W_down, activation: in
             raise ValueError("the weights' gradients are given all three, shaped as the weights, or none")
         grads = _glu_weights(g, dW_gate, dW_up, dW_down)[:3]
     shape, dev, bf16 = (g.info.n_nodes, 128), g.info.device, W_gate.dtype
-    _check(load().dg4_glu_bwd(g.handle, ctypes.byref(dsc), *_row(X, "X", shape, dev, bf16), *weights, activation,
+    _check(load().dg4_glu_bwd(g.handle, dsc, *_row(X, "X", shape, dev, bf16), *weights, activation,
                               *_row(dY, "dY", shape, dev, bf16), *_row(dX, "dX", shape, dev, bf16), *grads,
                               *_workspace(workspace, dev), _stream(stream, dev)))
 
@@ -631,7 +633,7 @@ def dg4_add_norm_fwd(g: Graph, dsc: dg4_desc, X, R, gamma, beta, eps, Z, Y, stre
     """Z = X + R, Y = Norm(Z); R, beta and Z may be None."""
     vecs = _vec(gamma, 1, g), _vec(beta, 1, g)
     shape, dev, dtype = (g.info.n_nodes, 128), g.info.device, _row_type(dsc)
-    _check(load().dg4_add_norm_fwd(g.handle, ctypes.byref(dsc), *_row(X, "X", shape, dev, dtype),
+    _check(load().dg4_add_norm_fwd(g.handle, dsc, *_row(X, "X", shape, dev, dtype),
                                    *_row(R, "R", shape, dev, dtype), *vecs, eps, *_row(Z, "Z", shape, dev, dtype),
                                    *_row(Y, "Y", shape, dev, dtype), _stream(stream, dev)))
 
@@ -644,7 +646,7 @@ def dg4_norm_bwd(g: Graph, dsc: dg4_desc, Z, gamma, eps, dY, D_res, dZ, dgamma, 
     """dZ = D_res + the gradient of Norm at Z for dY, and gamma's and beta's gradients; D_res and each output may be None."""
     gamma_, dgamma_, dbeta_ = _vec(gamma, 1, g), _vec(dgamma, 1, g), _vec(dbeta, 1, g)
     shape, dev, dtype = (g.info.n_nodes, 128), g.info.device, _row_type(dsc)
-    _check(load().dg4_norm_bwd(g.handle, ctypes.byref(dsc), *_row(Z, "Z", shape, dev, dtype), gamma_, eps,
+    _check(load().dg4_norm_bwd(g.handle, dsc, *_row(Z, "Z", shape, dev, dtype), gamma_, eps,
                                *_row(dY, "dY", shape, dev, dtype), *_row(D_res, "D_res", shape, dev, dtype),
                                *_row(dZ, "dZ", shape, dev, dtype), dgamma_, dbeta_, *_workspace(workspace, dev),
                                _stream(stream, dev)))
