@@ -524,7 +524,7 @@ dg4_status dg4_norm_gate_fwd(const dg4_graph* g, const dg4_desc* desc, const voi
  *
  * The gated feed-forward sub-layer and the norm of a residual sum, each with its backward pass.  Pre-norm they are used as
  *     N = Norm(H),  H' = H + GLU(N)            dN = GLU_bwd(dH'),  dH = dH' + Norm_bwd(dN)
- * and post-norm as  Z = H + GLU(H),  H' = Norm(Z).  (Sec. 3.5 keeps the Transformer block around the restricted attention;
+ * and post-norm as  Z = H + GLU(H),  H' = Norm(Z),  where dH = dZ + GLU_bwd(dZ) is the caller's sum.  (Sec. 3.5 keeps the Transformer block around the restricted attention;
  * a gated sub-layer in the place of its feed-forward one has no counterpart in the paper.)  The calls take all rows of the
  * handle (an edgeless one will do), enqueue on `stream`, allocate nothing, keep nothing between calls and can be captured;
  * calls on different streams are independent if their workspaces are different ones.  Gradients are overwritten, not added

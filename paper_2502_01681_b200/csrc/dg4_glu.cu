@@ -21,7 +21,7 @@
 // Rounding: the hidden values (act(G) U; dG, dU) go into the second products in bf16, the type of the operands they meet, off
 // by at most 2^-8 of themselves; everything else (products, activations, sums over rows and blocks) is held in 32 bits.
 //
-// 1.01M rows, d_ff = 512, SiLU, back to back: forward 405 us (980 TFLOP/s, 58 % of the measured burst rate), gradients 1 475 to
+// 1.01M rows, d_ff = 512, SiLU, back to back: forward 405 to 413 us (980 TFLOP/s, 58 % of the measured burst rate), gradients 1 475 to
 // 1 490 us; the board is at its 1 kW then and the clock at 1.5 to 1.65 of 1.97 GHz.  In short runs on 208 384 rows 76 us forward,
 // 112 for dX and 172 for the weights (back to back 84, 128 and 185).  d_ff = 2048 on 101 000 rows: 120 to 123 us (1 300 TFLOP/s).
 
