@@ -167,3 +167,20 @@ def test_workspace_sizes_are_the_handle_s_whichever_device_is_current():
         assert (dg4.dg4_glu_bwd_workspace_bytes(g, d, 512), dg4.dg4_norm_bwd_workspace_bytes(g, d)) == want
     finally:
         dg4.dg4_debug_override_current_device(-1)
+
+
+def test_several_rounds_of_row_groups_beside_dx():
+    """128 blocks and 2 345 tiles: three groups one after the other on the SMs that one group takes."""
+    n, d_ff = 300033, 8192
+    x, wg, wu, wd = glu_case(220, n, d_ff)
+    dy = normal(221, (n, 128))
+    g, d = edgeless(n), desc()
+    size = dg4.dg4_glu_bwd_workspace_bytes(g, d, d_ff)
+    assert size > dg4.dg4_glu_bwd_workspace_bytes(edgeless(131072), d, d_ff) == 0
+    ws, out, parts = workspace(size), glu_grads(x, wg, wu, wd), glu_grads(x, wg, wu, wd)
+    for _ in range(2):
+        dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["gelu"], dy, *out, ws)
+    dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["gelu"], dy, parts[0], None, None, None, None)
+    dg4.dg4_glu_bwd(g, d, x, wg, wu, wd, ACT["gelu"], dy, None, *parts[1:], ws)
+    assert all(torch.equal(p, q) for p, q in zip(out, parts)) and all(bool(torch.isfinite(t).all()) for t in out)
+    assert dg4.dg4_graph_poll_status(g) == dg4.DG4_OK
